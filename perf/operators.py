@@ -1,0 +1,772 @@
+"""Cases the operators of a Boss block of experts are timed on: routing, the experts' products, their combination,
+dropout -- each in the direction and type that the case says.
+
+A case is a dict of plain values; its "op" says which call a pass makes:
+
+  route          scores, choice and weights of each row's experts, and the (row, choice) pairs grouped by expert
+  route_grad     gradient of the logits
+  forward        product of the grouped rows with their experts' matrices, with the activation
+  grad_input     gradient of the grouped rows, through the activation that made them
+  grad_weight    gradient of the experts' matrices
+  combine        weighted sum of the experts' rows of each row, with dropout and the residual
+  combine_grad   gradient of the experts' rows and of the weights
+  dropout        dropout from the counter-based generator, with or without a residual
+
+Where `own` is false `run` is the plain form in elementary torch operations, in 32 bits (scores that decide a choice in
+64); where it is true `run` calls the framework.  `exact` is the definition in 64 bits.  All inputs are drawn on the GPU
+from the seed.
+"""
+import math
+
+import torch
+
+own = False
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+BYTES = {"f32": 4, "bf16": 2, "f16": 2}
+DROP_SEED, DROP_STEP = 1905, (7 << 32) + 3
+
+
+def listed():
+    return [
+        # A few rows answered one step at a time, 64 experts: launch and latency, nothing else.
+        {"name": "route_few_rows", "op": "route", "n": 5, "kept": 5, "E": 64, "K": 6, "dtype": "bf16",
+         "score": "softmax", "groups": 1, "top_groups": 1, "group_best": 1, "renorm": True, "scale": 1.0,
+         "bias": False, "masked": 0.0},
+        # A training batch of the benchmark's pool size, 256 experts in 8 groups, chosen with the balance bias.
+        {"name": "route_groups", "op": "route", "n": 16_384, "kept": 16_384, "E": 256, "K": 8, "dtype": "f32",
+         "score": "sigmoid", "groups": 8, "top_groups": 4, "group_best": 2, "renorm": True, "scale": 2.5,
+         "bias": True, "masked": 0.0},
+        # The routing's backward pass where it is widest: softmax without renormalisation reaches every logit; some
+        # experts are masked, some rows altogether.
+        {"name": "route_grad_softmax", "op": "route_grad", "n": 65_536, "kept": 60_001, "E": 128, "K": 2,
+         "dtype": "f16", "score": "softmax", "groups": 1, "top_groups": 1, "group_best": 1, "renorm": False,
+         "scale": 1.0, "bias": False, "masked": 0.02},
+        # One row through its experts' gated product: eight matrices are read for eight rows.
+        {"name": "forward_one_row", "op": "forward", "n": 1, "E": 64, "K": 8, "d_in": 2048, "d_out": 1024,
+         "act": "gated", "pre": False, "dtype": "bf16", "shared": True, "skew": 0.5},
+        # A serving batch: a few rows for each expert, the matrices still the larger part of what is read.
+        {"name": "forward_serving", "op": "forward", "n": 200, "E": 32, "K": 4, "d_in": 1024, "d_out": 2048,
+         "act": "none", "pre": False, "dtype": "f16", "shared": True, "skew": 0.5},
+        # The gated product of a training step, with what its backward pass needs; uneven experts.
+        {"name": "forward_gated", "op": "forward", "n": 8192, "E": 64, "K": 8, "d_in": 2048, "d_out": 1024,
+         "act": "gated", "pre": True, "dtype": "bf16", "shared": True, "skew": 0.5},
+        # The rows' gradient of the second product of a relu block, widths that fill no tile.
+        {"name": "grad_input_odd", "op": "grad_input", "n": 6001, "E": 16, "K": 2, "d_in": 1000, "d_out": 520,
+         "act": "relu", "dtype": "bf16", "shared": False, "skew": 1.0},
+        # The matrices' gradient of the training step above.
+        {"name": "grad_weight", "op": "grad_weight", "n": 8192, "E": 64, "K": 8, "d_in": 1024, "d_out": 2048,
+         "act": "none", "dtype": "bf16", "shared": False, "skew": 0.5, "out": "same"},
+        # The end of a training step's block: eight rows a token, dropout, residual.
+        {"name": "combine_dropout", "op": "combine", "n": 8192, "kept": 8000, "E": 64, "K": 8, "d": 2048,
+         "dtype": "bf16", "p": 0.1, "weights": True, "residual": True, "skew": 0.5},
+        # Its backward pass.
+        {"name": "combine_grad", "op": "combine_grad", "n": 8192, "kept": 8192, "E": 64, "K": 8, "d": 2048,
+         "dtype": "bf16", "p": 0.1, "weights": True, "residual": False, "skew": 0.5},
+        # Dropout of a few short rows of odd width, as at the end of a sublayer in small batches.
+        {"name": "dropout_few_rows", "op": "dropout", "n": 33, "kept": 33, "d": 517, "dtype": "f32", "p": 0.1,
+         "residual": False},
+        # Dropout and residual over the activations of a large batch.
+        {"name": "dropout_residual", "op": "dropout", "n": 65_536, "kept": 65_536, "d": 2048, "dtype": "bf16",
+         "p": 0.1, "residual": True},
+    ]
+
+
+MOST_FLOPS = 2 * 8192 * 8 * 2048 * 2048  # of the largest listed product
+
+
+def _log(rng, lo, hi):
+    """A whole number from lo to hi, even over its logarithm."""
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def _width(rng, lo, hi):
+    """A row width: powers of two, odd multiples of eight, odd ones."""
+    kind = rng.random()
+    if kind < 0.35:
+        return min(hi, 1 << rng.randint(lo.bit_length() - 1, hi.bit_length() - 1))
+    if kind < 0.8:
+        return min(hi, 8 * (_log(rng, max(1, lo // 8), hi // 8) | 1))
+    return min(hi - 1, _log(rng, lo, hi) | 1)
+
+
+def draw(rng):
+    op = rng.choice(["route", "route", "route_grad", "forward", "forward", "forward", "grad_input", "grad_weight",
+                     "combine", "combine_grad", "dropout"])
+    if op in ("route", "route_grad"):
+        E = rng.choice([4, 8, 16, 64, 128, 256]) if rng.random() < 0.6 else _log(rng, 2, 320)
+        n = _log(rng, 1, min(65_536, (1 << 23) // E))
+        groups, top_groups, group_best = 1, 1, 1
+        parts = [g for g in (2, 4, 8, 16) if E % g == 0 and E // g >= 2]
+        if parts and rng.random() < 0.5:
+            groups = rng.choice(parts)
+            top_groups, group_best = rng.randint(1, groups), rng.randint(1, 2)
+        K = min(_log(rng, 1, 12), top_groups * (E // groups))
+        return {"op": op, "n": n, "kept": n if rng.random() < 0.6 else rng.randint(0, n), "E": E, "K": K,
+                "dtype": rng.choice(["f32", "bf16", "f16"]), "score": rng.choice(["softmax", "sigmoid"]),
+                "groups": groups, "top_groups": top_groups, "group_best": group_best, "renorm": rng.random() < 0.6,
+                "scale": rng.choice([1.0, 2.5]), "bias": rng.random() < 0.5,
+                "masked": rng.choice([0.0, 0.0, 0.02, 0.4])}
+    if op == "dropout":
+        d = _width(rng, 16, 4096)
+        n = _log(rng, 1, min(65_536, (1 << 26) // d))
+        return {"op": op, "n": n, "kept": n if rng.random() < 0.6 else rng.randint(0, n), "d": d,
+                "dtype": rng.choice(["f32", "bf16", "f16"]), "p": rng.choice([0.0, 0.1, 0.3, 0.5]),
+                "residual": rng.random() < 0.5}
+    E = rng.choice([1, 4, 8, 16, 32, 64])
+    K = rng.randint(1, min(8, E))
+    if op in ("combine", "combine_grad"):
+        d = _width(rng, 16, 4096)
+        n = _log(rng, 1, min(20_000, (1 << 26) // (d * K)))
+        return {"op": op, "n": n, "kept": n if rng.random() < 0.6 else rng.randint(0, n), "E": E, "K": K, "d": d,
+                "dtype": rng.choice(["f32", "bf16", "f16"]), "p": rng.choice([0.0, 0.1, 0.3]),
+                "weights": rng.random() < 0.8, "residual": op == "combine" and rng.random() < 0.6,
+                "skew": rng.choice([0.0, 0.5, 1.0])}
+    d_in, d_out = _width(rng, 64, 4096), _width(rng, 64, 4096)
+    while E * d_in * d_out > (1 << 28):
+        E, K = E // 2, min(K, E // 2)
+    act = rng.choice(["none", "relu", "gated"])
+    twice = 2 if act == "gated" and op != "grad_weight" else 1
+    n = _log(rng, 1, max(1, min(20_000, MOST_FLOPS // (2 * K * d_in * d_out * twice))))
+    case = {"op": op, "n": n, "E": E, "K": K, "d_in": d_in, "d_out": d_out, "act": act,
+            "dtype": rng.choice(["bf16", "bf16", "f16"]), "shared": rng.random() < 0.5,
+            "skew": rng.choice([0.0, 0.5, 1.0])}
+    if op == "forward":
+        case["pre"] = act == "gated" and rng.random() < 0.5
+    if op == "grad_input":
+        case["shared"] = False
+    if op == "grad_weight":
+        case["act"], case["out"] = "none", rng.choice(["same", "f32"])
+    return case
+
+
+# ---------------------------------------------------------------------------
+# inputs
+
+
+def _gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed) * 7919 + 29)
+    return g
+
+
+def _normal(g, *shape, dtype=torch.float32, scale=1.0):
+    """Normal values; large tensors in slices, so that no 32-bit copy of the whole is held."""
+    out = torch.empty(*shape, dtype=dtype, device="cuda")
+    flat = out.view(-1)
+    for lo in range(0, flat.numel(), 1 << 26):
+        hi = min(flat.numel(), lo + (1 << 26))
+        flat[lo:hi] = torch.randn(hi - lo, generator=g, device="cuda") * scale
+    return out
+
+
+def _routing_logits(c, g):
+    """Logits of a router that has learned to prefer some experts; a share of the entries masked, some rows whole."""
+    x = torch.randn(c["n"], c["E"], generator=g, device="cuda") * 1.5
+    x += 0.5 * torch.randn(c["E"], generator=g, device="cuda")
+    if c["masked"] > 0:
+        x[torch.rand(c["n"], c["E"], generator=g, device="cuda") < c["masked"]] = -math.inf
+        x[torch.rand(c["n"], generator=g, device="cuda") < 0.01] = -math.inf
+    return x.to(DTYPES[c["dtype"]])
+
+
+def _plan(n, E, K, skew, g):
+    """Distinct experts for each row, some more wanted than others, and the pairs grouped by expert."""
+    want = torch.randn(n, E, generator=g, device="cuda") + skew * torch.randn(E, generator=g, device="cuda")
+    ids = torch.argsort(want, dim=1, descending=True)[:, :K].to(torch.int32).contiguous()
+    flat = ids.view(-1).long()
+    order = torch.argsort(flat, stable=True).to(torch.int32)
+    counts = torch.bincount(flat, minlength=E)
+    offsets = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    offsets[1:] = torch.cumsum(counts, 0)
+    slot = torch.empty(n * K, dtype=torch.int32, device="cuda")
+    slot[order.long()] = torch.arange(n * K, dtype=torch.int32, device="cuda")
+    return ids, order, offsets, slot.view(n, K), [int(v) for v in counts.tolist()]
+
+
+def _inputs(c, seed):
+    """The inputs of a pass, and nothing else."""
+    g, op = _gen(seed), c["op"]
+    s = {"case": c}
+    if "kept" in c:
+        s["count"] = torch.full((1,), c["kept"], dtype=torch.int32, device="cuda")
+    if op in ("route", "route_grad"):
+        s["logits"] = _routing_logits(c, g)
+        s["bias"] = 0.1 * torch.randn(c["E"], generator=g, device="cuda") if c["bias"] else None
+        if op == "route_grad":
+            s["ids"] = _choice(s)[0]
+            s["dweights"] = torch.randn(c["n"], c["K"], generator=g, device="cuda")
+        return s
+    dt = DTYPES[c["dtype"]]
+    if op == "dropout":
+        s["x"] = _normal(g, c["n"], c["d"], dtype=dt)
+        s["residual"] = _normal(g, c["n"], c["d"], dtype=dt) if c["residual"] else None
+        return s
+    s["ids"], s["order"], s["offsets"], s["slot"], s["counts"] = _plan(c["n"], c["E"], c["K"], c["skew"], g)
+    R = c["n"] * c["K"]
+    if op in ("combine", "combine_grad"):
+        s["y"] = _normal(g, R, c["d"], dtype=dt)
+        s["weights"] = None
+        if c["weights"]:
+            w = torch.rand(c["n"], c["K"], generator=g, device="cuda") + 0.05
+            s["weights"] = w / w.sum(1, keepdim=True)
+        s["residual"] = _normal(g, c["n"], c["d"], dtype=dt) if c["residual"] else None
+        if op == "combine_grad":
+            s["dout"] = _normal(g, c["n"], c["d"], dtype=dt)
+        return s
+    d_in, d_out, gated = c["d_in"], c["d_out"], c["act"] == "gated"
+    if op == "forward":
+        s["x"] = _normal(g, c["n"] if c["shared"] else R, d_in, dtype=dt)
+        s["w"] = _normal(g, c["E"], d_out * (2 if gated else 1), d_in, dtype=dt, scale=d_in ** -0.5)
+    elif op == "grad_input":
+        s["dout"] = _normal(g, R, d_out, dtype=dt)
+        s["w"] = _normal(g, c["E"], d_out, d_in, dtype=dt, scale=d_out ** -0.5)
+        s["saved"] = None
+        if c["act"] == "relu":
+            s["saved"] = _normal(g, R, d_in, dtype=dt).clamp_(min=0)
+        elif gated:
+            s["saved"] = _normal(g, R, 2 * d_in, dtype=dt)
+    else:
+        s["dout"] = _normal(g, R, d_out, dtype=dt)
+        s["x"] = _normal(g, c["n"] if c["shared"] else R, d_in, dtype=dt)
+    return s
+
+
+def _grad_dtype(c):
+    return torch.float32 if c["out"] == "f32" else DTYPES[c["dtype"]]
+
+
+def prepare(case, seed):
+    s = _inputs(case, seed)
+    if not own:
+        return s
+    from paper_1905_03381_amd import api
+    c, op = case, case["op"]
+    s["api"] = api
+    empty = lambda *shape, dtype: torch.zeros(*shape, dtype=dtype, device="cuda")
+    if op in ("route", "route_grad"):
+        s["cfg"] = api.route_config(c["score"], c["K"], n_groups=c["groups"], top_groups=c["top_groups"],
+                                    group_best=c["group_best"], renormalise=c["renorm"], scale=c["scale"])
+        if op == "route":
+            R = c["n"] * c["K"]
+            s["out"] = {"ids": empty(c["n"], c["K"], dtype=torch.int32),
+                        "weights": empty(c["n"], c["K"], dtype=torch.float32),
+                        "offsets": empty(c["E"] + 1, dtype=torch.int32), "order": empty(R, dtype=torch.int32),
+                        "slot": empty(c["n"], c["K"], dtype=torch.int32)}
+            s["ws"] = api.ExpertWorkspace(c["n"], c["K"], c["E"])
+        else:
+            s["out"] = {"dlogits": torch.zeros_like(s["logits"])}
+    elif op == "dropout":
+        s["out"] = {"out": torch.zeros_like(s["x"])}
+    elif op == "combine":
+        s["out"] = {"out": empty(c["n"], c["d"], dtype=DTYPES[c["dtype"]])}
+    elif op == "combine_grad":
+        s["out"] = {"dy": torch.zeros_like(s["y"])}
+        if c["weights"]:
+            s["out"]["dweights"] = empty(c["n"], c["K"], dtype=torch.float32)
+    elif op == "forward":
+        R, dt = c["n"] * c["K"], DTYPES[c["dtype"]]
+        s["out"] = {"out": empty(R, c["d_out"], dtype=dt)}
+        if c["pre"]:
+            s["out"]["pre"] = empty(R, 2 * c["d_out"], dtype=dt)
+    elif op == "grad_input":
+        R, dt = c["n"] * c["K"], DTYPES[c["dtype"]]
+        s["out"] = {"dx": empty(R, c["d_in"] * (2 if c["act"] == "gated" else 1), dtype=dt)}
+    else:
+        s["out"] = {"dw": empty(c["E"], c["d_out"], c["d_in"], dtype=_grad_dtype(c))}
+        s["ws"] = api.ExpertWorkspace(c["n"], c["K"], c["E"])
+    return s
+
+
+# ---------------------------------------------------------------------------
+# the framework's calls
+
+
+def _run_own(s):
+    api, c, out = s["api"], s["case"], s["out"]
+    op = c["op"]
+    if op == "route":
+        api.route(s["logits"], s["count"], s["bias"], s["cfg"], out["ids"], out["weights"],
+                  (out["offsets"], out["order"], out["slot"]), s["ws"])
+    elif op == "route_grad":
+        api.route_grad(s["logits"], s["count"], s["cfg"], s["ids"], s["dweights"], out["dlogits"])
+    elif op == "forward":
+        api.expert_forward(s["x"], s["order"] if c["shared"] else None, c["K"], s["offsets"], s["w"], c["act"],
+                           out["out"], out.get("pre"))
+    elif op == "grad_input":
+        api.expert_grad_input(s["dout"], s["offsets"], s["w"], c["act"], s["saved"], out["dx"])
+    elif op == "grad_weight":
+        api.expert_grad_weight(s["dout"], s["x"], s["order"] if c["shared"] else None, c["K"], s["offsets"],
+                               out["dw"], False, s["ws"])
+    elif op == "combine":
+        api.expert_combine(s["y"], s["slot"], s["weights"], s["count"], s["residual"], c["p"], DROP_SEED, DROP_STEP,
+                           out["out"])
+    elif op == "combine_grad":
+        api.expert_combine_grad(s["dout"], s["y"], s["slot"], s["weights"], s["count"], c["p"], DROP_SEED, DROP_STEP,
+                                out["dy"], out.get("dweights"))
+    else:
+        api.dropout(s["x"], s["count"], s["residual"], c["p"], DROP_SEED, DROP_STEP, out["out"])
+    return out
+
+
+# ---------------------------------------------------------------------------
+# the plain forms
+
+
+def _scores(x, kind):
+    """Scores in 64 bits and what can be chosen; -inf and NaN logits take an expert out."""
+    x = x.double()
+    free = x > -math.inf
+    if kind == "sigmoid":
+        return torch.where(free, torch.sigmoid(x), 0.0), free
+    top = torch.where(free, x, -math.inf).amax(1, keepdim=True)
+    e = torch.where(free, torch.exp(x - top), 0.0)
+    return e / e.sum(1, keepdim=True).clamp(min=1e-300), free
+
+
+def _choice(s):
+    """ids and weights of every row, kept or not."""
+    c = s["case"]
+    n, E, K, G = c["n"], c["E"], c["K"], c["groups"]
+    score, free = _scores(s["logits"], c["score"])
+    want = score if s["bias"] is None else score + s["bias"].double()
+    want = torch.where(free, want, -math.inf)
+    if G > 1:
+        best = torch.sort(want.view(n, G, E // G), dim=2, descending=True, stable=True).values[:, :, :c["group_best"]]
+        value = torch.where(best == -math.inf, 0.0, best).sum(2)
+        value = torch.where(best[:, :, 0] == -math.inf, -math.inf, value)
+        rank = torch.sort(value, dim=1, descending=True, stable=True).indices[:, :c["top_groups"]]
+        taken = torch.zeros(n, G, dtype=torch.bool, device="cuda").scatter_(1, rank, True)
+        want = torch.where(taken.repeat_interleave(E // G, dim=1), want, -math.inf)
+    top, ids = torch.sort(want, dim=1, descending=True, stable=True)
+    top, ids = top[:, :K], ids[:, :K]
+    there = top > -math.inf
+    w = torch.where(there, score.gather(1, ids), 0.0)
+    if c["renorm"]:
+        total = w.sum(1, keepdim=True)
+        w = torch.where(total > 0, w / total, 0.0)
+    return torch.where(there, ids, -1).to(torch.int32), (w * c["scale"]).float()
+
+
+def _run_route(s):
+    c = s["case"]
+    n, E, K, m = c["n"], c["E"], c["K"], c["kept"]
+    ids, weights = _choice(s)
+    ids, weights = ids.clone(), weights.clone()
+    ids[m:], weights[m:] = 0, 0.0
+    key = torch.full((n, K), E, dtype=torch.int64, device="cuda")
+    key[:m] = torch.where(ids[:m] < 0, E, ids[:m].long())
+    by, flat = torch.sort(key.view(-1), stable=True)
+    offsets = (by.view(1, -1) < torch.arange(E + 1, device="cuda").view(-1, 1)).sum(1).to(torch.int32) \
+        if E * n * K < (1 << 28) else torch.searchsorted(by, torch.arange(E + 1, device="cuda")).to(torch.int32)
+    total = by < E
+    order = torch.where(total, flat, 0).to(torch.int32)
+    slot = torch.zeros(n * K, dtype=torch.int32, device="cuda")
+    slot[flat] = torch.where(total, torch.arange(n * K, device="cuda"), -1).to(torch.int32)
+    slot = slot.view(n, K)
+    slot[m:] = 0
+    return {"ids": ids, "weights": weights, "offsets": offsets, "order": order, "slot": slot}
+
+
+def _run_route_grad(s):
+    c = s["case"]
+    ids, there = s["ids"].clamp(min=0).long(), s["ids"] >= 0
+    score, free = _scores(s["logits"], c["score"])
+    score = score.float()
+    a = torch.where(there, s["dweights"] * c["scale"], 0.0)
+    chosen = torch.where(there, score.gather(1, ids), 0.0)
+    ds = a
+    if c["renorm"]:
+        total = chosen.sum(1, keepdim=True)
+        ds = (a - (a * chosen).sum(1, keepdim=True) / total) / total
+        ds = torch.where(there & (total > 0), ds, 0.0)
+    full = torch.zeros_like(score).scatter_add_(1, ids, ds)
+    if c["score"] == "sigmoid":
+        d = full * score * (1 - score)
+    else:
+        d = score * (full - (ds * chosen).sum(1, keepdim=True))
+    d = torch.where(free, d, 0.0)
+    d[c["kept"]:] = 0
+    return {"dlogits": d.to(s["logits"].dtype)}
+
+
+def _segments(s):
+    """(expert, first, last) of the groups that hold rows."""
+    lo = 0
+    for e, k in enumerate(s["counts"]):
+        if k:
+            yield e, lo, lo + k
+        lo += k
+
+
+def _rows(s, x, lo, hi):
+    c = s["case"]
+    if not c["shared"]:
+        return x[lo:hi]
+    return x[(s["order"][lo:hi] // c["K"]).long()]
+
+
+def _run_forward(s):
+    c, dt = s["case"], s["x"].dtype
+    R, f = c["n"] * c["K"], c["d_out"]
+    out = {"out": torch.zeros(R, f, dtype=dt, device="cuda")}
+    if c["pre"]:
+        out["pre"] = torch.zeros(R, 2 * f, dtype=dt, device="cuda")
+    for e, lo, hi in _segments(s):
+        h = _rows(s, s["x"], lo, hi).float() @ s["w"][e].float().t()
+        if c["act"] == "relu":
+            out["out"][lo:hi] = h.clamp(min=0)
+        elif c["act"] == "gated":
+            out["out"][lo:hi] = h[:, :f] / (1 + torch.exp(-h[:, :f])) * h[:, f:]
+            if c["pre"]:
+                out["pre"][lo:hi] = h
+        else:
+            out["out"][lo:hi] = h
+    return out
+
+
+def _run_grad_input(s):
+    c, dt = s["case"], s["dout"].dtype
+    R, f = c["n"] * c["K"], c["d_in"]
+    dx = torch.zeros(R, f * (2 if c["act"] == "gated" else 1), dtype=dt, device="cuda")
+    for e, lo, hi in _segments(s):
+        d = s["dout"][lo:hi].float() @ s["w"][e].float()
+        if c["act"] == "relu":
+            d = torch.where(s["saved"][lo:hi] > 0, d, 0.0)
+        elif c["act"] == "gated":
+            gate, up = s["saved"][lo:hi, :f].float(), s["saved"][lo:hi, f:].float()
+            sig = 1 / (1 + torch.exp(-gate))
+            d = torch.cat([d * up * sig * (1 + gate * (1 - sig)), d * gate * sig], dim=1)
+        dx[lo:hi] = d
+    return {"dx": dx}
+
+
+def _run_grad_weight(s):
+    c = s["case"]
+    dw = torch.zeros(c["E"], c["d_out"], c["d_in"], dtype=_grad_dtype(c), device="cuda")
+    for e, lo, hi in _segments(s):
+        dw[e] = s["dout"][lo:hi].float().t() @ _rows(s, s["x"], lo, hi).float()
+    return {"dw": dw}
+
+
+def _mul32(a, b):
+    """High and low word of the product of two 32-bit words held in 64-bit integers."""
+    p = a * b  # wraps beyond 63 bits: the bits are those of the product
+    return (p >> 32) & 0xFFFFFFFF, p & 0xFFFFFFFF
+
+
+def _kept_elements(rows, d, p):
+    """keep[rows, d] and the scale of what is kept: Philox4x32-10 on (column / 8, row + 1, step), eight 16-bit draws."""
+    limit = round(65536 * (1.0 - float(torch.tensor(p, dtype=torch.float32))))
+    groups = (d + 7) // 8
+    c0 = torch.arange(groups, dtype=torch.int64, device="cuda").view(1, -1).expand(rows, groups)
+    c1 = torch.arange(1, rows + 1, dtype=torch.int64, device="cuda").view(-1, 1).expand(rows, groups)
+    c2 = torch.full_like(c0, DROP_STEP & 0xFFFFFFFF)
+    c3 = torch.full_like(c0, DROP_STEP >> 32)
+    k0, k1 = DROP_SEED & 0xFFFFFFFF, DROP_SEED >> 32
+    for _ in range(10):
+        hi0, lo0 = _mul32(c0, 0xD2511F53)
+        hi1, lo1 = _mul32(c2, 0xCD9E8D57)
+        c0, c1, c2, c3 = hi1 ^ c1 ^ k0, lo1, hi0 ^ c3 ^ k1, lo0
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    draws = torch.empty(rows, groups, 8, dtype=torch.bool, device="cuda")
+    for i, w in enumerate((c0, c1, c2, c3)):
+        draws[:, :, 2 * i] = (w & 0xFFFF) < limit
+        draws[:, :, 2 * i + 1] = (w >> 16) < limit
+    return draws.view(rows, groups * 8)[:, :d], 65536.0 / limit if limit else 0.0
+
+
+def _dropped(x, p):
+    if p == 0:
+        return x
+    keep, scale = _kept_elements(*x.shape, p)
+    return torch.where(keep, x * scale, 0.0)
+
+
+def _run_dropout(s):
+    c, m = s["case"], s["case"]["kept"]
+    out = torch.zeros_like(s["x"])
+    v = _dropped(s["x"][:m].float(), c["p"])
+    out[:m] = v if s["residual"] is None else v + s["residual"][:m].float()
+    return {"out": out}
+
+
+def _run_combine(s):
+    c, m = s["case"], s["case"]["kept"]
+    total = torch.zeros(m, c["d"], dtype=torch.float32, device="cuda")
+    for k in range(c["K"]):
+        term = s["y"][s["slot"][:m, k].long()].float()
+        total += term if s["weights"] is None else term * s["weights"][:m, k:k + 1]
+    total = _dropped(total, c["p"])
+    out = torch.zeros(c["n"], c["d"], dtype=s["y"].dtype, device="cuda")
+    out[:m] = total if s["residual"] is None else total + s["residual"][:m].float()
+    return {"out": out}
+
+
+def _run_combine_grad(s):
+    c, m = s["case"], s["case"]["kept"]
+    g = _dropped(s["dout"][:m].float(), c["p"])
+    out = {"dy": torch.zeros_like(s["y"])}
+    if c["weights"]:
+        out["dweights"] = torch.zeros(c["n"], c["K"], dtype=torch.float32, device="cuda")
+    for k in range(c["K"]):
+        at = s["slot"][:m, k].long()
+        out["dy"][at] = (g if s["weights"] is None else g * s["weights"][:m, k:k + 1]).to(s["y"].dtype)
+        if c["weights"]:
+            out["dweights"][:m, k] = (s["y"][at].float() * g).sum(1)
+    return out
+
+
+def run(state):
+    if own:
+        return _run_own(state)
+    return {"route": _run_route, "route_grad": _run_route_grad, "forward": _run_forward,
+            "grad_input": _run_grad_input, "grad_weight": _run_grad_weight, "combine": _run_combine,
+            "combine_grad": _run_combine_grad, "dropout": _run_dropout}[state["case"]["op"]](state)
+
+
+def work(case):
+    c, op, b = case, case["op"], BYTES[case["dtype"]]
+    if op == "route":  # logits in, ids and weights and the plan out
+        m = c["kept"]
+        return {"bytes": m * c["E"] * b + m * c["K"] * 16 + 4 * (c["E"] + 1), "flops": 4 * m * c["E"]}
+    if op == "route_grad":
+        m = c["kept"]
+        return {"bytes": 2 * m * c["E"] * b + m * c["K"] * 8, "flops": 6 * m * c["E"]}
+    if op == "dropout":
+        e = c["kept"] * c["d"]
+        return {"bytes": e * b * (3 if c["residual"] else 2), "flops": 2 * e}
+    if op in ("combine", "combine_grad"):
+        e = c["kept"] * c["d"]
+        pair = c["kept"] * c["K"] * (4 + (4 if c["weights"] else 0))
+        if op == "combine":
+            return {"bytes": e * b * (c["K"] + 1 + c["residual"]) + pair, "flops": 2 * e * c["K"]}
+        rows = 2 if c["weights"] else 1
+        return {"bytes": e * b * (1 + rows * c["K"]) + pair + (4 * c["kept"] * c["K"] if c["weights"] else 0),
+                "flops": 3 * e * c["K"]}
+    R, live = c["n"] * c["K"], min(c["E"], c["n"] * c["K"])
+    gated = 2 if c["act"] == "gated" else 1
+    rows_in = c["n"] if c["shared"] else R
+    if op == "forward":
+        weights = live * gated * c["d_out"] * c["d_in"]
+        out = R * c["d_out"] * (1 + (2 if c["pre"] else 0))
+        return {"bytes": b * (rows_in * c["d_in"] + weights + out) + 4 * R, "flops": 2 * R * c["d_in"] * c["d_out"] * gated}
+    if op == "grad_input":
+        saved = {"none": 0, "relu": 1, "gated": 2}[c["act"]] * R * c["d_in"]
+        return {"bytes": b * (R * c["d_out"] + live * c["d_out"] * c["d_in"] + saved + R * c["d_in"] * gated),
+                "flops": 2 * R * c["d_in"] * c["d_out"]}
+    ob = 4 if c["out"] == "f32" else b
+    return {"bytes": b * (R * c["d_out"] + rows_in * c["d_in"]) + ob * c["E"] * c["d_out"] * c["d_in"] + 4 * R,
+            "flops": 2 * R * c["d_in"] * c["d_out"]}
+
+
+# ---------------------------------------------------------------------------
+# the definitions in 64 bits
+
+
+def _exact_route(c, s):
+    n, E, K, m, G = c["n"], c["E"], c["K"], c["kept"], c["groups"]
+    x = s["logits"].to(torch.float64)
+    out_of = torch.isnan(x) | torch.isinf(x)  # the inputs hold no +inf
+    x = x.masked_fill(out_of, -1e4)
+    if c["score"] == "softmax":
+        p = torch.exp(x - x.max(1, keepdim=True).values).masked_fill(out_of, 0.0)
+        p = p / p.sum(1, keepdim=True).masked_fill(p.sum(1, keepdim=True) == 0, 1.0)
+    else:
+        p = (1.0 / (1.0 + torch.exp(-x))).masked_fill(out_of, 0.0)
+    v = p + (0.0 if s["bias"] is None else s["bias"].to(torch.float64))
+    v = v.masked_fill(out_of, -1e9)
+
+    def highest(t):  # value and lowest index of each row's maximum
+        top = t.max(1, keepdim=True).values
+        at = torch.arange(t.shape[1], device="cuda").expand_as(t)
+        return top[:, 0], torch.where(t == top, at, t.shape[1]).min(1).values
+
+    if G > 1:
+        left, value = v.clone(), torch.zeros(n, G, dtype=torch.float64, device="cuda")
+        has = torch.zeros(n, G, dtype=torch.bool, device="cuda")
+        for b in range(c["group_best"]):
+            for gi in range(G):
+                part = left[:, gi * (E // G):(gi + 1) * (E // G)]
+                top, at = highest(part)
+                ok = top > -1e8
+                value[:, gi] += torch.where(ok, top, 0.0)
+                has[:, gi] |= ok
+                part.scatter_(1, at.view(-1, 1), -1e9)
+        value = value.masked_fill(~has, -1e9)
+        allowed = torch.zeros(n, G, dtype=torch.bool, device="cuda")
+        for _ in range(c["top_groups"]):
+            _, at = highest(value)
+            allowed.scatter_(1, at.view(-1, 1), True)
+            value.scatter_(1, at.view(-1, 1), -2e9)
+        for gi in range(G):
+            v[:, gi * (E // G):(gi + 1) * (E // G)].masked_fill_(~allowed[:, gi:gi + 1], -1e9)
+    ids = torch.full((n, K), -1, dtype=torch.int32, device="cuda")
+    w = torch.zeros(n, K, dtype=torch.float64, device="cuda")
+    for k in range(K):
+        top, at = highest(v)
+        ok = top > -1e8
+        ids[:, k] = torch.where(ok, at, -1).to(torch.int32)
+        w[:, k] = torch.where(ok, p.gather(1, at.view(-1, 1))[:, 0], 0.0)
+        v.scatter_(1, at.view(-1, 1), -2e9)
+    if c["renorm"]:
+        w = w / w.sum(1, keepdim=True).masked_fill(w.sum(1, keepdim=True) == 0, 1.0)
+    w = w * c["scale"]
+    ids[m:], w[m:] = 0, 0.0
+    order = torch.zeros(n * K, dtype=torch.int32, device="cuda")
+    slot = torch.full((n * K,), -1, dtype=torch.int32, device="cuda")
+    offsets, lo, flat = [0], 0, ids[:m].reshape(-1)
+    for e in range(E):
+        at = torch.nonzero(flat == e)[:, 0]
+        order[lo:lo + at.numel()] = at.to(torch.int32)
+        slot[at] = torch.arange(lo, lo + at.numel(), dtype=torch.int32, device="cuda")
+        lo += at.numel()
+        offsets.append(lo)
+    slot = slot.view(n, K)
+    slot[m:] = 0
+    return {"ids": ids, "weights": w, "offsets": torch.tensor(offsets, dtype=torch.int32, device="cuda"),
+            "order": order, "slot": slot}
+
+
+def _exact_route_grad(c, s):
+    """By the chain rule with the whole Jacobian of the scores, a slice of the rows at a time."""
+    n, E, m = c["n"], c["E"], c["kept"]
+    d = torch.zeros(n, E, dtype=torch.float64, device="cuda")
+    step = max(1, (1 << 25) // (E * E))
+    for lo in range(0, m, step):
+        hi = min(m, lo + step)
+        x = s["logits"][lo:hi].to(torch.float64)
+        gone = torch.isinf(x)
+        ids = s["ids"][lo:hi]
+        pick = torch.zeros(hi - lo, c["K"], E, dtype=torch.float64, device="cuda")  # one-hot choices
+        pick.scatter_(2, ids.clamp(min=0).long().unsqueeze(2), 1.0)
+        pick *= (ids >= 0).unsqueeze(2)
+        dw = s["dweights"][lo:hi].to(torch.float64) * c["scale"]
+        if c["score"] == "softmax":
+            p = torch.exp(x - x.masked_fill(gone, -1e4).max(1, keepdim=True).values).masked_fill(gone, 0.0)
+            p = p / p.sum(1, keepdim=True).masked_fill(p.sum(1, keepdim=True) == 0, 1.0)
+            jac = torch.diag_embed(p) - p.unsqueeze(2) * p.unsqueeze(1)
+        else:
+            p = (1.0 / (1.0 + torch.exp(-x))).masked_fill(gone, 0.0)
+            jac = torch.diag_embed(p * (1.0 - p))
+        sel = (pick * p.unsqueeze(1)).sum(2)
+        if c["renorm"]:
+            total = sel.sum(1, keepdim=True).masked_fill(sel.sum(1, keepdim=True) == 0, 1.0)
+            g_sel = dw / total - (dw * sel).sum(1, keepdim=True) / total ** 2
+        else:
+            g_sel = dw
+        g_p = (pick * g_sel.unsqueeze(2)).sum(1)
+        d[lo:hi] = (jac * g_p.unsqueeze(1)).sum(2).masked_fill(gone, 0.0)
+    return {"dlogits": d}
+
+
+def _exact_product(c, s):
+    R, op, gated = c["n"] * c["K"], c["op"], c["act"] == "gated"
+    d_in, d_out = c["d_in"], c["d_out"]
+    f64 = lambda t: t.to(torch.float64)
+    zeros = lambda *shape: torch.zeros(*shape, dtype=torch.float64, device="cuda")
+    ends = s["offsets"].tolist()
+    source = s["order"].long()
+    if c["shared"]:
+        source = torch.div(source, c["K"], rounding_mode="floor")
+    else:
+        source = torch.arange(R, device="cuda")
+    if op == "forward":
+        out = {"out": zeros(R, d_out)}
+        if c["pre"]:
+            out["pre"] = zeros(R, 2 * d_out)
+    elif op == "grad_input":
+        out = {"dx": zeros(R, d_in * (2 if gated else 1))}
+    else:
+        out = {"dw": zeros(c["E"], d_out, d_in)}
+    for e in range(c["E"]):
+        q = slice(ends[e], ends[e + 1])
+        if ends[e] == ends[e + 1]:
+            continue
+        if op == "forward":
+            h = torch.matmul(f64(s["w"][e]), f64(s["x"][source[q]]).t()).t()
+            if gated:
+                a, b = h.split(d_out, dim=1)
+                out["out"][q] = a * b * torch.sigmoid(a)
+                if c["pre"]:
+                    out["pre"][q] = h
+            else:
+                out["out"][q] = torch.relu(h) if c["act"] == "relu" else h
+        elif op == "grad_input":
+            d = torch.matmul(f64(s["w"][e]).t(), f64(s["dout"][q]).t()).t()
+            if gated:
+                a, b = f64(s["saved"][q]).split(d_in, dim=1)
+                z = torch.sigmoid(a)
+                out["dx"][q, :d_in] = d * b * (z + a * z * (1 - z))
+                out["dx"][q, d_in:] = d * a * z
+            else:
+                out["dx"][q] = d * (f64(s["saved"][q]) > 0) if c["act"] == "relu" else d
+        else:
+            out["dw"][e] = torch.matmul(f64(s["x"][source[q]]).t(), f64(s["dout"][q])).t()
+    return out
+
+
+def _exact_mask(rows, d, p):
+    """Factor of every element: 0 or the scale.  The generator again, its products in 16-bit halves."""
+    limit = round(65536 * (1.0 - float(torch.tensor(p, dtype=torch.float32))))
+    groups, low = (d + 7) // 8, 0xFFFF
+    row, col = torch.meshgrid(torch.arange(rows, device="cuda") + 1, torch.arange(groups, device="cuda"), indexing="ij")
+    word = [col, row, torch.full_like(col, DROP_STEP % (1 << 32)), torch.full_like(col, DROP_STEP // (1 << 32))]
+    key = [DROP_SEED % (1 << 32), DROP_SEED // (1 << 32)]
+
+    def times(a, m):
+        x0, x1, m0, m1 = a & low, a >> 16, m & low, m >> 16
+        mid = x1 * m0 + (x0 * m0 >> 16)
+        mid2 = x0 * m1 + (mid & low)
+        return x1 * m1 + (mid >> 16) + (mid2 >> 16), ((mid2 & low) << 16) | (x0 * m0 & low)
+
+    for r in range(10):
+        (ah, al), (bh, bl) = times(word[0], 0xD2511F53), times(word[2], 0xCD9E8D57)
+        word = [bh ^ word[1] ^ ((key[0] + r * 0x9E3779B9) % (1 << 32)), bl,
+                ah ^ word[3] ^ ((key[1] + r * 0xBB67AE85) % (1 << 32)), al]
+    halves = torch.stack([h for w in word for h in (w & low, w >> 16)], dim=2).reshape(rows, groups * 8)[:, :d]
+    return (halves < limit).to(torch.float64) * (65536.0 / limit if limit else 0.0)
+
+
+def _exact_rows(c, s):
+    """dropout, combine and combine_grad, a slice of the rows at a time."""
+    n, m, d, op = c["n"], c["kept"], c["d"], c["op"]
+    f64 = lambda t: t.to(torch.float64)
+    mask = _exact_mask(m, d, c["p"]) if c["p"] > 0 and m else None
+    factor = lambda a, b: 1.0 if mask is None else mask[a:b]
+    out = {}
+    if op == "combine_grad":
+        out["dy"] = torch.zeros(n * c["K"], d, dtype=torch.float64, device="cuda")
+        if c["weights"]:
+            out["dweights"] = torch.zeros(n, c["K"], dtype=torch.float64, device="cuda")
+    else:
+        out["out"] = torch.zeros(n, d, dtype=torch.float64, device="cuda")
+    step = max(1, (1 << 24) // (d * c.get("K", 1)))
+    for lo in range(0, m, step):
+        hi = min(m, lo + step)
+        if op == "dropout":
+            v = f64(s["x"][lo:hi]) * factor(lo, hi)
+        else:
+            at = s["slot"][lo:hi].long()
+            w = torch.ones(hi - lo, c["K"], dtype=torch.float64, device="cuda") if s["weights"] is None \
+                else f64(s["weights"][lo:hi])
+            if op == "combine_grad":
+                g = f64(s["dout"][lo:hi]) * factor(lo, hi)
+                out["dy"][at.view(-1)] = (w.unsqueeze(2) * g.unsqueeze(1)).view(-1, d)
+                if c["weights"]:
+                    out["dweights"][lo:hi] = (f64(s["y"][at]) * g.unsqueeze(1)).sum(2)
+                continue
+            v = (f64(s["y"][at]) * w.unsqueeze(2)).sum(1) * factor(lo, hi)
+        out["out"][lo:hi] = v if s["residual"] is None else v + f64(s["residual"][lo:hi])
+    return out
+
+
+def exact(case, seed):
+    s = _inputs(case, seed)
+    if case["op"] == "route":
+        return _exact_route(case, s)
+    if case["op"] == "route_grad":
+        return _exact_route_grad(case, s)
+    if case["op"] in ("forward", "grad_input", "grad_weight"):
+        return _exact_product(case, s)
+    return _exact_rows(case, s)
