@@ -76,8 +76,9 @@ MOST_FLOPS = 2 * 8192 * 8 * 2048 * 2048  # of the largest listed product
 
 
 def _log(rng, lo, hi):
-    """A whole number from lo to hi, even over its logarithm."""
-    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+    """A whole number from lo to hi, even over its logarithm; round ones (multiples of 1024) are one less."""
+    v = int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+    return min(hi, max(lo, v - (v % 1024 == 0)))
 
 
 def _width(rng, lo, hi):
