@@ -73,6 +73,7 @@ def listed():
 
 
 MOST_FLOPS = 2 * 8192 * 8 * 2048 * 2048  # of the largest listed product
+MOST_BYTES = 900_000_000
 
 
 def _log(rng, lo, hi):
@@ -138,6 +139,8 @@ def draw(rng):
         case["shared"] = False
     if op == "grad_weight":
         case["act"], case["out"] = "none", rng.choice(["same", "f32"])
+    while work(case)["bytes"] > MOST_BYTES and case["n"] > 1:
+        case["n"] //= 2
     return case
 
 
