@@ -355,6 +355,153 @@ int32_t aa_train_epoch_stale(const aa_features *F, const float *y, const int32_t
                              int32_t *kept_hist, int32_t *kept_ids_hist, void *ws,
                              size_t ws_bytes, void *stream_boss, void *stream_gen);
 
+/* ---- A Boss block of experts ------------------------------------------------
+ * The operators a deep Boss needs around a feed-forward block of experts, trained
+ * (or asked) on the rows the Assistant kept: routing, the grouping of the (row,
+ * choice) pairs by expert, the experts' products and their gradients, the weighted
+ * combination of the experts' rows, and dropout from the generator the keep draws
+ * use.  The paper leaves the deep Boss's arithmetic to its framework, so these are
+ * this library's definitions.
+ *
+ * Conventions beyond those above
+ *  - `count` is a device scalar: rows [0, m), m = min(max(*count, 0), n_max), take
+ *    part; count == NULL means all n_max.  Outputs of the other rows are left
+ *    untouched.
+ *  - `dtype` is AA_F32, AA_BF16 or AA_F16; matrices are row-major with a leading
+ *    dimension in elements, at least the row's width (strides of up to 2^40 elements).
+ *    Pointers need the alignment of their type; rows on 16-byte boundaries
+ *    (8-byte for outputs of products) are the fast case, anything else is slower and not an error.
+ *  - Sums, scores and statistics are held in 32 bits or more and rounded once, to the
+ *    output's type (to nearest, ties to even).
+ *  - The pair of row t and its choice k is the number t * top_k + k.  A plan lists the pairs grouped by
+ *    expert, arrival order kept inside a group:
+ *      offsets[E + 1]  group e is [offsets[e], offsets[e + 1]),
+ *      order[q]        the pair at place q < offsets[E],
+ *      slot[pair]      its place, or -1 for a pair that has no expert.
+ *    PRECONDITION of the calls that read a plan: it was made by aa_route or
+ *    aa_expert_plan (offsets ascending from 0 to at most rows_max; slots below the number of
+ *    rows of y, no slot twice).
+ *  - Nothing here is added by floating-point atomics: the same call gives the same bits. */
+#define AA_F32 0
+#define AA_BF16 1
+#define AA_F16 2
+
+#define AA_SCORE_SOFTMAX 0
+#define AA_SCORE_SIGMOID 1
+
+#define AA_ACT_NONE 0
+#define AA_ACT_RELU 1
+#define AA_ACT_GATED 2 /* silu(gate) * up */
+
+#define AA_MAX_EXPERTS 1024
+#define AA_MAX_CHOICES 64
+
+typedef struct aa_route_config {
+  int32_t score;       /* AA_SCORE_SOFTMAX or AA_SCORE_SIGMOID */
+  int32_t top_k;       /* choices per row, 1 .. min(AA_MAX_CHOICES, top_groups * E / n_groups) */
+  int32_t n_groups;    /* groups of E / n_groups neighbouring experts (1: no groups); divides E */
+  int32_t top_groups;  /* groups a row may choose from */
+  int32_t group_best;  /* 1 or 2: a group's value is the sum of its so many highest choice values */
+  int32_t renormalise; /* not 0: the chosen scores are divided by their sum */
+  float scale;         /* factor of the weights */
+  int32_t reserved;
+} aa_route_config;
+
+/* Scratch of aa_route / aa_expert_plan with a plan and of aa_expert_grad_weight, for up to n_max
+ * rows, top_k choices and n_experts experts; 256-byte aligned, prepared once with aa_workspace_init(). */
+size_t aa_expert_workspace_bytes(int32_t n_max, int32_t top_k, int32_t n_experts);
+
+/* Routing.  For each row, E = n_experts logits (ld apart):
+ *   an expert is free if its logit is above -inf (a NaN is not);
+ *   score s_e: softmax over the free experts (if some logits are +inf, those share it evenly), or sigmoid;
+ *   choice value c_e = s_e + bias[e] (bias == NULL: s_e), none for experts that are not free or
+ *     whose value is NaN or -inf: those are never chosen;
+ *   the top_groups groups of highest value (the sum of the group_best highest c_e it has; a group without any
+ *     is never taken), then the top_k experts of highest c_e in them, highest first, ties to the
+ *     lowest index;
+ *   weight s_e (not c_e), divided by the sum of the chosen scores if cfg->renormalise (0 if that sum is 0),
+ *     times cfg->scale.
+ * ids[n_max][top_k] and weights[n_max][top_k] (fp32); a row with fewer than top_k experts to choose
+ * from has id -1 and weight 0 in the remaining places.  Choices are compared in 64 bits, so
+ * that near scores are told apart; without bias and groups that is the order of the logits.
+ * offsets, order and slot (all three or none) receive the plan of the ids, in the same call. */
+int32_t aa_route(const void *logits, int32_t dtype, int64_t ld, const int32_t *count, int32_t n_max,
+                 int32_t n_experts, const float *bias, const aa_route_config *cfg, int32_t *ids,
+                 float *weights, int32_t *offsets, int32_t *order, int32_t *slot, void *ws,
+                 size_t ws_bytes, void *stream);
+
+/* Gradient of aa_route's weights to the logits, the choice held fixed (the bias takes no
+ * gradient): dlogits[n_max][E] in the logits' type, every entry of the rows written.  ids as aa_route wrote
+ * them; dweights at an id of -1 are not read. */
+int32_t aa_route_grad(const void *logits, int32_t dtype, int64_t ld, const int32_t *count, int32_t n_max,
+                      int32_t n_experts, const aa_route_config *cfg, const int32_t *ids,
+                      const float *dweights, void *dlogits, int64_t ld_out, void *stream);
+
+/* The plan of given ids[n_max][top_k]; an id outside [0, n_experts) has no expert. */
+int32_t aa_expert_plan(const int32_t *ids, const int32_t *count, int32_t n_max, int32_t top_k,
+                       int32_t n_experts, int32_t *offsets, int32_t *order, int32_t *slot, void *ws,
+                       size_t ws_bytes, void *stream);
+
+/* The experts' products (dtype AA_BF16 or AA_F16, sums in fp32).  For place q of group e:
+ *   x_q = row (order ? order[q] / top_k : q) of x,   h = w[e] x_q,
+ *   out[q][d_out] = h (AA_ACT_NONE), max(h, 0) (AA_ACT_RELU; NaN stays NaN), or silu(h[0:d_out]) * h[d_out:2 d_out] (AA_ACT_GATED).
+ * w is [E][d_out][d_in], with AA_ACT_GATED [E][2 d_out][d_in] (gate rows, then up rows), contiguous.
+ * pre (AA_ACT_GATED only, may be NULL) receives h for the backward pass.  Rows of out at and beyond
+ * offsets[E] are left untouched. */
+int32_t aa_expert_forward(const void *x, int32_t dtype, int64_t ldx, const int32_t *order, int32_t top_k,
+                          const int32_t *offsets, int32_t rows_max, int32_t n_experts, int32_t d_in,
+                          int32_t d_out, const void *w, int32_t act, void *out, int64_t ldo, void *pre,
+                          int64_t ldpre, void *stream);
+
+/* Gradient of a product's rows: d = w[e]^T dout[q] (w [E][d_out][d_in]), taken back through the
+ * activation that made the product's input:
+ *   AA_ACT_NONE   dx[q][d_in] = d
+ *   AA_ACT_RELU   dx[q][d_in] = saved[q] > 0 ? d : 0          saved [.][d_in] = that input
+ *   AA_ACT_GATED  dx[q][2 d_in] = (d up silu'(gate), d silu(gate))   saved [.][2 d_in] = `pre` = (gate, up)
+ * saved is not read with AA_ACT_NONE. */
+int32_t aa_expert_grad_input(const void *dout, int32_t dtype, int64_t lddo, const int32_t *offsets,
+                             int32_t rows_max, int32_t n_experts, int32_t d_in, int32_t d_out,
+                             const void *w, int32_t act, const void *saved, int64_t lds, void *dx,
+                             int64_t lddx, void *stream);
+
+/* Gradient of the matrices: dw[e][d_out][d_in] = sum over the group's places of dout[q] x_q^T (x_q as in
+ * aa_expert_forward), in out_dtype (dtype or AA_F32); accumulate != 0 adds to what dw holds. An
+ * expert without rows gets zeros (accumulate: is left as it is). */
+int32_t aa_expert_grad_weight(const void *dout, int32_t dtype, int64_t lddo, const void *x, int64_t ldx,
+                              const int32_t *order, int32_t top_k, const int32_t *offsets,
+                              int32_t rows_max, int32_t n_experts, int32_t d_in, int32_t d_out, void *dw,
+                              int32_t out_dtype, int32_t accumulate, void *ws, size_t ws_bytes,
+                              void *stream);
+
+/* Dropout: an element of row r (0 .. m-1) and column c is kept if its 16-bit draw is below
+ * thr = round(65536 (1 - p)), and is then scaled by 65536 / thr, the inverse of the probability it
+ * was kept with; otherwise it is 0 whatever it held (thr == 0: everything is).  The draws are
+ * Philox4x32-10(counter = (c / 8, r + 1, lo32(step), hi32(step)), key = (lo32(seed), hi32(seed))), eight of 16 bits: draw
+ * c % 8 is the low (even) or high (odd) half of word (c % 8) / 2.  The second counter word is never 0, so a
+ * pool's keep draws under the same seed and step are other numbers.  0 <= p <= 1; p == 0 changes nothing.
+ * out = residual + dropout(x) (residual == NULL: without).  The backward pass is the same call
+ * on the gradient without a residual.  out may be x or residual. */
+int32_t aa_dropout(const void *x, int32_t dtype, int64_t ldx, const int32_t *count, int32_t n_max,
+                   int32_t d, const void *residual, int64_t ldr, float p, uint64_t seed, uint64_t step,
+                   void *out, int64_t ldo, void *stream);
+
+/* Weighted sum of each row's experts: out[t] = residual[t] + dropout(sum_k weights[t][k] y[slot[t][k]])
+ * over the slots that are not -1 (weights == NULL: all 1; that is also how the rows' gradients of
+ * aa_expert_grad_input are added up into the gradient of the block's input).  p == 0: no
+ * dropout.  A row without any slot gets its residual, or zeros. */
+int32_t aa_expert_combine(const void *y, int32_t dtype, int64_t ldy, const int32_t *slot,
+                          const float *weights, const int32_t *count, int32_t n_max, int32_t top_k,
+                          int32_t d, const void *residual, int64_t ldr, float p, uint64_t seed,
+                          uint64_t step, void *out, int64_t ldo, void *stream);
+
+/* Its gradient: g = dropout(dout[t]) (the same mask), dy[slot[t][k]] = weights[t][k] g,
+ * dweights[t][k] = y[slot[t][k]] . g (0 where the slot is -1).  dweights may be NULL, y is then not read.  The
+ * residual's gradient is dout itself. */
+int32_t aa_expert_combine_grad(const void *dout, int32_t dtype, int64_t lddo, const void *y, int64_t ldy,
+                               const int32_t *slot, const float *weights, const int32_t *count,
+                               int32_t n_max, int32_t top_k, int32_t d, float p, uint64_t seed,
+                               uint64_t step, void *dy, int64_t lddy, float *dweights, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

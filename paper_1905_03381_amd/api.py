@@ -16,6 +16,9 @@ LIB_PATH = os.path.join(_HERE, "libautoassist.so")
 
 AA_OK = 0
 AA_DENSE, AA_CSR = 0, 1
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # AA_F32, AA_BF16, AA_F16
+SCORES = {"softmax": 0, "sigmoid": 1}
+ACTIVATIONS = {"none": 0, "relu": 1, "gated": 2}
 
 SYMBOLS = [
     "aa_version", "aa_status_string", "aa_workspace_bytes", "aa_workspace_init", "aa_profile_hook",
@@ -26,6 +29,9 @@ SYMBOLS = [
     "aa_threshold_assistant_update", "aa_bucket_batches",
     "aa_pipeline_workspace_bytes", "aa_train_epoch_stale", "aa_sk_epoch",
     "aa_static_scratch_bytes", "aa_fused_step_static",
+    "aa_expert_workspace_bytes", "aa_route", "aa_route_grad", "aa_expert_plan", "aa_expert_forward",
+    "aa_expert_grad_input", "aa_expert_grad_weight", "aa_expert_combine", "aa_expert_combine_grad",
+    "aa_dropout",
 ]
 
 
@@ -45,6 +51,12 @@ class aa_step_config(C.Structure):
                 ("seed", C.c_uint64), ("step", C.c_uint64), ("T", C.c_void_p)]
 
 
+class aa_route_config(C.Structure):
+    _fields_ = [("score", C.c_int32), ("top_k", C.c_int32), ("n_groups", C.c_int32),
+                ("top_groups", C.c_int32), ("group_best", C.c_int32), ("renormalise", C.c_int32),
+                ("scale", C.c_float), ("reserved", C.c_int32)]
+
+
 _lib = None
 
 
@@ -58,7 +70,7 @@ def lib():
                       "there is no CPU fallback")
     L = C.CDLL(LIB_PATH)
     vp, i32, i64, u64, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_float, C.c_size_t
-    FP, CP = C.POINTER(aa_features), C.POINTER(aa_step_config)
+    FP, CP, RP = C.POINTER(aa_features), C.POINTER(aa_step_config), C.POINTER(aa_route_config)
     sig = {
         "aa_version": (i32, []),
         "aa_status_string": (C.c_char_p, [i32]),
@@ -86,6 +98,18 @@ def lib():
         "aa_pipeline_workspace_bytes": (sz, [i32, i32, i32]),
         "aa_train_epoch_stale": (i32, [FP, vp, vp, i64, i32, i32, vp, vp, vp, CP, vp, vp, vp, vp, sz, vp, vp]),
         "aa_bucket_batches": (i32, [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp, vp, sz, vp]),
+        "aa_expert_workspace_bytes": (sz, [i32, i32, i32]),
+        "aa_route": (i32, [vp, i32, i64, vp, i32, i32, vp, RP, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "aa_route_grad": (i32, [vp, i32, i64, vp, i32, i32, RP, vp, vp, vp, i64, vp]),
+        "aa_expert_plan": (i32, [vp, vp, i32, i32, i32, vp, vp, vp, vp, sz, vp]),
+        "aa_expert_forward": (i32, [vp, i32, i64, vp, i32, vp, i32, i32, i32, i32, vp, i32, vp, i64, vp, i64, vp]),
+        "aa_expert_grad_input": (i32, [vp, i32, i64, vp, i32, i32, i32, i32, vp, i32, vp, i64, vp, i64, vp]),
+        "aa_expert_grad_weight": (i32, [vp, i32, i64, vp, i64, vp, i32, vp, i32, i32, i32, i32, vp, i32, i32, vp,
+                                        sz, vp]),
+        "aa_expert_combine": (i32, [vp, i32, i64, vp, vp, vp, i32, i32, i32, vp, i64, f32, u64, u64, vp, i64, vp]),
+        "aa_expert_combine_grad": (i32, [vp, i32, i64, vp, i64, vp, vp, vp, i32, i32, i32, f32, u64, u64, vp, i64,
+                                         vp, vp]),
+        "aa_dropout": (i32, [vp, i32, i64, vp, i32, i32, vp, i64, f32, u64, u64, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -318,3 +342,203 @@ def bucket_batches(len_s, len_t, m_dev, m_max, width, n_buckets, token_budget, o
     _check(lib().aa_bucket_batches(_ptr(len_s), _ptr(len_t), _ptr(m_dev), m_max, width, n_buckets,
                                    token_budget, _ptr(order), _ptr(bucket_start), _ptr(batch_of),
                                    _ptr(n_batches), ws.ptr, ws.bytes, _stream()), "aa_bucket_batches")
+
+
+# ---- a Boss block of experts: routing, ragged products, combination, dropout ----
+#
+# Sizes, types and strides are read off the tensors: matrices are 2-d with neighbouring columns in
+# neighbouring elements (any row stride), matrices of all experts are contiguous [E, rows, columns],
+# index arrays are contiguous int32.
+
+
+def _require(ok, what):
+    if not ok:
+        raise AAError(what)
+
+
+def _matrix(t, name, dtype=None, width=None, rows=None):
+    """(pointer, row stride) of a 2-d CUDA tensor of the given type, width and number of rows (at least)."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2):
+        raise AAError(f"{name}: a 2-d CUDA tensor is needed")
+    n, d = t.shape
+    if dtype is not None and t.dtype != dtype:
+        raise AAError(f"{name}: {t.dtype} where {dtype} is needed")
+    if width is not None and d != width:
+        raise AAError(f"{name}: {d} columns where {width} are needed")
+    if rows is not None and n < rows:
+        raise AAError(f"{name}: {n} rows where {rows} are needed")
+    ld, step = t.stride()
+    if d > 1 and step != 1:
+        raise AAError(f"{name}: neighbouring columns must be neighbours in memory")
+    return t.data_ptr(), ld if n > 1 else d   # (a tensor of one row may state any stride)
+
+
+def _array(t, name, dtype, shape=None, least=None):
+    """Pointer of a contiguous CUDA tensor; None stays None."""
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+        raise AAError(f"{name}: a contiguous {dtype} CUDA tensor is needed")
+    if shape is not None and t.shape != shape:
+        raise AAError(f"{name}: shape {tuple(t.shape)}, not {tuple(shape)}")
+    if least is not None and t.numel() < least:
+        raise AAError(f"{name}: {t.numel()} entries where {least} are needed")
+    return t.data_ptr()
+
+
+def _type(t, name, products=False):
+    _require(isinstance(t, torch.Tensor) and t.dtype in DTYPES and not (products and t.dtype == torch.float32),
+             f"{name}: its type is not one this call takes")
+    return DTYPES[t.dtype]
+
+
+def _name_of(table, name, what):
+    _require(name in table, f"{what}: {name!r} is none of {sorted(table)}")
+    return table[name]
+
+
+class ExpertWorkspace:
+    """Device scratch of route / expert_plan (with a plan) and expert_grad_weight."""
+
+    def __init__(self, n_max, top_k, n_experts, device="cuda"):
+        self.bytes = int(lib().aa_expert_workspace_bytes(n_max, top_k, n_experts))
+        self.buf = torch.empty(self.bytes + 256, dtype=torch.uint8, device=device)
+        self.ptr = self.buf.data_ptr() + (-self.buf.data_ptr()) % 256
+        _check(lib().aa_workspace_init(self.ptr, self.bytes, _stream()), "aa_workspace_init")
+
+
+def route_config(score, top_k, n_groups=1, top_groups=1, group_best=1, renormalise=False, scale=1.0):
+    """score: "softmax" or "sigmoid"."""
+    return aa_route_config(_name_of(SCORES, score, "score"), top_k, n_groups, top_groups, group_best,
+                           int(bool(renormalise)), scale, 0)
+
+
+def _plan_pointers(plan, n, k, n_experts):
+    offsets, order, slot = plan
+    _require(offsets is not None and order is not None and slot is not None, "plan: offsets, order and slot")
+    return (_array(offsets, "offsets", torch.int32, (n_experts + 1,)), _array(order, "order", torch.int32, least=n * k),
+            _array(slot, "slot", torch.int32, (n, k)))
+
+
+def route(logits, count, bias, cfg, ids, weights, plan=None, ws=None):
+    """plan: (offsets[E + 1], order[n * top_k], slot[n, top_k]) to be made in the same call; ws then an ExpertWorkspace."""
+    dt = _type(logits, "logits")
+    x, ld = _matrix(logits, "logits")
+    n, E = logits.shape
+    p = (None, None, None) if plan is None else _plan_pointers(plan, n, cfg.top_k, E)
+    _check(lib().aa_route(x, dt, ld, _array(count, "count", torch.int32, least=1), n, E,
+                          _array(bias, "bias", torch.float32, (E,)), C.byref(cfg),
+                          _array(ids, "ids", torch.int32, (n, cfg.top_k)),
+                          _array(weights, "weights", torch.float32, (n, cfg.top_k)), *p,
+                          ws.ptr if ws else None, ws.bytes if ws else 0, _stream()), "aa_route")
+
+
+def route_grad(logits, count, cfg, ids, dweights, dlogits):
+    dt = _type(logits, "logits")
+    x, ld = _matrix(logits, "logits")
+    n, E = logits.shape
+    out, ld_out = _matrix(dlogits, "dlogits", logits.dtype, E, n)
+    _check(lib().aa_route_grad(x, dt, ld, _array(count, "count", torch.int32, least=1), n, E, C.byref(cfg),
+                               _array(ids, "ids", torch.int32, (n, cfg.top_k)),
+                               _array(dweights, "dweights", torch.float32, (n, cfg.top_k)), out, ld_out,
+                               _stream()), "aa_route_grad")
+
+
+def expert_plan(ids, count, n_experts, offsets, order, slot, ws):
+    _require(isinstance(ids, torch.Tensor) and ids.dim() == 2, "ids: a 2-d tensor")
+    n, k = ids.shape
+    p = _plan_pointers((offsets, order, slot), n, k, n_experts)
+    _check(lib().aa_expert_plan(_array(ids, "ids", torch.int32), _array(count, "count", torch.int32, least=1), n, k,
+                                n_experts, *p, ws.ptr, ws.bytes, _stream()), "aa_expert_plan")
+
+
+def _grouped_rows(x, order, top_k, rows, name):
+    """Rows that a product over `rows` places may read must be there."""
+    if order is None:
+        _require(x.shape[0] >= rows, f"{name}: {x.shape[0]} rows where {rows} are needed")
+        return None
+    _require(top_k >= 1 and x.shape[0] * top_k >= rows, f"{name}: {x.shape[0]} rows for {rows} pairs")
+    return _array(order, "order", torch.int32, least=rows)
+
+
+def expert_forward(x, order, top_k, offsets, w, act, out, pre=None):
+    """Places 0 .. out.shape[0] - 1 at most; order None: place q reads row q of x (top_k is then not used)."""
+    dt, a = _type(x, "x", products=True), _name_of(ACTIVATIONS, act, "act")
+    _require(w.dim() == 3 and w.shape[1] % (2 if act == "gated" else 1) == 0, "w: [E, rows, d_in]")
+    E, d_in, d_out = w.shape[0], w.shape[2], w.shape[1] // (2 if act == "gated" else 1)
+    rows = out.shape[0]
+    xp, ldx = _matrix(x, "x", width=d_in)
+    op, ldo = _matrix(out, "out", x.dtype, d_out)
+    pp, ldp = (None, 0) if pre is None else _matrix(pre, "pre", x.dtype, 2 * d_out, rows)
+    ordp = _grouped_rows(x, order, top_k, rows, "x")
+    _check(lib().aa_expert_forward(xp, dt, ldx, ordp, top_k, _array(offsets, "offsets", torch.int32, (E + 1,)), rows, E,
+                                   d_in, d_out, _array(w, "w", x.dtype), a, op, ldo, pp, ldp, _stream()),
+           "aa_expert_forward")
+
+
+def expert_grad_input(dout, offsets, w, act, saved, dx):
+    dt, a = _type(dout, "dout", products=True), _name_of(ACTIVATIONS, act, "act")
+    _require(w.dim() == 3, "w: [E, d_out, d_in]")
+    E, d_out, d_in = w.shape
+    rows, wide = dx.shape[0], d_in * (2 if act == "gated" else 1)
+    gp, ldg = _matrix(dout, "dout", width=d_out, rows=rows)
+    xp, ldx = _matrix(dx, "dx", dout.dtype, wide)
+    sp, lds = (None, 0) if act == "none" else _matrix(saved, "saved", dout.dtype, wide, rows)
+    _check(lib().aa_expert_grad_input(gp, dt, ldg, _array(offsets, "offsets", torch.int32, (E + 1,)), rows, E, d_in,
+                                      d_out, _array(w, "w", dout.dtype), a, sp, lds, xp, ldx, _stream()),
+           "aa_expert_grad_input")
+
+
+def expert_grad_weight(dout, x, order, top_k, offsets, dw, accumulate, ws):
+    dt = _type(dout, "dout", products=True)
+    _require(dw.dim() == 3 and dw.dtype in (dout.dtype, torch.float32), "dw: [E, d_out, d_in] of dout's type or float32")
+    E, d_out, d_in = dw.shape
+    rows = dout.shape[0]
+    gp, ldg = _matrix(dout, "dout", width=d_out)
+    xp, ldx = _matrix(x, "x", dout.dtype, d_in)
+    ordp = _grouped_rows(x, order, top_k, rows, "x")
+    _check(lib().aa_expert_grad_weight(gp, dt, ldg, xp, ldx, ordp, top_k,
+                                       _array(offsets, "offsets", torch.int32, (E + 1,)), rows, E, d_in, d_out,
+                                       _array(dw, "dw", dw.dtype), DTYPES[dw.dtype], int(bool(accumulate)), ws.ptr,
+                                       ws.bytes, _stream()), "aa_expert_grad_weight")
+
+
+def dropout(x, count, residual, p, seed, step, out):
+    dt = _type(x, "x")
+    n, d = x.shape
+    xp, ldx = _matrix(x, "x")
+    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, d, n)
+    op, ldo = _matrix(out, "out", x.dtype, d, n)
+    _check(lib().aa_dropout(xp, dt, ldx, _array(count, "count", torch.int32, least=1), n, d, rp, ldr, p, seed, step,
+                            op, ldo, _stream()), "aa_dropout")
+
+
+def expert_combine(y, slot, weights, count, residual, p, seed, step, out):
+    dt = _type(y, "y")
+    _require(isinstance(slot, torch.Tensor) and slot.dim() == 2, "slot: a 2-d tensor")
+    n, k = slot.shape
+    d = y.shape[1]
+    yp, ldy = _matrix(y, "y")
+    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", y.dtype, d, n)
+    op, ldo = _matrix(out, "out", y.dtype, d, n)
+    _check(lib().aa_expert_combine(yp, dt, ldy, _array(slot, "slot", torch.int32),
+                                   _array(weights, "weights", torch.float32, (n, k)),
+                                   _array(count, "count", torch.int32, least=1), n, k, d, rp, ldr, p, seed, step, op,
+                                   ldo, _stream()), "aa_expert_combine")
+
+
+def expert_combine_grad(dout, y, slot, weights, count, p, seed, step, dy, dweights):
+    """y is only read for dweights: both may be None."""
+    dt = _type(dout, "dout")
+    _require(isinstance(slot, torch.Tensor) and slot.dim() == 2, "slot: a 2-d tensor")
+    n, k = slot.shape
+    d = dout.shape[1]
+    gp, ldg = _matrix(dout, "dout", rows=n)
+    _require(y is not None or dweights is None, "y: needed for dweights")
+    yp, ldy = (None, d) if y is None else _matrix(y, "y", dout.dtype, d)
+    dyp, lddy = _matrix(dy, "dy", dout.dtype, d)
+    _check(lib().aa_expert_combine_grad(gp, dt, ldg, yp, ldy, _array(slot, "slot", torch.int32),
+                                        _array(weights, "weights", torch.float32, (n, k)),
+                                        _array(count, "count", torch.int32, least=1), n, k, d, p, seed, step, dyp, lddy,
+                                        _array(dweights, "dweights", torch.float32, (n, k)), _stream()),
+           "aa_expert_combine_grad")

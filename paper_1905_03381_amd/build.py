@@ -22,8 +22,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libautoassist.so")
 TRACE_LIB = os.path.join(HERE, "libautoassist_trace.so")
 PROBE = os.path.join(HERE, "bare_read_probe")
-SOURCES = ["aa_api.hip", "aa_batching.hip", "aa_dense.hip", "aa_general.hip", "aa_select.hip",
-           "aa_small.hip", "aa_wide.hip"]
+SOURCES = ["aa_experts.hip", "aa_api.hip", "aa_batching.hip", "aa_boss_api.hip", "aa_dense.hip",
+           "aa_general.hip", "aa_route.hip", "aa_rows.hip", "aa_select.hip", "aa_small.hip", "aa_wide.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-munsafe-fp-atomics",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function", "-Rpass-analysis=kernel-resource-usage"]
