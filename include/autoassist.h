@@ -369,8 +369,8 @@ int32_t aa_train_epoch_stale(const aa_features *F, const float *y, const int32_t
  *    untouched.
  *  - `dtype` is AA_F32, AA_BF16 or AA_F16; matrices are row-major with a leading
  *    dimension in elements, at least the row's width (strides of up to 2^40 elements).
- *    Pointers need the alignment of their type; rows on 16-byte boundaries
- *    (8-byte for outputs of products) are the fast case, anything else is slower and not an error.
+ *    Pointers need the alignment of their type; rows on 16-byte boundaries are the
+ *    fast case (products: and widths of whole multiples of 8), anything else is slower and not an error.
  *  - Sums, scores and statistics are held in 32 bits or more and rounded once, to the
  *    output's type (to nearest, ties to even).
  *  - The pair of row t and its choice k is the number t * top_k + k.  A plan lists the pairs grouped by

@@ -45,6 +45,13 @@ int32_t check_words(const void *p, bool needed) {
 // Rows of `width` elements can be moved 16 bytes at a time, but for a shorter end.
 bool rows_on_16(const void *p, int64_t ld, int bytes) { return on(p, 16) && ld * bytes % 16 == 0; }
 
+// What the kernels that move 16 bytes at a time address with 32 bits a lane: rows by their place in units of 16
+// bytes; rows that run along the result by their place among 31.
+bool in_reach(const void *p, int64_t rows, int64_t ld) {
+  return rows_on_16(p, ld, 2) && (rows == 0 || ld / 8 < (1ll << 32) / rows);
+}
+bool columns_in_reach(const void *p, int64_t ld) { return rows_on_16(p, ld, 2) && ld < (1ll << 25); }
+
 size_t plan_bytes(int64_t n_max, int32_t top_k, int32_t n_experts) {
   return align_up(plan_table_ints(n_max, top_k, n_experts) * sizeof(int32_t), 256);
 }
@@ -196,8 +203,8 @@ int32_t aa_expert_forward(const void *x, int32_t dtype, int64_t ldx, const int32
   a.pre = pre;
   a.ldpre = ldpre;
   a.act = act;
-  a.aligned = d_in % 8 == 0 && ldx % 8 == 0 && on(x, 16) && on(w, 16);
-  a.out_vec = on(out, 8) && ldo % 4 == 0 && (!pre || (on(pre, 8) && ldpre % 4 == 0 && d_out % 4 == 0));
+  a.aligned = d_in % 8 == 0 && in_reach(x, rows_max, ldx) && in_reach(w, 2 * (int64_t)d_out, d_in);
+  a.out_vec = rows_on_16(out, ldo, 2) && (!pre || (rows_on_16(pre, ldpre, 2) && d_out % 8 == 0));
   return hip_status(launch_expert_forward(a, dtype == AA_F16, as_stream(stream)));
 }
 
@@ -226,9 +233,9 @@ int32_t aa_expert_grad_input(const void *dout, int32_t dtype, int64_t lddo, cons
   a.saved = saved;
   a.lds = lds;
   a.act = act;
-  a.aligned = d_in % 8 == 0 && d_out % 8 == 0 && lddo % 8 == 0 && on(dout, 16) && on(w, 16);
-  a.out_vec = on(dx, 8) && lddx % 4 == 0 && (act != AA_ACT_GATED || d_in % 4 == 0) &&
-              (act == AA_ACT_NONE || (on(saved, 8) && lds % 4 == 0));
+  a.aligned = d_in % 8 == 0 && d_out % 8 == 0 && in_reach(dout, rows_max, lddo) && columns_in_reach(w, d_in);
+  a.out_vec = rows_on_16(dx, lddx, 2) && (act != AA_ACT_GATED || d_in % 8 == 0) &&
+              (act == AA_ACT_NONE || rows_on_16(saved, lds, 2));
   return hip_status(launch_expert_grad_input(a, dtype == AA_F16, as_stream(stream)));
 }
 
@@ -259,8 +266,8 @@ int32_t aa_expert_grad_weight(const void *dout, int32_t dtype, int64_t lddo, con
   a.ldo = d_in;
   a.out_f32 = out_dtype == AA_F32;
   a.accumulate = accumulate != 0;
-  a.aligned = d_in % 8 == 0 && d_out % 8 == 0 && lddo % 8 == 0 && ldx % 8 == 0 && on(dout, 16) && on(x, 16);
-  a.out_vec = on(dw, a.out_f32 ? 16 : 8) && d_in % 4 == 0;
+  a.aligned = d_in % 8 == 0 && d_out % 8 == 0 && columns_in_reach(dout, lddo) && columns_in_reach(x, ldx);
+  a.out_vec = rows_on_16(dw, d_in, type_bytes(out_dtype));
   a.partial = reinterpret_cast<float *>(static_cast<char *>(ws) + 256);
   a.partial_bytes = kGradWeightPartialBytes;
   return hip_status(launch_expert_grad_weight(a, dtype == AA_F16, as_stream(stream)));
