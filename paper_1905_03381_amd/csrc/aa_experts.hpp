@@ -26,12 +26,13 @@ struct ProductArgs {
   int32_t out_vec;  // four neighbouring outputs (and what is read beside them) can be moved at once
   float *partial;   // grad_weight: room for the parts of a split sum
   size_t partial_bytes;
+  int32_t parts;    // (chosen at launch) parts a tile's sum over rows comes in
 };
 
 hipError_t launch_expert_forward(const ProductArgs &a, bool f16, hipStream_t st);
 hipError_t launch_expert_grad_input(const ProductArgs &a, bool f16, hipStream_t st);
 hipError_t launch_expert_grad_weight(const ProductArgs &a, bool f16, hipStream_t st);
 
-constexpr size_t kGradWeightPartialBytes = 32u << 20;
+constexpr size_t kGradWeightPartialBytes = 64u << 20;
 
 }  // namespace aa
