@@ -121,7 +121,8 @@ struct Stage {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int c = chunk(h, t) * 8, from = ALIGNED && c >= width ? 0 : c;
-      at[h] = (uint32_t)(from + (GATHER ? 0 : t / kChunks * (int)ld)) * (uint32_t)sizeof(T);
+      // (not ALIGNED: any stride, so that the thread's row is multiplied with it in 64 bits, where it is read)
+      at[h] = (uint32_t)(from + (GATHER || !ALIGNED ? 0 : t / kChunks * (int)ld)) * (uint32_t)sizeof(T);
       left[h] = width - c;
     }
     order = order_;
@@ -149,7 +150,7 @@ struct Stage {
       b = reinterpret_cast<const char *>(base + (int64_t)(pair / top_k) * ld);
       return reinterpret_cast<const T *>(b + fresh(at[it & 1], k));
     } else {
-      b = reinterpret_cast<const char *>(base + (int64_t)(k + it * kRowsASlot) * ld);
+      b = reinterpret_cast<const char *>(base + (int64_t)(k + it * kRowsASlot + (ALIGNED ? 0 : t / kChunks)) * ld);
       return reinterpret_cast<const T *>(b + fresh(at[it & 1], k));
     }
   }

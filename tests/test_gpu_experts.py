@@ -483,6 +483,22 @@ def test_products_beyond_32_bit_offsets():
     assert torch.equal(x, want)
 
 
+@pytest.mark.parametrize("far", [(1 << 28) + 8, (1 << 28) + 9])
+def test_grad_weight_of_rows_far_apart(far):
+    """Rows of both operands 2^28 elements apart: a step's rows lie beyond 32 bits of bytes from each other."""
+    n, f, d = 20, 72, 64
+    store = torch.empty((n - 1) * far + 256, dtype=BF16, device="cuda")
+    dout, x = store.as_strided((n, f), (far, 1)), store.as_strided((n, d), (far, 1), 104)
+    vals = normal((n, f), BF16, 1).cuda(), normal((n, d), BF16, 2).cuda()
+    dout.copy_(vals[0])
+    x.copy_(vals[1])
+    offsets, ws = int_dev([0, 3, n]), api.ExpertWorkspace(n, 1, 2)
+    got, want = torch.empty(2, f, d, device="cuda"), torch.empty(2, f, d, device="cuda")
+    api.expert_grad_weight(dout, x, None, 1, offsets, got, False, ws)
+    api.expert_grad_weight(*vals, None, 1, offsets, want, False, ws)
+    assert torch.equal(got, want)
+
+
 # ---------------------------------------------------------------------------
 # dropout and combination
 
