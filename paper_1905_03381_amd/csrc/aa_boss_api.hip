@@ -143,11 +143,10 @@ int32_t aa_route(const void *logits, int32_t dtype, int64_t ld, const int32_t *c
     AA_TRY(check_plan(n_max, offsets, order, slot));
     AA_TRY(check_ws(ws, ws_bytes, 256 + plan_bytes(n_max, cfg->top_k, n_experts)));
   }
-  const RouteArgs r = {logits, ld, count, n_max, n_experts, bias, *cfg, ids, weights};
-  AA_TRY(hip_status(launch_route(r, dtype, as_stream(stream))));
-  if (!plan) return AA_OK;
-  return hip_status(launch_expert_plan(plan_args(ids, count, n_max, cfg->top_k, n_experts, offsets, order, slot, ws),
-                                       as_stream(stream)));
+  const RouteArgs r = {logits, dtype, 0, ld, count, n_max, n_experts, bias, *cfg, ids, weights};
+  if (!plan) return hip_status(launch_route(r, nullptr, as_stream(stream)));
+  const PlanArgs p = plan_args(ids, count, n_max, cfg->top_k, n_experts, offsets, order, slot, ws);
+  return hip_status(launch_route(r, &p, as_stream(stream)));
 }
 
 int32_t aa_route_grad(const void *logits, int32_t dtype, int64_t ld, const int32_t *count, int32_t n_max,
@@ -161,8 +160,8 @@ int32_t aa_route_grad(const void *logits, int32_t dtype, int64_t ld, const int32
   AA_TRY(check_words(count, false));
   AA_TRY(check_words(ids, n_max > 0));
   AA_TRY(check_words(dweights, n_max > 0));
-  const RouteGradArgs r = {logits, ld, count, n_max, n_experts, *cfg, ids, dweights, dlogits, ld_out};
-  return hip_status(launch_route_grad(r, dtype, as_stream(stream)));
+  const RouteGradArgs r = {logits, dtype, 0, ld, count, n_max, n_experts, *cfg, ids, dweights, dlogits, ld_out};
+  return hip_status(launch_route_grad(r, as_stream(stream)));
 }
 
 int32_t aa_expert_plan(const int32_t *ids, const int32_t *count, int32_t n_max, int32_t top_k, int32_t n_experts,

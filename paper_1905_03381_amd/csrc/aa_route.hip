@@ -1,5 +1,12 @@
 // Routing of rows to experts, its gradient, and the grouping of the (row, choice) pairs by expert.
+//
+// A row's logits are held in registers, neighbouring experts in a lane, so that a tie's lowest index is the lowest lane's
+// first.  What is exchanged between lanes goes over the vector units' own paths (LDS permutes took 124 us of a call that
+// takes 45 now: 16,384 rows, 256 experts in 8 groups, 8 choices).  Bound by instructions: a turn of the choice
+// is a maximum over the lanes, and scores are exponentials in 64 bits; the logits themselves are read at a few TB/s.
 #include "aa_route.hpp"
+
+#include <type_traits>
 
 namespace aa {
 
@@ -17,228 +24,493 @@ __device__ __forceinline__ int rows_in_use(const int32_t *count, int n_max) {
   return count ? min(max(*count, 0), n_max) : n_max;
 }
 
-__device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int off = kWave / 2; off > 0; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, kWave));
-  return v;
+// Largest value and sum over aligned groups of LPR (16 or 64) lanes, every lane gets it: inside a row of 16 lanes
+// quad swaps, half mirror, mirror; across rows exchanges with the lanes 16 and 32 away.  No LDS.
+template <int CTRL>
+__device__ __forceinline__ float lane_move(float v) {
+  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+template <int CTRL>
+__device__ __forceinline__ double lane_move(double v) {
+  const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xF, 0xF, true);
+  const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xF, 0xF, true);
+  return __hiloint2double(hi, lo);
 }
 
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int off = kWave / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
-  return v;
+template <bool FAR>  // the lane 16 or (FAR) 32 away and this one, in some order
+__device__ __forceinline__ void exchange(uint32_t v, uint32_t *x, uint32_t *y) {
+  const auto r = FAR ? __builtin_amdgcn_permlane32_swap(v, v, false, false)
+                     : __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  *x = r[0];
+  *y = r[1];
+}
+template <bool FAR>
+__device__ __forceinline__ void exchange(float v, float *x, float *y) {
+  uint32_t a, b;
+  exchange<FAR>(__float_as_uint(v), &a, &b);
+  *x = __uint_as_float(a);
+  *y = __uint_as_float(b);
+}
+template <bool FAR>
+__device__ __forceinline__ void exchange(double v, double *x, double *y) {
+  uint32_t al, bl, ah, bh;
+  exchange<FAR>((uint32_t)__double2loint(v), &al, &bl);
+  exchange<FAR>((uint32_t)__double2hiint(v), &ah, &bh);
+  *x = __hiloint2double((int)ah, (int)al);
+  *y = __hiloint2double((int)bh, (int)bl);
 }
 
-__device__ __forceinline__ float wave_sum(float v) { return group_sum<kWave>(v); }
+__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
+__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
 
-// One wave a row, expert e = lane + 64 i.  Scores and choice values are doubles: near scores are told apart
-// as the formulas have them.
-template <typename T, int EPL>
-__global__ __launch_bounds__(256) void k_route(const RouteArgs a) {
-  __shared__ double s_value[4][kMaxExperts];   // choice values, for the groups
-  __shared__ double s_group[4][kMaxExperts];   // group values
-  __shared__ uint8_t s_taken[4][kMaxExperts];  // groups to choose from
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row = blockIdx.x * 4 + wave;
-  if (row >= rows_in_use(a.count, a.n_max)) return;
-  const int E = a.n_experts, K = a.cfg.top_k;
-  const T *x_row = static_cast<const T *>(a.logits) + (int64_t)row * a.ld;
-  float x[EPL];
-  float top = kNegInf;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    const int e = lane + i * kWave;
-    x[i] = e < E ? (float)x_row[e] : kNegInf;
-    if (!(x[i] > kNegInf)) x[i] = kNegInf;  // (a NaN: not free)
-    top = fmaxf(top, x[i]);
+template <int LPR, typename V>
+__device__ __forceinline__ V lanes_max(V v) {
+  static_assert(LPR == 16 || LPR == 64, "");
+  v = larger(v, lane_move<0xB1>(v));
+  v = larger(v, lane_move<0x4E>(v));
+  v = larger(v, lane_move<0x141>(v));
+  v = larger(v, lane_move<0x140>(v));
+  if (LPR == 64) {
+    V x, y;
+    exchange<false>(v, &x, &y);
+    exchange<true>(larger(x, y), &x, &y);
+    v = larger(x, y);
   }
-  double s[EPL], c[EPL];
-  if (a.cfg.score == AA_SCORE_SOFTMAX) {
-    top = wave_max(top);
-    double sum = 0.0;
+  return v;
+}
+
+template <int LPR, typename V>
+__device__ __forceinline__ V lanes_sum(V v) {
+  static_assert(LPR == 16 || LPR == 64, "");
+  v += lane_move<0xB1>(v);
+  v += lane_move<0x4E>(v);
+  v += lane_move<0x141>(v);
+  v += lane_move<0x140>(v);
+  if (LPR == 64) {
+    V x, y;
+    exchange<false>(v, &x, &y);
+    exchange<true>(x + y, &x, &y);
+    v = x + y;
+  }
+  return v;
+}
+
+// N neighbouring logits of a row, -inf for those at or past E and for NaN.  vec: they exist whole or not at all, and can
+// be moved at once.
+template <typename T, int N>
+__device__ __forceinline__ void load_logits(const T *row, int e0, int E, bool vec, float *x) {
+  constexpr int kOn = N * sizeof(T) < 16 ? N * sizeof(T) : 16;
+  typedef T Line __attribute__((ext_vector_type(N), aligned(kOn)));
+  if (vec) {
+    if (e0 < E) {
+      const Line v = *reinterpret_cast<const Line *>(row + e0);
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      // (+inf - +inf: those that are +inf share the whole)
-      s[i] = !(x[i] > kNegInf) ? 0.0 : x[i] == top ? 1.0 : exp((double)x[i] - (double)top);
-      sum += s[i];
+      for (int i = 0; i < N; ++i) x[i] = (float)v[i];
     }
-    sum = wave_sum(sum);
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) s[i] = sum > 0.0 ? s[i] / sum : 0.0;
   } else {
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) s[i] = x[i] > kNegInf ? 1.0 / (1.0 + exp(-(double)x[i])) : 0.0;
+    for (int i = 0; i < N; ++i) x[i] = (float)row[min(e0 + i, E - 1)];
   }
 #pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    const int e = lane + i * kWave;
-    // Without bias and groups the order is that of the logits, also where scores round to one value.
-    c[i] = x[i] > kNegInf ? (a.bias ? s[i] + (double)a.bias[e] : a.cfg.n_groups > 1 ? s[i] : (double)x[i])
-                          : (double)kNegInf;
-    if (!(c[i] > (double)kNegInf)) c[i] = (double)kNegInf;
-  }
-  const int G = a.cfg.n_groups;
-  if (G > 1) {
-    const int size = E / G;
+  for (int i = 0; i < N; ++i)
+    if (e0 + i >= E || !(x[i] > kNegInf)) x[i] = kNegInf;
+}
+
+template <int N>
+__device__ __forceinline__ void load_logits(const void *logits, int dtype, int64_t at, int e0, int E, bool vec, float *x) {
+  if (dtype == AA_BF16) load_logits<__bf16, N>(static_cast<const __bf16 *>(logits) + at, e0, E, vec, x);
+  else if (dtype == AA_F16) load_logits<_Float16, N>(static_cast<const _Float16 *>(logits) + at, e0, E, vec, x);
+  else load_logits<float, N>(static_cast<const float *>(logits) + at, e0, E, vec, x);
+}
+
+template <typename T, int N>
+__device__ __forceinline__ void store_logits(T *row, int e0, int E, bool vec, const float *x) {
+  constexpr int kOn = N * sizeof(T) < 16 ? N * sizeof(T) : 16;
+  typedef T Line __attribute__((ext_vector_type(N), aligned(kOn)));
+  if (vec) {
+    if (e0 >= E) return;
+    Line v;
 #pragma unroll
-    for (int i = 0; i < EPL; ++i)
-      if (lane + i * kWave < E) s_value[wave][lane + i * kWave] = c[i];
-    wave_sync();
-    for (int g = lane; g < G; g += kWave) {
-      double first = kNegInf, second = kNegInf;
-      for (int q = 0; q < size; ++q) {
-        const double v = s_value[wave][g * size + q];
-        if (v > first) {
-          second = first;
-          first = v;
-        } else if (v > second) {
-          second = v;
-        }
-      }
-      s_group[wave][g] = a.cfg.group_best == 2 && second > (double)kNegInf ? first + second : first;
-    }
-    wave_sync();
-    for (int g = lane; g < G; g += kWave) {
-      const double v = s_group[wave][g];
-      int rank = 0;
-      for (int q = 0; q < G; ++q) {
-        const double o = s_group[wave][q];
-        rank += (o > v || (o == v && q < g)) ? 1 : 0;
-      }
-      s_taken[wave][g] = rank < a.cfg.top_groups && v > (double)kNegInf ? 1 : 0;
-    }
-    wave_sync();
+    for (int i = 0; i < N; ++i) v[i] = (T)x[i];
+    *reinterpret_cast<Line *>(row + e0) = v;
+  } else {
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      const int e = lane + i * kWave;
-      if (e < E && !s_taken[wave][e / size]) c[i] = (double)kNegInf;
-    }
-  }
-  // lane k keeps choice k
-  int my_id = -1;
-  double my_score = 0.0;
-  for (int k = 0; k < K; ++k) {
-    double best = c[0], score = s[0];
-    int at = lane;
-#pragma unroll
-    for (int i = 1; i < EPL; ++i)
-      if (c[i] > best) {
-        best = c[i];
-        score = s[i];
-        at = lane + i * kWave;
-      }
-#pragma unroll
-    for (int off = kWave / 2; off > 0; off >>= 1) {
-      const double ob = __shfl_xor(best, off, kWave), os = __shfl_xor(score, off, kWave);
-      const int oa = __shfl_xor(at, off, kWave);
-      if (ob > best || (ob == best && oa < at)) {
-        best = ob;
-        score = os;
-        at = oa;
-      }
-    }
-    if (!(best > (double)kNegInf)) break;
-#pragma unroll
-    for (int i = 0; i < EPL; ++i)
-      if (at == lane + i * kWave) c[i] = (double)kNegInf;
-    if (lane == k) {
-      my_id = at;
-      my_score = score;
-    }
-  }
-  if (a.cfg.renormalise) {
-    const double sum = wave_sum(my_score);
-    my_score = sum > 0.0 ? my_score / sum : 0.0;
-  }
-  if (lane < K) {
-    const int64_t at = (int64_t)row * K + lane;
-    a.ids[at] = my_id;
-    a.weights[at] = my_id < 0 ? 0.0f : (float)(my_score * (double)a.cfg.scale);
+    for (int i = 0; i < N; ++i)
+      if (e0 + i < E) row[e0 + i] = (T)x[i];
   }
 }
 
-// One wave a row; lane k keeps choice k.  With v the score of the choices and a = scale dweights:
+// exp(v) of v <= 0 in 64 bits, 0 far below: v = n ln 2 + r, |r| <= ln 2 / 2, and the power series of e^r to r^13 (the
+// next term is below 2^-57).  Half the instructions of the library's, which serves all of the range.
+__device__ __forceinline__ double exp_below(double v) {
+  constexpr double kTerms[12] = {1.0 / 6227020800, 1.0 / 479001600, 1.0 / 39916800, 1.0 / 3628800, 1.0 / 362880, 1.0 / 40320, 1.0 / 5040, 1.0 / 720, 1.0 / 120, 1.0 / 24, 1.0 / 6, 1.0 / 2};
+  v = v > -800.0 ? v : -800.0;
+  const double n = rint(v * 1.4426950408889634);
+  const double r = fma(-n, 2.3190468138462996e-17, fma(-n, 0.6931471805599453, v));
+  double p = kTerms[0];
+#pragma unroll
+  for (int i = 1; i < 12; ++i) p = fma(p, r, kTerms[i]);
+  p = fma(p, r, 1.0);
+  p = fma(p, r, 1.0);
+  return ldexp(p, (int)n);
+}
+
+// 1 / v for 1 <= v <= 2, by Newton's steps.
+__device__ __forceinline__ double reciprocal(double v) {
+  double r = __builtin_amdgcn_rcp(v);
+  r = fma(fma(-v, r, 1.0), r, r);
+  return fma(fma(-v, r, 1.0), r, r);
+}
+
+// 1 / (1 + e^-v), without overflow and without cancellation on either side.
+__device__ __forceinline__ double sigmoid64(double v) {
+  const double t = exp_below(v > 0.0 ? -v : v), r = reciprocal(1.0 + t);
+  return v > 0.0 ? r : t * r;
+}
+
+// What the lanes of a row tell each other.
+template <int LPR>
+struct Choices {
+  static constexpr int kMost = LPR == 16 ? 16 : kMaxChoices;
+  double value[kWave / LPR][kMost];
+  int id[kWave / LPR][kMost];
+};
+
+// Takes the experts of groups that are not among the row's top_groups out of c.  A group's value is the sum of its
+// group_best largest.
+template <int LPR, int EPL>
+__device__ __forceinline__ void leave_groups(const RouteArgs &a, int sub, double *room, double *c) {
+  const int E = a.n_experts, G = a.cfg.n_groups, size = E / G;
+  const double none = (double)kNegInf;
+  const bool two = a.cfg.group_best == 2;
+  const int lanes = size / EPL;  // of a group
+  if (size % EPL == 0 && (lanes & (lanes - 1)) == 0) {
+    // groups of whole lanes, as many as a power of two
+    double first = none, second = none;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      second = fmax(second, fmin(first, c[i]));
+      first = fmax(first, c[i]);
+    }
+    const auto join = [&](double f1, double s1, double f2, double s2) {
+      second = fmax(fmax(s1, s2), fmin(f1, f2));
+      first = fmax(f1, f2);
+    };
+    if (lanes > 1) join(first, second, lane_move<0xB1>(first), lane_move<0xB1>(second));
+    if (lanes > 2) join(first, second, lane_move<0x4E>(first), lane_move<0x4E>(second));
+    if (lanes > 4) join(first, second, lane_move<0x141>(first), lane_move<0x141>(second));
+    if (lanes > 8) join(first, second, lane_move<0x140>(first), lane_move<0x140>(second));
+    if constexpr (LPR == 64) {
+      double f1, s1, f2, s2;
+      if (lanes > 16) {
+        exchange<false>(first, &f1, &f2);
+        exchange<false>(second, &s1, &s2);
+        join(f1, s1, f2, s2);
+      }
+      if (lanes > 32) {
+        exchange<true>(first, &f1, &f2);
+        exchange<true>(second, &s1, &s2);
+        join(f1, s1, f2, s2);
+      }
+    }
+    const double v = two && second > none ? first + second : first;
+    const int g = sub / lanes;
+    int rank = 0;
+    for (int q = 0; q < G; ++q) {
+      double o;
+      if constexpr (LPR == 64)
+        o = __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), q * lanes),
+                             __builtin_amdgcn_readlane(__double2loint(v), q * lanes));
+      else
+        o = __shfl(v, q * lanes, LPR);
+      rank += (o > v || (o == v && q < g)) ? 1 : 0;
+    }
+    if (rank >= a.cfg.top_groups) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) c[i] = none;
+    }
+    return;
+  }
+  // any groups: one lane a group at a time, through LDS
+#pragma unroll
+  for (int i = 0; i < EPL; ++i)
+    if (sub * EPL + i < E) room[sub * EPL + i] = c[i];
+  wave_sync();
+  double v[EPL];  // of group sub + i LPR
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    const int g = sub + i * LPR;
+    double first = none, second = none;
+    if (g < G) {
+      for (int q = 0; q < size; ++q) {
+        const double o = room[g * size + q];
+        second = fmax(second, fmin(first, o));
+        first = fmax(first, o);
+      }
+    }
+    v[i] = two && second > none ? first + second : first;
+  }
+  wave_sync();
+#pragma unroll
+  for (int i = 0; i < EPL; ++i)
+    if (sub + i * LPR < G) room[sub + i * LPR] = v[i];
+  wave_sync();
+  bool taken[EPL];
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    const int g = sub + i * LPR;
+    int rank = 0;
+    for (int q = 0; q < G; ++q) {
+      const double o = room[q];
+      rank += (o > v[i] || (o == v[i] && q < g)) ? 1 : 0;
+    }
+    taken[i] = rank < a.cfg.top_groups;
+  }
+  wave_sync();
+#pragma unroll
+  for (int i = 0; i < EPL; ++i)
+    if (sub + i * LPR < G) room[sub + i * LPR] = taken[i] ? 1.0 : 0.0;
+  wave_sync();
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    const int e = sub * EPL + i;
+    if (e < E && room[e / size] == 0.0) c[i] = none;
+  }
+  wave_sync();  // (room is the next row's)
+}
+
+// One row, by LPR lanes of EPL neighbouring experts each (live: there is one).  Scores are doubles.  With a bias or
+// groups so are the choice values (BY_SCORE): near scores are told apart as the formulas have them.  Without, the order
+// is that of the logits, also where scores round to one value, and only the chosen experts' scores are needed (softmax:
+// and the sum over all, unless it cancels).
+template <int LPR, int EPL, bool BY_SCORE>
+__device__ __forceinline__ void route_row(const RouteArgs &a, int row, bool live, int lane, Choices<LPR> &ch, double *room) {
+  typedef typename std::conditional<BY_SCORE, double, float>::type Key;
+  const int sub = lane % LPR, in_wave = lane / LPR, e0 = sub * EPL;
+  const int E = a.n_experts, K = a.cfg.top_k;
+  const bool softmax = a.cfg.score == AA_SCORE_SOFTMAX, renorm = a.cfg.renormalise != 0;
+  float x[EPL];
+  if (live) {
+    load_logits<EPL>(a.logits, a.dtype, (int64_t)row * a.ld, e0, E, a.vec, x);
+  } else {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) x[i] = kNegInf;
+  }
+  float top = kNegInf;
+  double sum = 1.0;
+  if (softmax) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) top = fmaxf(top, x[i]);
+    top = lanes_max<LPR>(top);
+  }
+  // (+inf - +inf: those that are +inf share the whole)
+  auto raw = [&](float v) {
+    if (!(v > kNegInf)) return 0.0;
+    if (!softmax) return sigmoid64((double)v);
+    return v == top ? 1.0 : exp_below((double)v - (double)top);
+  };
+  double s[BY_SCORE ? EPL : 1];
+  Key c[EPL];
+  if constexpr (BY_SCORE) {
+    double part = 0.0;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      s[i] = raw(x[i]);
+      part += s[i];
+    }
+    if (softmax) {
+      sum = lanes_sum<LPR>(part);
+      const double inv = sum > 0.0 ? 1.0 / sum : 0.0;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) s[i] *= inv;
+    }
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      c[i] = s[i] + (a.bias ? (double)a.bias[min(e0 + i, E - 1)] : 0.0);
+      if (!(x[i] > kNegInf) || !(c[i] > (double)kNegInf)) c[i] = (double)kNegInf;
+    }
+    if (a.cfg.n_groups > 1) leave_groups<LPR, EPL>(a, sub, room, c);
+  } else {
+    if (softmax && !renorm) {
+      double part = 0.0;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) part += raw(x[i]);
+      sum = lanes_sum<LPR>(part);
+    }
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) c[i] = x[i];
+  }
+  // Every lane keeps the first of its largest; the lowest lane that holds the largest of all wins a turn.  Doubles
+  // are compared as floats first, whose order is the same but for ties: only those take a second look.
+  int got = 0;
+  Key best;
+  float near;  // best in 32 bits
+  int at;
+  auto find = [&]() {
+    best = c[0];
+    at = 0;
+#pragma unroll
+    for (int i = 1; i < EPL; ++i) {
+      at = c[i] > best ? i : at;
+      best = larger(best, c[i]);
+    }
+    near = (float)best;
+  };
+  const auto of_row = [&](unsigned long long wave) {
+    return LPR < kWave ? (wave >> (in_wave * LPR)) & ((1ull << (LPR & 63)) - 1ull) : wave;
+  };
+  find();
+  for (int k = 0; k < K; ++k) {
+    const float all = lanes_max<LPR>(near);
+    const bool mine = near == all && all > kNegInf;
+    unsigned long long wave = __ballot(mine);
+    if (wave == 0ull) break;
+    unsigned long long who = of_row(wave);
+    if constexpr (BY_SCORE) {
+      if (__any(__popcll(who) > 1)) {
+        const double exact = lanes_max<LPR>(mine ? best : (double)kNegInf);
+        wave = __ballot(mine && best == exact);
+        who = of_row(wave);
+      }
+    }
+    got += who != 0ull ? 1 : 0;
+    if (who != 0ull && sub == __ffsll((long long)who) - 1) {
+      ch.id[in_wave][k] = e0 + at;
+      double v = 0.0;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i)
+        if (i == at) {
+          v = BY_SCORE ? s[BY_SCORE ? i : 0] : (double)x[i];
+          c[i] = (Key)kNegInf;
+        }
+      ch.value[in_wave][k] = v;
+      find();
+    }
+  }
+  wave_sync();
+  double score = 0.0;
+  int id = -1;
+  if (sub < got) {
+    id = ch.id[in_wave][sub];
+    score = ch.value[in_wave][sub];
+    if constexpr (!BY_SCORE) {
+      score = raw((float)score);
+      if (softmax && !renorm) score = sum > 0.0 ? score / sum : 0.0;
+    }
+  }
+  wave_sync();  // (the room is the next row's)
+  if (renorm) {
+    const double all = lanes_sum<LPR>(score);
+    score = all > 0.0 ? score / all : 0.0;
+  }
+  if (live && sub < K) {
+    const int64_t to = (int64_t)row * K + sub;
+    a.ids[to] = id;
+    a.weights[to] = id < 0 ? 0.0f : (float)(score * (double)a.cfg.scale);
+  }
+}
+
+template <int LPR, int EPL, bool BY_SCORE>
+__global__ __launch_bounds__(256) void k_route(const RouteArgs a) {
+  constexpr int kRows = kWave / LPR;  // a wave at once
+  extern __shared__ double room[];   // [rows of the block][E], for groups that are not whole lanes
+  __shared__ Choices<LPR> choices[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int rows = rows_in_use(a.count, a.n_max);
+  for (int64_t base = ((int64_t)blockIdx.x * 4 + wave) * kRows; base < rows; base += (int64_t)gridDim.x * 4 * kRows) {
+    const int64_t row = base + lane / LPR;
+    route_row<LPR, EPL, BY_SCORE>(a, (int)row, row < rows, lane, choices[wave],
+                                  room + (wave * kRows + lane / LPR) * a.n_experts);
+  }
+}
+
+// LPR lanes a row, EPL neighbouring experts each; lane k keeps choice k.  With v the score of the choices and
+// a = scale dweights:
 //   renormalised   ds_k = (a_k - sum a v / S) / S,  S = sum v
 //   sigmoid        dlogit_k = ds_k v_k (1 - v_k), 0 elsewhere
 //   softmax        dlogit_e = s_e (ds_e - sum ds v); renormalised: the softmax over the choices alone.
-template <typename T, int EPL>
+template <int LPR, int EPL>
 __global__ __launch_bounds__(256) void k_route_grad(const RouteGradArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int row = blockIdx.x * 4 + wave;
-  if (row >= rows_in_use(a.count, a.n_max)) return;
+  constexpr int kRows = kWave / LPR;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % LPR, e0 = sub * EPL;
+  const int rows = rows_in_use(a.count, a.n_max);
   const int E = a.n_experts, K = a.cfg.top_k;
-  const T *x_row = static_cast<const T *>(a.logits) + (int64_t)row * a.ld;
-  int id = -1;
-  float d = 0.f, xk = kNegInf;
-  if (lane < K) {
-    id = a.ids[(int64_t)row * K + lane];
-    if (id < 0 || id >= E) id = -1;
-    if (id >= 0) {
-      d = a.dweights[(int64_t)row * K + lane] * a.cfg.scale;
-      xk = (float)x_row[id];
-      if (!(xk > kNegInf)) id = -1, xk = kNegInf, d = 0.f;
-    }
-  }
   const bool softmax = a.cfg.score == AA_SCORE_SOFTMAX, renorm = a.cfg.renormalise != 0;
-  float base[EPL];  // what the experts that are not chosen get
-  float v;          // this lane's choice
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) base[i] = 0.f;
-  if (softmax && !renorm) {
-    float x[EPL], top = kNegInf, sum = 0.f;
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      const int e = lane + i * kWave;
-      x[i] = e < E ? (float)x_row[e] : kNegInf;
-      if (!(x[i] > kNegInf)) x[i] = kNegInf;
-      top = fmaxf(top, x[i]);
+  for (int64_t base = ((int64_t)blockIdx.x * 4 + wave) * kRows; base < rows; base += (int64_t)gridDim.x * 4 * kRows) {
+    const int64_t row = base + lane / LPR;
+    const bool live = row < rows;
+    float x[EPL];
+    if (live && softmax && !renorm) load_logits<EPL>(a.logits, a.dtype, row * a.ld, e0, E, a.vec, x);
+    int id = -1;
+    float d = 0.f, xk = kNegInf;
+    if (live && sub < K) {
+      id = a.ids[row * K + sub];
+      d = a.dweights[row * K + sub] * a.cfg.scale;
+      if (id < 0 || id >= E) id = -1;
+      if (id >= 0) load_logits<1>(a.logits, a.dtype, row * a.ld, id, E, false, &xk);
+      if (!(xk > kNegInf)) id = -1, d = 0.f;
     }
-    top = wave_max(top);
+    float base_[EPL];  // what the experts that are not chosen get
+    float v;           // this lane's choice
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      x[i] = !(x[i] > kNegInf) ? 0.f : x[i] == top ? 1.f : expf(x[i] - top);
-      sum += x[i];
-    }
-    sum = wave_sum(sum);
-    const float inv = sum > 0.f ? 1.f / sum : 0.f;
-    const float sk = id < 0 ? 0.f : xk == top ? inv : expf(xk - top) * inv;
-    const float dot = wave_sum(d * sk);
+    for (int i = 0; i < EPL; ++i) base_[i] = 0.f;
+    if (softmax && !renorm) {
+      float top = kNegInf, sum = 0.f;
+      if (!live) {
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) base[i] = -x[i] * inv * dot;
-    v = sk * (d - dot);
-  } else if (softmax) {
-    const float top = wave_max(xk);
-    const float ek = id < 0 ? 0.f : xk == top ? 1.f : expf(xk - top);
-    const float sum = wave_sum(ek);
-    const float wk = sum > 0.f ? ek / sum : 0.f;
-    v = wk * (d - wave_sum(d * wk));
-  } else {
-    const float sk = id < 0 ? 0.f : 1.f / (1.f + expf(-xk));
-    const float rest = id < 0 ? 0.f : 1.f / (1.f + expf(xk));  // 1 - sk, without the cancellation
-    if (renorm) {
-      const float sum = wave_sum(sk);
-      const float wk = sum > 0.f ? sk / sum : 0.f;
-      v = sum > 0.f ? wk * rest * (d - wave_sum(d * wk)) : 0.f;
+        for (int i = 0; i < EPL; ++i) x[i] = kNegInf;
+      }
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) top = fmaxf(top, x[i]);
+      top = lanes_max<LPR>(top);
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) {
+        x[i] = !(x[i] > kNegInf) ? 0.f : x[i] == top ? 1.f : expf(x[i] - top);
+        sum += x[i];
+      }
+      sum = lanes_sum<LPR>(sum);
+      const float inv = sum > 0.f ? 1.f / sum : 0.f;
+      const float sk = id < 0 ? 0.f : xk == top ? inv : expf(xk - top) * inv;
+      const float dot = lanes_sum<LPR>(d * sk);
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) base_[i] = -x[i] * inv * dot;
+      v = sk * (d - dot);
+    } else if (softmax) {
+      const float top = lanes_max<LPR>(xk);
+      const float ek = id < 0 ? 0.f : xk == top ? 1.f : expf(xk - top);
+      const float sum = lanes_sum<LPR>(ek);
+      const float wk = sum > 0.f ? ek / sum : 0.f;
+      v = wk * (d - lanes_sum<LPR>(d * wk));
     } else {
-      v = d * sk * rest;
+      const float sk = id < 0 ? 0.f : 1.f / (1.f + expf(-xk));
+      const float rest = id < 0 ? 0.f : 1.f / (1.f + expf(xk));  // 1 - sk, without the cancellation
+      if (renorm) {
+        const float sum = lanes_sum<LPR>(sk);
+        const float wk = sum > 0.f ? sk / sum : 0.f;
+        v = sum > 0.f ? wk * rest * (d - lanes_sum<LPR>(d * wk)) : 0.f;
+      } else {
+        v = d * sk * rest;
+      }
+    }
+    for (int k = 0; k < K; ++k) {
+      const int at = __shfl(id, k, LPR) - e0;
+      const float vk = __shfl(v, k, LPR);
+#pragma unroll
+      for (int i = 0; i < EPL; ++i)
+        if (at == i) base_[i] = vk;
+    }
+    if (live) {
+      const int64_t to = row * a.ld_out;
+      if (a.dtype == AA_BF16) store_logits<__bf16, EPL>(static_cast<__bf16 *>(a.dlogits) + to, e0, E, a.vec, base_);
+      else if (a.dtype == AA_F16) store_logits<_Float16, EPL>(static_cast<_Float16 *>(a.dlogits) + to, e0, E, a.vec, base_);
+      else store_logits<float, EPL>(static_cast<float *>(a.dlogits) + to, e0, E, a.vec, base_);
     }
   }
-  T *out = static_cast<T *>(a.dlogits) + (int64_t)row * a.ld_out;
-  for (int k = 0; k < K; ++k) {
-    const int at = __builtin_amdgcn_readlane(id, k);
-    const float vk = lane_read(v, k);
-#pragma unroll
-    for (int i = 0; i < EPL; ++i)
-      if (at == lane + i * kWave) base[i] = vk;
-  }
-#pragma unroll
-  for (int i = 0; i < EPL; ++i)
-    if (lane + i * kWave < E) out[lane + i * kWave] = (T)base[i];
 }
 
 // ---- grouping -------------------------------------------------------------------------------------------
 // A stable counting sort: counts per tile, then every block adds up what lies before its tile and places
-// its pairs.  Ranks inside a wave come from ballots over the bits of the expert's number.
+// its pairs.  Ranks inside a wave come from ballots over the bits of the expert's number.  A single tile counts for itself.
 constexpr int kPlanThreads = 1024;
 constexpr int kPlanWaves = kPlanThreads / kWave;
 constexpr int kPlanRounds = kPlanTile / kPlanThreads;
@@ -259,13 +531,17 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan_counts(const PlanArgs a) 
   for (int e = threadIdx.x; e < E; e += kPlanThreads) a.table[(size_t)blockIdx.x * E + e] = hist[e];
 }
 
-__global__ __launch_bounds__(kPlanThreads) void k_plan_place(const PlanArgs a, int tiles) {
-  __shared__ int place[kPlanWaves][kMaxExperts];  // first the waves' counts, then where their next pair goes
+// The pairs of tile `tile` of `tiles`, by a block of kPlanThreads; MOST: experts there is room for.
+template <int MOST>
+__device__ __forceinline__ void place_tile(const PlanArgs &a, int tile, int tiles) {
+  __shared__ int place[kPlanWaves][MOST];  // first the waves' counts, then where their next pair goes
+  __shared__ int totals[2][MOST];          // of all tiles, of those before this one
   __shared__ int scan[kPlanWaves + 1];
   const int E = a.n_experts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int pairs = rows_in_use(a.count, a.n_max) * a.top_k;
-  for (int i = threadIdx.x; i < kPlanWaves * E; i += kPlanThreads) place[i / E][i % E] = 0;
-  const int first = blockIdx.x * kPlanTile + wave * (kPlanTile / kPlanWaves);
+  for (int e = lane; e < E; e += kWave) place[wave][e] = 0;
+  if ((int)threadIdx.x < E) totals[0][threadIdx.x] = totals[1][threadIdx.x] = 0;
+  const int first = tile * kPlanTile + wave * (kPlanTile / kPlanWaves);
   int id[kPlanRounds];
 #pragma unroll
   for (int r = 0; r < kPlanRounds; ++r) {
@@ -273,25 +549,42 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan_place(const PlanArgs a, i
     id[r] = p < pairs ? a.ids[p] : -1;
     if (id[r] >= E) id[r] = -1;
   }
-  int before = 0, all = 0;  // of expert threadIdx.x
-  if ((int)threadIdx.x < E)
-    for (int t = 0; t < tiles; ++t) {
-      const int c = a.table[(size_t)t * E + threadIdx.x];
-      all += c;
-      before += t < (int)blockIdx.x ? c : 0;
-    }
-  int total;
-  const int start = block_exclusive_scan(all, scan, &total);  // (its barriers: `place` is cleared)
-  if (blockIdx.x == 0) {
-    if ((int)threadIdx.x < E) a.offsets[threadIdx.x] = start;
-    if (threadIdx.x == 0) a.offsets[E] = total;
-  }
+  __syncthreads();
 #pragma unroll
   for (int r = 0; r < kPlanRounds; ++r)
     if (id[r] >= 0) atomicAdd(&place[wave][id[r]], 1);
+  if (tiles > 1) {
+    // kPlanThreads / E threads an expert, each a share of the tiles
+    const int shares = kPlanThreads / E, e = threadIdx.x % E, share = threadIdx.x / E;
+    if (share < shares) {
+      int before = 0, all = 0;
+#pragma unroll 8
+      for (int t = share; t < tiles; t += shares) {
+        const int c = a.table[(size_t)t * E + e];
+        all += c;
+        before += t < tile ? c : 0;
+      }
+      atomicAdd(&totals[0][e], all);
+      atomicAdd(&totals[1][e], before);
+    }
+  }
   __syncthreads();
+  int all = 0;
   if ((int)threadIdx.x < E) {
-    int run = start + before;
+    all = totals[0][threadIdx.x];
+    if (tiles <= 1) {
+#pragma unroll
+      for (int w = 0; w < kPlanWaves; ++w) all += place[w][threadIdx.x];
+    }
+  }
+  int total;
+  const int start = block_exclusive_scan(all, scan, &total);
+  if (tile == 0) {
+    if ((int)threadIdx.x < E) a.offsets[threadIdx.x] = start;
+    if (threadIdx.x == 0) a.offsets[E] = total;
+  }
+  if ((int)threadIdx.x < E) {
+    int run = start + totals[1][threadIdx.x];
     for (int w = 0; w < kPlanWaves; ++w) {
       const int c = place[w][threadIdx.x];
       place[w][threadIdx.x] = run;
@@ -321,51 +614,114 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan_place(const PlanArgs a, i
   }
 }
 
-template <typename T>
-hipError_t route_by_width(const RouteArgs &a, hipStream_t st) {
-  const dim3 grid((a.n_max + 3) / 4), block(256);
-  const int E = a.n_experts;
-  if (E <= 64) hipLaunchKernelGGL((k_route<T, 1>), grid, block, 0, st, a);
-  else if (E <= 128) hipLaunchKernelGGL((k_route<T, 2>), grid, block, 0, st, a);
-  else if (E <= 256) hipLaunchKernelGGL((k_route<T, 4>), grid, block, 0, st, a);
-  else if (E <= 512) hipLaunchKernelGGL((k_route<T, 8>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((k_route<T, 16>), grid, block, 0, st, a);
-  return hipGetLastError();
+__global__ __launch_bounds__(kPlanThreads) void k_plan_place(const PlanArgs a, int tiles) {
+  place_tile<kMaxExperts>(a, blockIdx.x, tiles);
 }
 
-template <typename T>
-hipError_t route_grad_by_width(const RouteGradArgs &a, hipStream_t st) {
-  const dim3 grid((a.n_max + 3) / 4), block(256);
-  const int E = a.n_experts;
-  if (E <= 64) hipLaunchKernelGGL((k_route_grad<T, 1>), grid, block, 0, st, a);
-  else if (E <= 128) hipLaunchKernelGGL((k_route_grad<T, 2>), grid, block, 0, st, a);
-  else if (E <= 256) hipLaunchKernelGGL((k_route_grad<T, 4>), grid, block, 0, st, a);
-  else if (E <= 512) hipLaunchKernelGGL((k_route_grad<T, 8>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((k_route_grad<T, 16>), grid, block, 0, st, a);
-  return hipGetLastError();
+// Routing and plan of a few rows by one block: a launch instead of two or three.
+template <int LPR, int EPL, bool BY_SCORE>
+__global__ __launch_bounds__(kPlanThreads) void k_route_few(const RouteArgs a, const PlanArgs p) {
+  constexpr int kRows = kWave / LPR;
+  extern __shared__ double room[];
+  __shared__ Choices<LPR> choices[kPlanWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int rows = rows_in_use(a.count, a.n_max);
+  for (int base = wave * kRows; base < rows; base += kPlanWaves * kRows) {
+    const int row = base + lane / LPR;
+    route_row<LPR, EPL, BY_SCORE>(a, row, row < rows, lane, choices[wave], room + (wave * kRows + lane / LPR) * a.n_experts);
+  }
+  __syncthreads();  // (the ids are written)
+  place_tile<LPR * EPL>(p, 0, 1);
+}
+
+// Whether every lane's EPL logits exist whole or not at all and can be moved at once.
+bool whole_lanes(const void *p, int64_t ld, int32_t E, int epl, int32_t dtype) {
+  const int bytes = dtype == AA_F32 ? 4 : 2, on = epl * bytes < 16 ? epl * bytes : 16;
+  return E % epl == 0 && ld * bytes % on == 0 && reinterpret_cast<uintptr_t>(p) % on == 0;
+}
+
+bool groups_need_room(const RouteArgs &a, int epl) {
+  const int size = a.n_experts / a.cfg.n_groups, lanes = size / epl;
+  return a.cfg.n_groups > 1 && (size % epl != 0 || (lanes & (lanes - 1)) != 0);
+}
+
+dim3 blocks_for(int32_t n_max, int rows_a_block) {
+  const int64_t want = ((int64_t)n_max + rows_a_block - 1) / rows_a_block;
+  return dim3((uint32_t)(want < (1 << 22) ? want : 1 << 22));  // (blocks take turns)
+}
+
+// The lanes of a row: 16 of up to 8 experts where they hold the choices too, else the wave (65,536 rows, 4 choices, sigmoid,
+// without and with a bias: 32 experts 10.4 / 16.2 us, a wave a row 31.3 / 41.3; 128 experts 17.0 / 50.9 and 33.9 / 54.3).
+template <typename Launch>
+hipError_t by_width(int32_t E, int32_t K, Launch launch) {
+  using std::integral_constant;
+  if (K <= 16 && E <= 128) {
+    const integral_constant<int, 16> lpr;
+    if (E <= 16) return launch(lpr, integral_constant<int, 1>());
+    if (E <= 32) return launch(lpr, integral_constant<int, 2>());
+    if (E <= 64) return launch(lpr, integral_constant<int, 4>());
+    return launch(lpr, integral_constant<int, 8>());
+  }
+  const integral_constant<int, 64> lpr;
+  if (E <= 64) return launch(lpr, integral_constant<int, 1>());
+  if (E <= 128) return launch(lpr, integral_constant<int, 2>());
+  if (E <= 256) return launch(lpr, integral_constant<int, 4>());
+  if (E <= 512) return launch(lpr, integral_constant<int, 8>());
+  return launch(lpr, integral_constant<int, 16>());
 }
 
 }  // namespace
 
-hipError_t launch_route(const RouteArgs &a, int32_t dtype, hipStream_t st) {
-  if (a.n_max == 0) return hipSuccess;
-  if (dtype == AA_BF16) return route_by_width<__bf16>(a, st);
-  if (dtype == AA_F16) return route_by_width<_Float16>(a, st);
-  return route_by_width<float>(a, st);
+hipError_t launch_route(const RouteArgs &args, const PlanArgs *plan, hipStream_t st) {
+  RouteArgs a = args;
+  const bool by_score = a.bias || a.cfg.n_groups > 1;
+  if (a.n_max == 0) return plan ? launch_expert_plan(*plan, st) : hipSuccess;
+  bool planned = false;
+  const hipError_t e = by_width(a.n_experts, a.cfg.top_k, [&](auto lpr, auto epl) {
+    constexpr int LPR = decltype(lpr)::value, EPL = decltype(epl)::value, kRows = kWave / LPR;
+    a.vec = whole_lanes(a.logits, a.ld, a.n_experts, EPL, a.dtype);
+    const size_t room = groups_need_room(a, EPL) ? (size_t)kRows * a.n_experts * sizeof(double) : 0;  // a wave
+    if constexpr (LPR * EPL <= 256) {
+      // Rows that its waves take at once: 1 to 64 rows, 64 experts, 6 choices 7.9 to 8.2 us, as two launches 10.5; 128
+      // rows 11.0 and 10.5.  A wave a row: only half as many (256 experts in groups with a bias, 5 rows 10.2 and
+      // 11.4 us, 16 rows 13.3 and 11.6).
+      if (plan && (int64_t)a.n_max * a.cfg.top_k <= kPlanTile && a.n_max <= (LPR == 16 ? 64 : 8) &&
+          room * kPlanWaves <= 32 << 10) {
+        planned = true;
+        if (by_score)
+          hipLaunchKernelGGL((k_route_few<LPR, EPL, true>), dim3(1), dim3(kPlanThreads), room * kPlanWaves, st, a, *plan);
+        else
+          hipLaunchKernelGGL((k_route_few<LPR, EPL, false>), dim3(1), dim3(kPlanThreads), 0, st, a, *plan);
+        return hipGetLastError();
+      }
+    }
+    const dim3 grid = blocks_for(a.n_max, 4 * kRows);
+    if (by_score) hipLaunchKernelGGL((k_route<LPR, EPL, true>), grid, dim3(256), room * 4, st, a);
+    else hipLaunchKernelGGL((k_route<LPR, EPL, false>), grid, dim3(256), 0, st, a);
+    return hipGetLastError();
+  });
+  if (e != hipSuccess || !plan || planned) return e;
+  return launch_expert_plan(*plan, st);
 }
 
-hipError_t launch_route_grad(const RouteGradArgs &a, int32_t dtype, hipStream_t st) {
+hipError_t launch_route_grad(const RouteGradArgs &args, hipStream_t st) {
+  RouteGradArgs a = args;
   if (a.n_max == 0) return hipSuccess;
-  if (dtype == AA_BF16) return route_grad_by_width<__bf16>(a, st);
-  if (dtype == AA_F16) return route_grad_by_width<_Float16>(a, st);
-  return route_grad_by_width<float>(a, st);
+  return by_width(a.n_experts, a.cfg.top_k, [&](auto lpr, auto epl) {
+    constexpr int LPR = decltype(lpr)::value, EPL = decltype(epl)::value;
+    a.vec = whole_lanes(a.logits, a.ld, a.n_experts, EPL, a.dtype) &&
+            whole_lanes(a.dlogits, a.ld_out, a.n_experts, EPL, a.dtype);
+    hipLaunchKernelGGL((k_route_grad<LPR, EPL>), blocks_for(a.n_max, 4 * (kWave / LPR)), dim3(256), 0, st, a);
+    return hipGetLastError();
+  });
 }
 
 hipError_t launch_expert_plan(const PlanArgs &a, hipStream_t st) {
   const int tiles = (int)(((int64_t)a.n_max * a.top_k + kPlanTile - 1) / kPlanTile);
-  if (tiles > 0) {
+  if (tiles > 1) {
     hipLaunchKernelGGL(k_plan_counts, dim3(tiles), dim3(kPlanThreads), 0, st, a);
-    if (hipGetLastError() != hipSuccess) return hipErrorLaunchFailure;
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
   }
   hipLaunchKernelGGL(k_plan_place, dim3(tiles > 0 ? tiles : 1), dim3(kPlanThreads), 0, st, a, tiles);
   return hipGetLastError();

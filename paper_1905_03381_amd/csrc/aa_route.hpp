@@ -11,6 +11,7 @@ constexpr int kPlanTile = 2048;  // pairs grouped by one block
 
 struct RouteArgs {
   const void *logits;
+  int32_t dtype, vec;  // vec (set at launch): a lane's logits can be moved at once
   int64_t ld;
   const int32_t *count;
   int32_t n_max, n_experts;
@@ -22,6 +23,7 @@ struct RouteArgs {
 
 struct RouteGradArgs {
   const void *logits;
+  int32_t dtype, vec;
   int64_t ld;
   const int32_t *count;
   int32_t n_max, n_experts;
@@ -37,7 +39,7 @@ struct PlanArgs {
   const int32_t *count;
   int32_t n_max, top_k, n_experts;
   int32_t *offsets, *order, *slot;
-  int32_t *table;  // [tiles][E] counts, then [E] totals
+  int32_t *table;  // [tiles][E] counts
 };
 
 inline size_t plan_table_ints(int64_t n_max, int32_t top_k, int32_t n_experts) {
@@ -45,8 +47,9 @@ inline size_t plan_table_ints(int64_t n_max, int32_t top_k, int32_t n_experts) {
   return (tiles + 1) * (size_t)n_experts;
 }
 
-hipError_t launch_route(const RouteArgs &a, int32_t dtype, hipStream_t st);
-hipError_t launch_route_grad(const RouteGradArgs &a, int32_t dtype, hipStream_t st);
+// plan: made in the same call (may be NULL)
+hipError_t launch_route(const RouteArgs &a, const PlanArgs *plan, hipStream_t st);
+hipError_t launch_route_grad(const RouteGradArgs &a, hipStream_t st);
 hipError_t launch_expert_plan(const PlanArgs &a, hipStream_t st);
 
 }  // namespace aa
