@@ -2,8 +2,9 @@
 //
 // A row's logits are held in registers, neighbouring experts in a lane, so that a tie's lowest index is the lowest lane's
 // first.  What is exchanged between lanes goes over the vector units' own paths (LDS permutes took 124 us of a call that
-// takes 45 now: 16,384 rows, 256 experts in 8 groups, 8 choices).  Bound by instructions: a turn of the choice
-// is a maximum over the lanes, and scores are exponentials in 64 bits; the logits themselves are read at a few TB/s.
+// takes 36 now, 9 of it the plan: 16,384 rows, 256 experts in 8 groups, 8 choices).  Bound by instructions: a turn of
+// the choice is a maximum over a lane's experts and over the lanes, scores are exponentials in 64 bits; reading the logits is
+// a small part (of 65,536 rows of 128 experts 15 us, 2.3 TB/s, without a bias, 33 with one).
 #include "aa_route.hpp"
 
 #include <type_traits>
@@ -172,66 +173,68 @@ __device__ __forceinline__ double sigmoid64(double v) {
 template <int LPR>
 struct Choices {
   static constexpr int kMost = LPR == 16 ? 16 : kMaxChoices;
-  double value[kWave / LPR][kMost];
   int id[kWave / LPR][kMost];
 };
 
 // Takes the experts of groups that are not among the row's top_groups out of c.  A group's value is the sum of its
-// group_best largest.
+// group_best largest.  Groups of whole lanes, as many as a power of two.
 template <int LPR, int EPL>
-__device__ __forceinline__ void leave_groups(const RouteArgs &a, int sub, double *room, double *c) {
+__device__ __forceinline__ void leave_groups(const RouteArgs &a, int sub, double *c) {
+  const int G = a.cfg.n_groups;
+  const double none = (double)kNegInf;
+  const bool two = a.cfg.group_best == 2;
+  const int lanes = a.n_experts / G / EPL;  // of a group
+  double first = none, second = none;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    second = fmax(second, fmin(first, c[i]));
+    first = fmax(first, c[i]);
+  }
+  const auto join = [&](double f1, double s1, double f2, double s2) {
+    second = fmax(fmax(s1, s2), fmin(f1, f2));
+    first = fmax(f1, f2);
+  };
+  if (lanes > 1) join(first, second, lane_move<0xB1>(first), lane_move<0xB1>(second));
+  if (lanes > 2) join(first, second, lane_move<0x4E>(first), lane_move<0x4E>(second));
+  if (lanes > 4) join(first, second, lane_move<0x141>(first), lane_move<0x141>(second));
+  if (lanes > 8) join(first, second, lane_move<0x140>(first), lane_move<0x140>(second));
+  if constexpr (LPR == 64) {
+    double f1, s1, f2, s2;
+    if (lanes > 16) {
+      exchange<false>(first, &f1, &f2);
+      exchange<false>(second, &s1, &s2);
+      join(f1, s1, f2, s2);
+    }
+    if (lanes > 32) {
+      exchange<true>(first, &f1, &f2);
+      exchange<true>(second, &s1, &s2);
+      join(f1, s1, f2, s2);
+    }
+  }
+  const double v = two && second > none ? first + second : first;
+  const int g = sub / lanes;
+  int rank = 0;
+  for (int q = 0; q < G; ++q) {
+    double o;
+    if constexpr (LPR == 64)
+      o = __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), q * lanes),
+                           __builtin_amdgcn_readlane(__double2loint(v), q * lanes));
+    else
+      o = __shfl(v, q * lanes, LPR);
+    rank += (o > v || (o == v && q < g)) ? 1 : 0;
+  }
+  if (rank >= a.cfg.top_groups) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) c[i] = none;
+  }
+}
+
+// The same for groups of any size: a lane takes a group, through LDS.
+template <int LPR, int EPL>
+__device__ __forceinline__ void leave_any_groups(const RouteArgs &a, int sub, double *room, double *c) {
   const int E = a.n_experts, G = a.cfg.n_groups, size = E / G;
   const double none = (double)kNegInf;
   const bool two = a.cfg.group_best == 2;
-  const int lanes = size / EPL;  // of a group
-  if (size % EPL == 0 && (lanes & (lanes - 1)) == 0) {
-    // groups of whole lanes, as many as a power of two
-    double first = none, second = none;
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      second = fmax(second, fmin(first, c[i]));
-      first = fmax(first, c[i]);
-    }
-    const auto join = [&](double f1, double s1, double f2, double s2) {
-      second = fmax(fmax(s1, s2), fmin(f1, f2));
-      first = fmax(f1, f2);
-    };
-    if (lanes > 1) join(first, second, lane_move<0xB1>(first), lane_move<0xB1>(second));
-    if (lanes > 2) join(first, second, lane_move<0x4E>(first), lane_move<0x4E>(second));
-    if (lanes > 4) join(first, second, lane_move<0x141>(first), lane_move<0x141>(second));
-    if (lanes > 8) join(first, second, lane_move<0x140>(first), lane_move<0x140>(second));
-    if constexpr (LPR == 64) {
-      double f1, s1, f2, s2;
-      if (lanes > 16) {
-        exchange<false>(first, &f1, &f2);
-        exchange<false>(second, &s1, &s2);
-        join(f1, s1, f2, s2);
-      }
-      if (lanes > 32) {
-        exchange<true>(first, &f1, &f2);
-        exchange<true>(second, &s1, &s2);
-        join(f1, s1, f2, s2);
-      }
-    }
-    const double v = two && second > none ? first + second : first;
-    const int g = sub / lanes;
-    int rank = 0;
-    for (int q = 0; q < G; ++q) {
-      double o;
-      if constexpr (LPR == 64)
-        o = __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), q * lanes),
-                             __builtin_amdgcn_readlane(__double2loint(v), q * lanes));
-      else
-        o = __shfl(v, q * lanes, LPR);
-      rank += (o > v || (o == v && q < g)) ? 1 : 0;
-    }
-    if (rank >= a.cfg.top_groups) {
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) c[i] = none;
-    }
-    return;
-  }
-  // any groups: one lane a group at a time, through LDS
 #pragma unroll
   for (int i = 0; i < EPL; ++i)
     if (sub * EPL + i < E) room[sub * EPL + i] = c[i];
@@ -279,39 +282,46 @@ __device__ __forceinline__ void leave_groups(const RouteArgs &a, int sub, double
   wave_sync();  // (room is the next row's)
 }
 
+// What a choice goes by: the logits; scores, with a bias or groups of whole lanes; groups of any size.
+enum By { kByLogit, kByScore, kByAnyGroups };
+
 // One row, by LPR lanes of EPL neighbouring experts each (live: there is one).  Scores are doubles.  With a bias or
-// groups so are the choice values (BY_SCORE): near scores are told apart as the formulas have them.  Without, the order
-// is that of the logits, also where scores round to one value, and only the chosen experts' scores are needed (softmax:
-// and the sum over all, unless it cancels).
-template <int LPR, int EPL, bool BY_SCORE>
+// groups so are the choice values: near scores are told apart as the formulas have them.  Without, the order is that
+// of the logits, also where scores round to one value.  The turns of the choice go by 32 bits of each value, whose order is
+// the same but for ties; experts that tie in them are computed again and compared in 64.
+template <int LPR, int EPL, By BY>
 __device__ __forceinline__ void route_row(const RouteArgs &a, int row, bool live, int lane, Choices<LPR> &ch, double *room) {
-  typedef typename std::conditional<BY_SCORE, double, float>::type Key;
   const int sub = lane % LPR, in_wave = lane / LPR, e0 = sub * EPL;
   const int E = a.n_experts, K = a.cfg.top_k;
   const bool softmax = a.cfg.score == AA_SCORE_SOFTMAX, renorm = a.cfg.renormalise != 0;
+  const int64_t from = (int64_t)row * a.ld;
   float x[EPL];
   if (live) {
-    load_logits<EPL>(a.logits, a.dtype, (int64_t)row * a.ld, e0, E, a.vec, x);
+    load_logits<EPL>(a.logits, a.dtype, from, e0, E, a.vec, x);
   } else {
 #pragma unroll
     for (int i = 0; i < EPL; ++i) x[i] = kNegInf;
   }
   float top = kNegInf;
-  double sum = 1.0;
   if (softmax) {
 #pragma unroll
     for (int i = 0; i < EPL; ++i) top = fmaxf(top, x[i]);
     top = lanes_max<LPR>(top);
   }
   // (+inf - +inf: those that are +inf share the whole)
-  auto raw = [&](float v) {
+  const auto raw = [&](float v) {
     if (!(v > kNegInf)) return 0.0;
     if (!softmax) return sigmoid64((double)v);
     return v == top ? 1.0 : exp_below((double)v - (double)top);
   };
-  double s[BY_SCORE ? EPL : 1];
-  Key c[EPL];
-  if constexpr (BY_SCORE) {
+  double inv = 1.0;
+  const auto value = [&](float v, double score, int e) {
+    const double c = score + (a.bias ? (double)a.bias[e] : 0.0);
+    return v > kNegInf && c > (double)kNegInf ? c : (double)kNegInf;
+  };
+  float c[EPL];
+  if constexpr (BY != kByLogit) {
+    double s[EPL];
     double part = 0.0;
 #pragma unroll
     for (int i = 0; i < EPL; ++i) {
@@ -319,84 +329,73 @@ __device__ __forceinline__ void route_row(const RouteArgs &a, int row, bool live
       part += s[i];
     }
     if (softmax) {
-      sum = lanes_sum<LPR>(part);
-      const double inv = sum > 0.0 ? 1.0 / sum : 0.0;
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) s[i] *= inv;
+      part = lanes_sum<LPR>(part);
+      inv = part > 0.0 ? 1.0 / part : 0.0;
     }
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      c[i] = s[i] + (a.bias ? (double)a.bias[min(e0 + i, E - 1)] : 0.0);
-      if (!(x[i] > kNegInf) || !(c[i] > (double)kNegInf)) c[i] = (double)kNegInf;
-    }
-    if (a.cfg.n_groups > 1) leave_groups<LPR, EPL>(a, sub, room, c);
+    for (int i = 0; i < EPL; ++i) s[i] = value(x[i], s[i] * inv, min(e0 + i, E - 1));
+    if constexpr (BY == kByAnyGroups) leave_any_groups<LPR, EPL>(a, sub, room, s);
+    else if (a.cfg.n_groups > 1) leave_groups<LPR, EPL>(a, sub, s);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) c[i] = (float)s[i];
   } else {
     if (softmax && !renorm) {
       double part = 0.0;
 #pragma unroll
       for (int i = 0; i < EPL; ++i) part += raw(x[i]);
-      sum = lanes_sum<LPR>(part);
+      part = lanes_sum<LPR>(part);
+      inv = part > 0.0 ? 1.0 / part : 0.0;
     }
 #pragma unroll
     for (int i = 0; i < EPL; ++i) c[i] = x[i];
   }
-  // Every lane keeps the first of its largest; the lowest lane that holds the largest of all wins a turn.  Doubles
-  // are compared as floats first, whose order is the same but for ties: only those take a second look.
-  int got = 0;
-  Key best;
-  float near;  // best in 32 bits
-  int at;
-  auto find = [&]() {
-    best = c[0];
-    at = 0;
-#pragma unroll
-    for (int i = 1; i < EPL; ++i) {
-      at = c[i] > best ? i : at;
-      best = larger(best, c[i]);
-    }
-    near = (float)best;
-  };
   const auto of_row = [&](unsigned long long wave) {
     return LPR < kWave ? (wave >> (in_wave * LPR)) & ((1ull << (LPR & 63)) - 1ull) : wave;
   };
-  find();
+  int got = 0;
   for (int k = 0; k < K; ++k) {
-    const float all = lanes_max<LPR>(near);
-    const bool mine = near == all && all > kNegInf;
-    unsigned long long wave = __ballot(mine);
+    float all = c[0];
+#pragma unroll
+    for (int i = 1; i < EPL; ++i) all = larger(all, c[i]);
+    all = lanes_max<LPR>(all);
+    uint32_t held = 0;  // bit i: this lane's expert i has the largest value
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) held |= c[i] == all ? 1u << i : 0u;
+    if (!(all > kNegInf)) held = 0;
+    unsigned long long wave = __ballot(held != 0);
     if (wave == 0ull) break;
-    unsigned long long who = of_row(wave);
-    if constexpr (BY_SCORE) {
-      if (__any(__popcll(who) > 1)) {
-        const double exact = lanes_max<LPR>(mine ? best : (double)kNegInf);
-        wave = __ballot(mine && best == exact);
-        who = of_row(wave);
+    if constexpr (BY != kByLogit) {
+      if (__any(__popcll(of_row(wave)) > 1 || (held & (held - 1)) != 0)) {
+        double best = (double)kNegInf;
+        int at = 0;
+        for (uint32_t left = held; left != 0; left &= left - 1) {
+          const int i = __ffs((int)left) - 1;
+          float v;
+          load_logits<1>(a.logits, a.dtype, from, e0 + i, E, false, &v);
+          const double exact = value(v, raw(v) * inv, e0 + i);
+          if (exact > best) best = exact, at = i;
+        }
+        const double most = lanes_max<LPR>(best);
+        held = held != 0 && best == most ? 1u << at : 0u;
+        wave = __ballot(held != 0);
       }
     }
+    const unsigned long long who = of_row(wave);
     got += who != 0ull ? 1 : 0;
-    if (who != 0ull && sub == __ffsll((long long)who) - 1) {
-      ch.id[in_wave][k] = e0 + at;
-      double v = 0.0;
+    if (sub != __ffsll((long long)who) - 1) held = 0;
+    const int at = __ffs((int)held) - 1;  // (-1: the lowest lane that holds it is another)
+    if (at >= 0) ch.id[in_wave][k] = e0 + at;
 #pragma unroll
-      for (int i = 0; i < EPL; ++i)
-        if (i == at) {
-          v = BY_SCORE ? s[BY_SCORE ? i : 0] : (double)x[i];
-          c[i] = (Key)kNegInf;
-        }
-      ch.value[in_wave][k] = v;
-      find();
-    }
+    for (int i = 0; i < EPL; ++i) c[i] = i == at ? kNegInf : c[i];
   }
   wave_sync();
   double score = 0.0;
   int id = -1;
   if (sub < got) {
     id = ch.id[in_wave][sub];
-    score = ch.value[in_wave][sub];
-    if constexpr (!BY_SCORE) {
-      score = raw((float)score);
-      if (softmax && !renorm) score = sum > 0.0 ? score / sum : 0.0;
-    }
+    float v;
+    load_logits<1>(a.logits, a.dtype, from, id, E, false, &v);
+    score = raw(v) * inv;
   }
   wave_sync();  // (the room is the next row's)
   if (renorm) {
@@ -410,17 +409,17 @@ __device__ __forceinline__ void route_row(const RouteArgs &a, int row, bool live
   }
 }
 
-template <int LPR, int EPL, bool BY_SCORE>
+template <int LPR, int EPL, By BY>
 __global__ __launch_bounds__(256) void k_route(const RouteArgs a) {
   constexpr int kRows = kWave / LPR;  // a wave at once
-  extern __shared__ double room[];   // [rows of the block][E], for groups that are not whole lanes
+  extern __shared__ double room[];   // [rows of the block][E] (kByAnyGroups)
   __shared__ Choices<LPR> choices[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int rows = rows_in_use(a.count, a.n_max);
   for (int64_t base = ((int64_t)blockIdx.x * 4 + wave) * kRows; base < rows; base += (int64_t)gridDim.x * 4 * kRows) {
     const int64_t row = base + lane / LPR;
-    route_row<LPR, EPL, BY_SCORE>(a, (int)row, row < rows, lane, choices[wave],
-                                  room + (wave * kRows + lane / LPR) * a.n_experts);
+    route_row<LPR, EPL, BY>(a, (int)row, row < rows, lane, choices[wave],
+                            BY == kByAnyGroups ? room + (wave * kRows + lane / LPR) * a.n_experts : nullptr);
   }
 }
 
@@ -618,17 +617,16 @@ __global__ __launch_bounds__(kPlanThreads) void k_plan_place(const PlanArgs a, i
   place_tile<kMaxExperts>(a, blockIdx.x, tiles);
 }
 
-// Routing and plan of a few rows by one block: a launch instead of two or three.
-template <int LPR, int EPL, bool BY_SCORE>
+// Routing and plan of a few rows by one block: a launch instead of two.
+template <int LPR, int EPL, By BY>
 __global__ __launch_bounds__(kPlanThreads) void k_route_few(const RouteArgs a, const PlanArgs p) {
   constexpr int kRows = kWave / LPR;
-  extern __shared__ double room[];
   __shared__ Choices<LPR> choices[kPlanWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int rows = rows_in_use(a.count, a.n_max);
   for (int base = wave * kRows; base < rows; base += kPlanWaves * kRows) {
     const int row = base + lane / LPR;
-    route_row<LPR, EPL, BY_SCORE>(a, row, row < rows, lane, choices[wave], room + (wave * kRows + lane / LPR) * a.n_experts);
+    route_row<LPR, EPL, BY>(a, row, row < rows, lane, choices[wave], nullptr);
   }
   __syncthreads();  // (the ids are written)
   place_tile<LPR * EPL>(p, 0, 1);
@@ -640,9 +638,10 @@ bool whole_lanes(const void *p, int64_t ld, int32_t E, int epl, int32_t dtype) {
   return E % epl == 0 && ld * bytes % on == 0 && reinterpret_cast<uintptr_t>(p) % on == 0;
 }
 
-bool groups_need_room(const RouteArgs &a, int epl) {
+// No groups, or each of whole lanes, as many as a power of two.
+bool groups_of_lanes(const RouteArgs &a, int epl) {
   const int size = a.n_experts / a.cfg.n_groups, lanes = size / epl;
-  return a.cfg.n_groups > 1 && (size % epl != 0 || (lanes & (lanes - 1)) != 0);
+  return a.cfg.n_groups == 1 || (size % epl == 0 && (lanes & (lanes - 1)) == 0);
 }
 
 dim3 blocks_for(int32_t n_max, int rows_a_block) {
@@ -650,17 +649,18 @@ dim3 blocks_for(int32_t n_max, int rows_a_block) {
   return dim3((uint32_t)(want < (1 << 22) ? want : 1 << 22));  // (blocks take turns)
 }
 
-// The lanes of a row: 16 of up to 8 experts where they hold the choices too, else the wave (65,536 rows, 4 choices, sigmoid,
-// without and with a bias: 32 experts 10.4 / 16.2 us, a wave a row 31.3 / 41.3; 128 experts 17.0 / 50.9 and 33.9 / 54.3).
+// The lanes of a row: 16 for up to most16 experts where they hold the choices too, else the wave (65,536 rows, 4 choices,
+// sigmoid, without and with a bias: 32 experts 10.4 / 16.2 us, a wave a row 31.3 / 41.3).
 template <typename Launch>
-hipError_t by_width(int32_t E, int32_t K, Launch launch) {
+hipError_t by_width(int32_t E, int32_t K, int32_t most16, Launch launch) {
   using std::integral_constant;
-  if (K <= 16 && E <= 128) {
+  if (K <= 16 && E <= most16) {
     const integral_constant<int, 16> lpr;
     if (E <= 16) return launch(lpr, integral_constant<int, 1>());
     if (E <= 32) return launch(lpr, integral_constant<int, 2>());
     if (E <= 64) return launch(lpr, integral_constant<int, 4>());
-    return launch(lpr, integral_constant<int, 8>());
+    if (E <= 128) return launch(lpr, integral_constant<int, 8>());
+    return launch(lpr, integral_constant<int, 16>());
   }
   const integral_constant<int, 64> lpr;
   if (E <= 64) return launch(lpr, integral_constant<int, 1>());
@@ -674,30 +674,36 @@ hipError_t by_width(int32_t E, int32_t K, Launch launch) {
 
 hipError_t launch_route(const RouteArgs &args, const PlanArgs *plan, hipStream_t st) {
   RouteArgs a = args;
-  const bool by_score = a.bias || a.cfg.n_groups > 1;
   if (a.n_max == 0) return plan ? launch_expert_plan(*plan, st) : hipSuccess;
   bool planned = false;
-  const hipError_t e = by_width(a.n_experts, a.cfg.top_k, [&](auto lpr, auto epl) {
+  const bool by_score = a.bias || a.cfg.n_groups > 1;
+  // Beyond 128 experts 16 lanes hold 16 each.  By logits that is better at any size (16,384 rows, 256 experts, 4 choices
+  // 7.7 us, a wave a row 11.5); by scores it takes many registers, and rows that fill the chip (8 groups, 8 choices:
+  // 16,384 rows 25.9 and 30.5 us, 4096 rows 12.1 and 11.0); groups of any size are worse (65,536 rows of 200 311 and 160).
+  const bool many = !by_score || (a.n_max >= 8192 && groups_of_lanes(a, 16));
+  const hipError_t e = by_width(a.n_experts, a.cfg.top_k, many ? 256 : 128, [&](auto lpr, auto epl) {
     constexpr int LPR = decltype(lpr)::value, EPL = decltype(epl)::value, kRows = kWave / LPR;
     a.vec = whole_lanes(a.logits, a.ld, a.n_experts, EPL, a.dtype);
-    const size_t room = groups_need_room(a, EPL) ? (size_t)kRows * a.n_experts * sizeof(double) : 0;  // a wave
-    if constexpr (LPR * EPL <= 256) {
+    const bool any_groups = !groups_of_lanes(a, EPL);
+    if constexpr (LPR * EPL <= 256 && EPL <= 8) {
       // Rows that its waves take at once: 1 to 64 rows, 64 experts, 6 choices 7.9 to 8.2 us, as two launches 10.5; 128
-      // rows 11.0 and 10.5.  A wave a row: only half as many (256 experts in groups with a bias, 5 rows 10.2 and
-      // 11.4 us, 16 rows 13.3 and 11.6).
-      if (plan && (int64_t)a.n_max * a.cfg.top_k <= kPlanTile && a.n_max <= (LPR == 16 ? 64 : 8) &&
-          room * kPlanWaves <= 32 << 10) {
+      // rows 11.0 and 10.5.  A wave a row: half as many (256 experts in groups with a bias, 5 rows 9.9 and 11.4 us, 16
+      // rows 12.6 and 11.6).
+      if (plan && !any_groups && (int64_t)a.n_max * a.cfg.top_k <= kPlanTile && a.n_max <= (LPR == 16 ? 64 : 8)) {
         planned = true;
         if (by_score)
-          hipLaunchKernelGGL((k_route_few<LPR, EPL, true>), dim3(1), dim3(kPlanThreads), room * kPlanWaves, st, a, *plan);
+          hipLaunchKernelGGL((k_route_few<LPR, EPL, kByScore>), dim3(1), dim3(kPlanThreads), 0, st, a, *plan);
         else
-          hipLaunchKernelGGL((k_route_few<LPR, EPL, false>), dim3(1), dim3(kPlanThreads), 0, st, a, *plan);
+          hipLaunchKernelGGL((k_route_few<LPR, EPL, kByLogit>), dim3(1), dim3(kPlanThreads), 0, st, a, *plan);
         return hipGetLastError();
       }
     }
-    const dim3 grid = blocks_for(a.n_max, 4 * kRows);
-    if (by_score) hipLaunchKernelGGL((k_route<LPR, EPL, true>), grid, dim3(256), room * 4, st, a);
-    else hipLaunchKernelGGL((k_route<LPR, EPL, false>), grid, dim3(256), 0, st, a);
+    const dim3 grid = blocks_for(a.n_max, 4 * kRows), block(256);
+    const size_t room = (size_t)4 * kRows * a.n_experts * sizeof(double);
+    if (any_groups) {
+      if constexpr (LPR * EPL < 256 || LPR == 64) hipLaunchKernelGGL((k_route<LPR, EPL, kByAnyGroups>), grid, block, room, st, a);
+    } else if (by_score) hipLaunchKernelGGL((k_route<LPR, EPL, kByScore>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((k_route<LPR, EPL, kByLogit>), grid, block, 0, st, a);
     return hipGetLastError();
   });
   if (e != hipSuccess || !plan || planned) return e;
@@ -707,7 +713,7 @@ hipError_t launch_route(const RouteArgs &args, const PlanArgs *plan, hipStream_t
 hipError_t launch_route_grad(const RouteGradArgs &args, hipStream_t st) {
   RouteGradArgs a = args;
   if (a.n_max == 0) return hipSuccess;
-  return by_width(a.n_experts, a.cfg.top_k, [&](auto lpr, auto epl) {
+  return by_width(a.n_experts, a.cfg.top_k, 128, [&](auto lpr, auto epl) {
     constexpr int LPR = decltype(lpr)::value, EPL = decltype(epl)::value;
     a.vec = whole_lanes(a.logits, a.ld, a.n_experts, EPL, a.dtype) &&
             whole_lanes(a.dlogits, a.ld_out, a.n_experts, EPL, a.dtype);

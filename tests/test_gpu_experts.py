@@ -764,3 +764,14 @@ def test_block_repeats_bit_for_bit_on_another_stream_and_in_a_graph():
         torch.cuda.synchronize()
         for k in want:
             assert torch.equal(want[k], out[k]), (turn, k)
+
+
+@pytest.mark.parametrize("n", [9000, 129, 65, 64, 8])
+def test_route_by_every_number_of_lanes(n):
+    """Row counts on both sides of where the kernels change, with ties in every row: the lowest index comes first."""
+    for E, K, kw in ((256, 8, dict(groups=8, top_groups=4, group_best=2)), (256, 8, dict()), (200, 3, dict(groups=8, top_groups=3)),
+                     (64, 6, dict()), (64, 16, dict(groups=16, top_groups=9, group_best=2)),
+                     (64, 17, dict()))[:1 if n > 1000 else None]:
+        x = (normal((n, E), F32, 5, 1.5) * 4).round() / 4
+        check_route(x, K, "sigmoid", bias=((normal((E,), F32, 6) * 2).round() / 8).numpy(), **kw)
+        check_route(x, K, "softmax", **kw)
