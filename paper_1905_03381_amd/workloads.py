@@ -7,6 +7,7 @@
     python -m paper_1905_03381_amd.workloads stale         # stale Boss / Assistant pipeline
     python -m paper_1905_03381_amd.workloads rho           # dense fused step at fixed keep rates
     python -m paper_1905_03381_amd.workloads score         # dense scoring pass at growing pool sizes
+    python -m paper_1905_03381_amd.workloads experts       # a Boss with a block of experts on the kept rows
 
 Each prints one JSON line: the stages of the workload with their time per call (HIP events
 on the launch stream, median of the repeats), the bytes each stage has to move and the
@@ -377,7 +378,80 @@ def score(a, torch, api, synth):
             "stages": stages}
 
 
-WORKLOADS = {"rho": rho, "sparse": sparse, "images": images, "translation": translation, "sk": sk,
+def experts(a, torch, api, synth):
+    """A Boss with a block of 32 gated experts, four a row, trained on the rows the Assistant keeps.
+
+    n rows of 512 in pools of 16,384 (fewer if n is smaller): score + keep, gather of the kept rows in bf16, the block
+    and a linear read-out with hinge loss, gradients, SGD on fp32 copies of the weights, running-median threshold and
+    Assistant update.  The host never waits inside a step."""
+    from .boss import ExpertBlock
+    n, d, f, E, K = a.n or 262_144, 512, 512, 32, 4
+    P = min(16_384, n // 4)
+    X, y, _ = synth.dense_svm(n=n, d=d, threads=a.threads)
+    X *= d ** 0.5
+    Xd, yd = torch.from_numpy(X).cuda(), torch.from_numpy(y).cuda()
+    Xb, F = Xd.to(torch.bfloat16), api.Features.dense(Xd)
+    perm = torch.from_numpy(synth.epoch_permutation(n, seed=7, epoch=0)).cuda()
+    block = ExpertBlock(P, d, f, E, K, p=0.1)
+    masters = [w.float() for w in block.weights()]
+    z = lambda *s, t=torch.float32: torch.zeros(*s, dtype=t, device="cuda")
+    read = torch.from_numpy(synth.planted_w(d, seed=5)).cuda() * d ** -0.5
+    ws, phi, b, T = api.Workspace(P, d), z(d), z(1), z(1)
+    seen, cnt = z(1, t=torch.int32), z(1, t=torch.int32)
+    prob, keep, pos, ids = z(P), z(P, t=torch.uint8), z(P, t=torch.int32), z(P, t=torch.int32)
+    x, out, dout, dx = (z(P, d, t=torch.bfloat16) for _ in range(4))
+    row, loss = torch.arange(P, device="cuda"), z(P)
+
+    def generate(t):
+        idx = perm[t * P:(t + 1) * P]
+        api.score_shrink(F, idx, P, phi, b, 0.1, 42, t, None, prob, keep, pos, cnt, ws)
+        api.gather(Xb, 2 * d, idx, pos, cnt, P, x, ids)
+
+    def forward(t):
+        block.forward(x, cnt, t, out)
+        yk, live = yd[ids.long()], row < cnt
+        margin = yk * (out.float() @ read)
+        loss.copy_(torch.where(live, (1 - margin).clamp(min=0), 0.0))
+        slope = torch.where(live & (margin < 1), -yk / cnt.clamp(min=1), 0.0)
+        dout.copy_(slope[:, None] * read)
+
+    def backward(t):
+        block.backward(x, cnt, t, dout, dx)
+
+    def update(t):
+        for w, m, g in zip(block.weights(), masters, block.grads):
+            m.add_(g, alpha=-16.0)
+            w.copy_(m)
+        api.threshold_update(loss, cnt, P, 0.9, T, seen)
+        api.assistant_update(F, ids, cnt, P, loss, T, phi, b, 0.1, 0.0, ws)
+
+    steps, kept, losses, times = max(1, n // P), [], [], {}
+    for epoch in range(3):
+        for t in range(steps):
+            marks = [torch.cuda.Event(enable_timing=True) for _ in range(5)]
+            marks[0].record()
+            for part, after in zip((generate, forward, backward, update), marks[1:]):
+                part(epoch * steps + t if part in (forward, backward) else t)
+                after.record()
+            if epoch or t:                          # the first step loads the kernels
+                for name, lo, hi in zip(("generate", "forward", "backward", "update"), marks, marks[1:]):
+                    times.setdefault(name, []).append((lo, hi))
+            kept.append(cnt.clone())
+            losses.append(loss.sum() / cnt.clamp(min=1))
+    torch.cuda.synchronize()
+    us = {k: float(np.median([lo.elapsed_time(hi) * 1e3 for lo, hi in v])) for k, v in times.items()}
+    m = float(torch.stack(kept).float().mean())
+    flops = 2 * m * K * 3 * f * d
+    curve = torch.stack(losses).view(-1).tolist()
+    stages = [_stage("score + keep + gather of the kept rows (bf16)", us["generate"], P * (4 * d + 9) + m * 4 * d),
+              _stage("block of experts, read-out and loss", us["forward"], note=f"{flops / us['forward'] / 1e6:.0f} TFLOP/s"),
+              _stage("gradients", us["backward"], note=f"{2 * flops / us['backward'] / 1e6:.0f} TFLOP/s"),
+              _stage("SGD on the block, threshold and Assistant update", us["update"])]
+    return {"workload": f"Boss of {E} experts ({K} a row), n={n} d={d} f={f} pool={P}", "stages": stages,
+            "kept_per_pool": m, "loss_first": curve[0], "loss_last": curve[-1]}
+
+
+WORKLOADS = {"experts": experts, "rho": rho, "sparse": sparse, "images": images, "translation": translation, "sk": sk,
              "stale": stale, "score": score}
 
 

@@ -775,3 +775,44 @@ def test_route_by_every_number_of_lanes(n):
         x = (normal((n, E), F32, 5, 1.5) * 4).round() / 4
         check_route(x, K, "sigmoid", bias=((normal((E,), F32, 6) * 2).round() / 8).numpy(), **kw)
         check_route(x, K, "softmax", **kw)
+
+
+def test_boss_block_trains_on_what_the_assistant_keeps(capsys):
+    """The experts workload end to end: kept rows only, and a loss that falls."""
+    import json
+    from paper_1905_03381_amd import workloads
+    workloads.main(["experts", "--n", "32768", "--threads", "4"])
+    out = json.loads([l for l in capsys.readouterr().out.splitlines() if l.startswith("{")][0])
+    assert all(s["us"] > 0 for s in out["stages"]) and 0 < out["kept_per_pool"] <= 8192
+    assert out["loss_last"] < 0.8 * out["loss_first"], out
+
+
+def test_boss_block_gradients_against_autograd():
+    """ExpertBlock with the router's share of the input's gradient, against automatic differentiation in 64 bits.  As
+    above: 16 half steps of the largest value, one more rounding for the router's part."""
+    from paper_1905_03381_amd.boss import ExpertBlock
+    n, m, E, K, d, f = 70, 61, 8, 2, 64, 48
+    block = ExpertBlock(n, d, f, E, K, p=0.2)
+    x, dout = normal((n, d), BF16, 3).cuda(), normal((n, d), BF16, 4).cuda()
+    count = torch.tensor([m], dtype=torch.int32, device="cuda")
+    out, dx = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    block.forward(x, count, 9, out)
+    block.backward(x, count, 9, dout, dx)
+    assert (out[m:] == 7).all() and (dx[m:] == 7).all()
+    X = x[:m].double().cpu().requires_grad_(True)
+    Wr, W1, W2 = (w.double().cpu().requires_grad_(True) for w in block.weights())
+    ids = block.ids[:m].cpu().long()
+    s = torch.softmax(X @ Wr[0].t(), 1).gather(1, ids)
+    wts = s / s.sum(1, keepdim=True)
+    y = torch.zeros(m, d, dtype=torch.float64)
+    for k in range(K):
+        h = (W1[ids[:, k]] @ X[:, :, None])[:, :, 0]
+        h = torch.nn.functional.silu(h[:, :f]) * h[:, f:]
+        y = y + wts[:, k:k + 1] * (W2[ids[:, k]] @ h[:, :, None])[:, :, 0]
+    want = X + y * torch.from_numpy(R.drop_factor(m, d, 0.2, block.seed, 9))
+    want.backward(dout[:m].double().cpu())
+    u = 17 * half_step(BF16)
+    for name, got, ref in (("out", out[:m], want), ("dx", dx[:m], X.grad), ("router", block.grads[0], Wr.grad),
+                           ("gate_up", block.grads[1], W1.grad), ("down", block.grads[2], W2.grad)):
+        w = ref.detach().numpy()
+        assert np.abs(f64(got) - w).max() <= u * np.abs(w).max(), (name, np.abs(f64(got) - w).max(), np.abs(w).max())
