@@ -32,6 +32,7 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef s16x8 s16x8_any __attribute__((aligned(2)));  // (global memory is read at any address)
 
 constexpr int kStep = 64;  // summed dimension of one LDS tile
 
@@ -47,6 +48,13 @@ __device__ __forceinline__ f4 mfma16(const s16x8 a, const s16x8 b, const f4 c, _
 
 // What is read where the summed dimension has ended.
 __device__ const uint4 kZeros = {0u, 0u, 0u, 0u};
+
+// Sixteen bytes at p, or zeros.  (Said to be global memory: a choice between two pointers would be read as memory of any
+// kind, and what waits for LDS then waits for it.)
+typedef const __attribute__((address_space(1))) s16x8_any global16;
+__device__ __forceinline__ global16 *there_or_zeros(const void *p, bool there) {
+  return there ? (global16 *)p : (global16 *)&kZeros;
+}
 
 __device__ __forceinline__ void load_lds16(const void *src, char *dst) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
@@ -91,6 +99,7 @@ struct Stage {
   int left[2];
   const int32_t *order;
   int top_k, next[TR && GATHER ? kSlots : 1];
+  s16x8 held[ALIGNED ? 1 : kSlots];
 
   static __device__ int k_row(int it, int t) { return it * kRowsASlot + t / kChunks; }
   static __device__ int chunk(int it, int t) {
@@ -155,7 +164,8 @@ struct Stage {
     }
   }
 
-  // The slice of k, k + 1, .. k + kStep - 1; what lies at or past k_end is zero.
+  // The slice of k, k + 1, .. k + kStep - 1; what lies at or past k_end is zero.  ALIGNED: its transfer to LDS.  Else
+  // it is asked for here and waits in registers for put().
   template <bool TAIL>
   __device__ void load(char *lds, int k, int k_end) {
     const int t = fresh_thread(k), wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -168,19 +178,29 @@ struct Stage {
 #pragma unroll
     for (int it = 0; it < kSlots; ++it) {
       const T *src = source(it, k, t, TR && GATHER ? now[TR && GATHER ? it : 0] : 0);
-      const int n = TR ? left[it & 1] : k_end - (k + chunk(0, t) * 8);  // elements of the chunk that exist (not ALIGNED)
       const bool there = !TAIL || (TR ? k + k_row(it, t) : k + chunk(0, t) * 8) < k_end;
-      if (ALIGNED) {
+      if constexpr (ALIGNED) {
         if (TAIL) src = there ? src : reinterpret_cast<const T *>(&kZeros);
         load_lds16(src, lds + (it * NT + wave * kWave) * 16);
       } else {
-        s16x8 v;
-        const short *p = reinterpret_cast<const short *>(src), *zero = reinterpret_cast<const short *>(&kZeros);
+        // elements of the chunk that exist
+        const int n = there ? (TR ? left[it & 1] : k_end - (k + chunk(0, t) * 8)) : 0;
+        held[it] = *there_or_zeros(src, n >= 8);
+        if (n > 0 && n < 8) {
+          const short *p = reinterpret_cast<const short *>(src);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = *(there && j < n ? p + j : zero);  // (no branch: all are asked for at once)
-        *reinterpret_cast<s16x8 *>(lds + (it * NT + t) * 16) = v;
+          for (int j = 0; j < 8; ++j) {
+            const short v = p[j < n ? j : 0];
+            held[it][j] = j < n ? v : (short)0;
+          }
+        }
       }
     }
+  }
+
+  __device__ void put(char *lds) {
+#pragma unroll
+    for (int it = 0; it < kSlots; ++it) *reinterpret_cast<s16x8 *>(lds + (it * NT + (int)threadIdx.x) * 16) = held[it];
   }
 };
 
@@ -190,6 +210,13 @@ template <int N>
 __device__ __forceinline__ void wait_and_meet() {
   __builtin_amdgcn_sched_barrier(0);
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// The same where nothing is transferred to LDS but written: what registers wait for may still be on its way.
+__device__ __forceinline__ void meet() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
   __builtin_amdgcn_sched_barrier(0);
 }
 
@@ -480,6 +507,23 @@ __global__ __launch_bounds__(WI *WJ *kWave, 2) void k_product(const ProductArgs 
       Q.template load<true>(to + kBytesP, at, k_end);
     }
   };
+  auto put = [&](char *to) __attribute__((always_inline)) {
+    if constexpr (!ALIGNED) {
+      P.put(to);
+      Q.put(to + kBytesP);
+    }
+  };
+  // The slice two steps on into the buffer that is free (not ALIGNED: it has come to the registers during the last
+  // step, and the one after it is asked for).
+  auto refill = [&](char *to, int at, int k_end) __attribute__((always_inline)) {
+    if (at >= k_end) return;
+    if constexpr (ALIGNED) {
+      load(to, at, k_end);
+    } else {
+      put(to);
+      if (at + kStep < k_end) load(nullptr, at + kStep, k_end);
+    }
+  };
   // Takes up a tile: its addresses, and its first slices on their way.
   constexpr int kFirst = NB == 2 ? 2 : NB - 1;
   auto begin = [&](const Tile &g) __attribute__((always_inline)) {
@@ -508,7 +552,11 @@ __global__ __launch_bounds__(WI *WJ *kWave, 2) void k_product(const ProductArgs 
       if constexpr (TRQ) Q.ask_rows(g.k0, g.k_end);
 #pragma unroll
       for (int b = 0; b < kFirst; ++b)
-        if (b == 0 || g.k0 + b * kStep < g.k_end) load(smem + b * kBuffer, g.k0 + b * kStep, g.k_end);
+        if (b == 0 || g.k0 + b * kStep < g.k_end) {
+          load(smem + b * kBuffer, g.k0 + b * kStep, g.k_end);
+          put(smem + b * kBuffer);
+        }
+      if (!ALIGNED && g.k0 + kFirst * kStep < g.k_end) load(nullptr, g.k0 + kFirst * kStep, g.k_end);
     }
   };
 
@@ -556,7 +604,8 @@ __global__ __launch_bounds__(WI *WJ *kWave, 2) void k_product(const ProductArgs 
     // of one that has been used.  Early in the second half of a step everybody has read its buffer and the next
     // one has arrived: the slice two steps on goes into the free buffer during the rest.
     if (NB == 2 && k < k_end) {
-      if (ALIGNED && k + kStep < k_end) wait_and_meet<kLoads>();
+      if (!ALIGNED) meet();
+      else if (k + kStep < k_end) wait_and_meet<kLoads>();
       else wait_and_meet<0>();
       if (live) {
         s16x8 fp[2][FI], fq[2][FJ];
@@ -580,7 +629,8 @@ __global__ __launch_bounds__(WI *WJ *kWave, 2) void k_product(const ProductArgs 
           multiply(0, 0, FI);
           interleave<kReads, 0, FI * FJ>();
           multiply(1, 0, kAhead);
-          wait_and_meet<0>();
+          if constexpr (ALIGNED) wait_and_meet<0>();
+          else meet();
           if constexpr (decltype(whole)::value) {  // the slice two steps on is there and is a whole one
             read(0, other, 0);
             P.template load<false>(here, k + 2 * kStep, k_end);
@@ -588,7 +638,7 @@ __global__ __launch_bounds__(WI *WJ *kWave, 2) void k_product(const ProductArgs 
             multiply(1, kAhead, FI);
             interleave<kReads, kLoads, (FI - kAhead) * FJ>();
           } else {
-            if (k + 2 * kStep < k_end) load(here, k + 2 * kStep, k_end);
+            refill(here, k + 2 * kStep, k_end);
             read(0, other, 0);
             multiply(1, kAhead, FI);
             interleave<kReads, 0, (FI - kAhead) * FJ>();
@@ -604,8 +654,9 @@ __global__ __launch_bounds__(WI *WJ *kWave, 2) void k_product(const ProductArgs 
         for (; k < k_end; buf ^= 1) step(smem + buf * kBuffer, smem + (buf ^ 1) * kBuffer, std::false_type());
       } else {
         for (int odd = 0; k < k_end; k += kStep, odd ^= 1) {
-          wait_and_meet<0>();
-          if (k + 2 * kStep < k_end) load(smem + odd * kBuffer, k + 2 * kStep, k_end);
+          if constexpr (ALIGNED) wait_and_meet<0>();
+          else meet();
+          refill(smem + odd * kBuffer, k + 2 * kStep, k_end);
         }
       }
     }
@@ -685,13 +736,14 @@ __global__ __launch_bounds__(256) void k_product_few(const ProductArgs a) {
   }
   if (e < 0) return;
   e = __builtin_amdgcn_readfirstlane(e);
-  const int j0 = blockIdx.x * (16 * kOut), K = a.d_in;
+  // (rows at any address; what is left of a chunk of eight at the end comes last)
+  const int j0 = blockIdx.x * (16 * kOut), K = a.d_in & ~7, rest = a.d_in & 7;
   const T *w = static_cast<const T *>(a.mat) + (size_t)e * a.d_out * a.d_in * (GATED ? 2 : 1);
   const T *wr[NF];  // a lane's matrix rows
 #pragma unroll
   for (int f = 0; f < NF; ++f) {
     const int c = min(j0 + f % kOut * 16 + (lane & 15), a.d_out - 1) + (GATED && f >= kOut ? a.d_out : 0);
-    wr[f] = w + (size_t)c * K + (lane >> 4) * 8;
+    wr[f] = w + (size_t)c * a.d_in + (lane >> 4) * 8;
   }
   for (int q0 = lo; q0 < hi; q0 += 16 * MF) {
     const T *xr[MF];
@@ -709,8 +761,7 @@ __global__ __launch_bounds__(256) void k_product_few(const ProductArgs a) {
         const bool there = at + (lane >> 4) * 8 < K;
 #pragma unroll
         for (int f = 0; f < NF; ++f)
-          fw[slot][f][h] = __builtin_nontemporal_load(
-              there ? reinterpret_cast<const s16x8 *>(wr[f] + at) : reinterpret_cast<const s16x8 *>(&kZeros));
+          fw[slot][f][h] = __builtin_nontemporal_load(there_or_zeros(wr[f] + at, there));
       }
     };
     auto ask_rows = [&](int slot, int k) __attribute__((always_inline)) {
@@ -720,7 +771,7 @@ __global__ __launch_bounds__(256) void k_product_few(const ProductArgs a) {
         const bool there = at + (lane >> 4) * 8 < K;
 #pragma unroll
         for (int m = 0; m < MF; ++m)
-          fx[slot][m][h] = *(there ? reinterpret_cast<const s16x8 *>(xr[m] + at) : reinterpret_cast<const s16x8 *>(&kZeros));
+          fx[slot][m][h] = *there_or_zeros(xr[m] + at, there);
       }
     };
     constexpr int kTurn = kWaves * kStep;
@@ -748,6 +799,25 @@ __global__ __launch_bounds__(256) void k_product_few(const ProductArgs a) {
         ask_rows(s, k + kAhead * kTurn);
         k += kTurn;
       }
+    }
+    if (rest != 0 && wave == kWaves - 1) {
+      const auto ends = [&](const T *row) {  // (the first lanes of four hold it, the others zeros)
+        s16x8 v = {0, 0, 0, 0, 0, 0, 0, 0};
+        const short *p = reinterpret_cast<const short *>(row + K);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < rest && lane < 16) v[i] = p[i];
+        return v;
+      };
+      s16x8 ew[NF], ex[MF];
+#pragma unroll
+      for (int f = 0; f < NF; ++f) ew[f] = ends(wr[f]);
+#pragma unroll
+      for (int m = 0; m < MF; ++m) ex[m] = ends(xr[m]);
+#pragma unroll
+      for (int f = 0; f < NF; ++f)
+#pragma unroll
+        for (int m = 0; m < MF; ++m) acc[f][m] = mfma16(ew[f], ex[m], acc[f][m], T());
     }
     if (wave > 0) {
 #pragma unroll
@@ -855,8 +925,8 @@ hipError_t launch_few(const ProductArgs &a, hipStream_t st) {
 template <typename T, int MODE, int ACT>
 hipError_t launch_product(const ProductArgs &a, hipStream_t st) {
   if (MODE != kGradWeight && a.rows_max == 0) return hipSuccess;
-  if (!a.aligned) return launch_tiles<T, MODE, ACT, 2, 2, 4, 4, 2, false>(a, st);
   if (MODE == kGradWeight) {
+    if (!a.aligned) return launch_tiles<T, MODE, ACT, 2, 2, 4, 4, 2, false>(a, st);
     // (parts make up for few tiles; 4 experts x 10,000 rows, 256 x 256: 30 us in tiles of 256, 27 of 128; 16 x 750 rows,
     // 1000 x 520: 30 and 43)
     if ((int64_t)a.d_in * a.d_out <= 256 * 256) return launch_tiles<T, MODE, ACT, 2, 2, 4, 4, 2, true>(a, st);
@@ -875,6 +945,7 @@ hipError_t launch_product(const ProductArgs &a, hipStream_t st) {
       if (rows <= 32 && n128 <= 320)
         return rows <= 16 ? launch_few<T, ACT, 2, 1>(a, st) : launch_few<T, ACT, 2, 2>(a, st);
     }
+    if (!a.aligned) return launch_tiles<T, MODE, ACT, 2, 2, 4, 4, 2, false>(a, st);
     if (t32 < t128 && t32 < t256) return launch_tiles<T, MODE, ACT, 2, 2, 1, 2, 6, true>(a, st);
     if (t128 < t256) return launch_tiles<T, MODE, ACT, 2, 2, 4, 4, 2, true>(a, st);
     return launch_tiles<T, MODE, ACT, 2, 4, 8, 4, 2, true>(a, st);
