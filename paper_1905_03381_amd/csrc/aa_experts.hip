@@ -17,6 +17,10 @@
 // and spilled) 1126 / 1295 / 1348; blocks that stay and ask for the next tile's slices before they write this one's results: 16,384 x 2048 x
 // 2048 forward 1130 -> 1200.  Four waves of 128 x 128 (709) and tiles of 128 x 256 in steps of 32, two a compute unit
 // (870 to 916), were slower.
+//
+// Operands off 16-byte boundaries or of widths that are no multiples of 8 are read into registers, sixteen bytes at a time at
+// any address, while the slice before is multiplied, and written to LDS from there.  (Two bytes at a time, and waited for
+// where they were asked for: 271 x 6 rows of 8 experts, 1893 x 2808, 179 us; now 56.)
 #include "aa_experts.hpp"
 
 #include "aa_route.hpp"
@@ -945,6 +949,7 @@ hipError_t launch_product(const ProductArgs &a, hipStream_t st) {
       if (rows <= 32 && n128 <= 320)
         return rows <= 16 ? launch_few<T, ACT, 2, 1>(a, st) : launch_few<T, ACT, 2, 2>(a, st);
     }
+    // (what goes through registers: the one tile that has them.  271 x 6 rows, 8 experts of 1893 x 2808: 56 us)
     if (!a.aligned) return launch_tiles<T, MODE, ACT, 2, 2, 4, 4, 2, false>(a, st);
     if (t32 < t128 && t32 < t256) return launch_tiles<T, MODE, ACT, 2, 2, 1, 2, 6, true>(a, st);
     if (t128 < t256) return launch_tiles<T, MODE, ACT, 2, 2, 4, 4, 2, true>(a, st);
