@@ -203,7 +203,6 @@ int32_t aa_expert_forward(const void *x, int32_t dtype, int64_t ldx, const int32
   a.ldpre = ldpre;
   a.act = act;
   a.aligned = d_in % 8 == 0 && in_reach(x, rows_max, ldx) && in_reach(w, 2 * (int64_t)d_out, d_in);
-  a.out_vec = rows_on_16(out, ldo, 2) && (!pre || (rows_on_16(pre, ldpre, 2) && d_out % 8 == 0));
   return hip_status(launch_expert_forward(a, dtype == AA_F16, as_stream(stream)));
 }
 
@@ -233,8 +232,6 @@ int32_t aa_expert_grad_input(const void *dout, int32_t dtype, int64_t lddo, cons
   a.lds = lds;
   a.act = act;
   a.aligned = d_in % 8 == 0 && d_out % 8 == 0 && in_reach(dout, rows_max, lddo) && columns_in_reach(w, d_in);
-  a.out_vec = rows_on_16(dx, lddx, 2) && (act != AA_ACT_GATED || d_in % 8 == 0) &&
-              (act == AA_ACT_NONE || rows_on_16(saved, lds, 2));
   return hip_status(launch_expert_grad_input(a, dtype == AA_F16, as_stream(stream)));
 }
 
@@ -266,7 +263,6 @@ int32_t aa_expert_grad_weight(const void *dout, int32_t dtype, int64_t lddo, con
   a.out_f32 = out_dtype == AA_F32;
   a.accumulate = accumulate != 0;
   a.aligned = d_in % 8 == 0 && d_out % 8 == 0 && columns_in_reach(dout, lddo) && columns_in_reach(x, ldx);
-  a.out_vec = rows_on_16(dw, d_in, type_bytes(out_dtype));
   a.partial = reinterpret_cast<float *>(static_cast<char *>(ws) + 256);
   a.partial_bytes = kGradWeightPartialBytes;
   return hip_status(launch_expert_grad_weight(a, dtype == AA_F16, as_stream(stream)));
@@ -291,7 +287,6 @@ int32_t aa_dropout(const void *x, int32_t dtype, int64_t ldx, const int32_t *cou
   a.ldr = ldr;
   a.out = out;
   a.ldo = ldo;
-  a.vec = rows_on_16(x, ldx, bytes) && rows_on_16(out, ldo, bytes) && (!residual || rows_on_16(residual, ldr, bytes));
   return hip_status(launch_dropout(a, dtype, as_stream(stream)));
 }
 
@@ -320,7 +315,6 @@ int32_t aa_expert_combine(const void *y, int32_t dtype, int64_t ldy, const int32
   a.ldr = ldr;
   a.out = out;
   a.ldo = ldo;
-  a.vec = rows_on_16(y, ldy, bytes) && rows_on_16(out, ldo, bytes) && (!residual || rows_on_16(residual, ldr, bytes));
   return hip_status(launch_expert_combine(a, dtype, as_stream(stream)));
 }
 
@@ -352,7 +346,6 @@ int32_t aa_expert_combine_grad(const void *dout, int32_t dtype, int64_t lddo, co
   a.out = dy;
   a.ldo = lddy;
   a.dweights = dweights;
-  a.vec = rows_on_16(dout, lddo, bytes) && rows_on_16(dy, lddy, bytes) && (!dweights || rows_on_16(y, ldy, bytes));
   return hip_status(launch_expert_combine_grad(a, dtype, as_stream(stream)));
 }
 

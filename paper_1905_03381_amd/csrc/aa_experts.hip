@@ -293,17 +293,17 @@ __device__ __forceinline__ int group_of_tile(const int *before, int n_experts, i
 
 __device__ __forceinline__ float sigmoid_fast(float v) { return 1.0f / (1.0f + __expf(-v)); }
 
-// N (4 or 8) neighbouring results of a lane; the first n of them exist, vec: and can be moved at once.
+// N (4 or 8) neighbouring results of a lane, at any address; the first n of them exist.
 template <int N>
 struct Run {
   float v[N];
 };
 
 template <typename T, int N>
-__device__ __forceinline__ void store_run(T *p, const Run<N> &x, int n, bool vec) {
+__device__ __forceinline__ void store_run(T *p, const Run<N> &x, int n) {
   constexpr int kPer = N * sizeof(T) < 16 ? N : 16 / sizeof(T);
-  typedef T Line __attribute__((ext_vector_type(kPer)));
-  if (vec && n >= N) {
+  typedef T Line __attribute__((ext_vector_type(kPer), aligned(sizeof(T))));
+  if (n >= N) {
 #pragma unroll
     for (int h = 0; h < N / kPer; ++h) {
       Line o;
@@ -319,11 +319,11 @@ __device__ __forceinline__ void store_run(T *p, const Run<N> &x, int n, bool vec
 }
 
 template <typename T, int N>
-__device__ __forceinline__ Run<N> load_run(const T *p, int n, bool vec) {
+__device__ __forceinline__ Run<N> load_run(const T *p, int n) {
   constexpr int kPer = N * sizeof(T) < 16 ? N : 16 / sizeof(T);
-  typedef T Line __attribute__((ext_vector_type(kPer)));
+  typedef T Line __attribute__((ext_vector_type(kPer), aligned(sizeof(T))));
   Run<N> x;
-  if (vec && n >= N) {
+  if (n >= N) {
 #pragma unroll
     for (int h = 0; h < N / kPer; ++h) {
       const Line o = reinterpret_cast<const Line *>(p)[h];
@@ -357,7 +357,6 @@ template <typename T, int MODE, int ACT, int N>
 __device__ __forceinline__ void finish(const ProductArgs &a, int64_t q, int j, const Run<N> &v, const Run<N> &up) {
   T *o = static_cast<T *>(a.out) + q * a.ldo + j;
   const int n = (MODE == kForward ? a.d_out : a.d_in) - j;
-  const bool vec = a.out_vec;
   Run<N> r = v;
   if (MODE == kForward) {
     if (ACT == AA_ACT_RELU) {
@@ -369,17 +368,17 @@ __device__ __forceinline__ void finish(const ProductArgs &a, int64_t q, int j, c
       for (int i = 0; i < N; ++i) r.v[i] = v.v[i] * sigmoid_fast(v.v[i]) * up.v[i];
       if (a.pre) {
         T *h = static_cast<T *>(a.pre) + q * a.ldpre + j;
-        store_run(h, v, n, vec);
-        store_run(h + a.d_out, up, n, vec);
+        store_run(h, v, n);
+        store_run(h + a.d_out, up, n);
       }
     }
   } else if (ACT == AA_ACT_RELU) {
-    const Run<N> s = load_run<T, N>(static_cast<const T *>(a.saved) + q * a.lds + j, n, vec);
+    const Run<N> s = load_run<T, N>(static_cast<const T *>(a.saved) + q * a.lds + j, n);
 #pragma unroll
     for (int i = 0; i < N; ++i) r.v[i] = s.v[i] > 0.f ? v.v[i] : 0.f;
   } else if (ACT == AA_ACT_GATED) {
     const T *s = static_cast<const T *>(a.saved) + q * a.lds + j;
-    const Run<N> g = load_run<T, N>(s, n, vec), u = load_run<T, N>(s + a.d_in, n, vec);
+    const Run<N> g = load_run<T, N>(s, n), u = load_run<T, N>(s + a.d_in, n);
     Run<N> du;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -387,20 +386,20 @@ __device__ __forceinline__ void finish(const ProductArgs &a, int64_t q, int j, c
       r.v[i] = v.v[i] * u.v[i] * (z + g.v[i] * z * (1.0f - z));
       du.v[i] = v.v[i] * g.v[i] * z;
     }
-    store_run(o + a.d_in, du, n, vec);
+    store_run(o + a.d_in, du, n);
   }
-  store_run(o, r, n, vec);
+  store_run(o, r, n);
 }
 
 template <typename T, int N>
-__device__ __forceinline__ void finish_weight(T *o, const Run<N> &v, int n, bool accumulate, bool vec) {
+__device__ __forceinline__ void finish_weight(T *o, const Run<N> &v, int n, bool accumulate) {
   Run<N> r = v;
   if (accumulate) {
-    const Run<N> old = load_run<T, N>(o, n, vec);
+    const Run<N> old = load_run<T, N>(o, n);
 #pragma unroll
     for (int i = 0; i < N; ++i) r.v[i] += old.v[i];
   }
-  store_run(o, r, n, vec);
+  store_run(o, r, n);
 }
 
 // Where the parts of a sum over a long range of rows go: part s of tile t is [BM][BN] at (t parts + s) BM BN.
@@ -696,11 +695,11 @@ __global__ __launch_bounds__(WI *WJ *kWave, 2) void k_product(const ProductArgs 
           if constexpr (MODE == kGradWeight) {
             const size_t at = ((size_t)done.e * a.d_out + r) * a.d_in + c;
             if (a.parts > 1)
-              store_run(a.partial + (done.unit * BM + (r - done.i0)) * BN + (c - done.j0), v, 8, true);
+              store_run(a.partial + (done.unit * BM + (r - done.i0)) * BN + (c - done.j0), v, 8);
             else if (a.out_f32)
-              finish_weight(static_cast<float *>(a.out) + at, v, a.d_in - c, a.accumulate, a.out_vec);
+              finish_weight(static_cast<float *>(a.out) + at, v, a.d_in - c, a.accumulate);
             else
-              finish_weight(static_cast<T *>(a.out) + at, v, a.d_in - c, a.accumulate, a.out_vec);
+              finish_weight(static_cast<T *>(a.out) + at, v, a.d_in - c, a.accumulate);
           } else {
             finish<T, MODE, ACT>(a, r, c, v, up);
           }
@@ -865,8 +864,8 @@ __global__ __launch_bounds__(256) void k_join_parts(const ProductArgs a) {
   for (int s = 1; s < a.parts; ++s) sum += *reinterpret_cast<const f4 *>(p + (size_t)s * (BM * BN));
   const size_t at = ((size_t)e * a.d_out + r) * a.d_in + c;
   const Run<4> v = four_columns(sum);
-  if (a.out_f32) finish_weight(static_cast<float *>(a.out) + at, v, a.d_in - c, a.accumulate, a.out_vec);
-  else finish_weight(static_cast<T *>(a.out) + at, v, a.d_in - c, a.accumulate, a.out_vec);
+  if (a.out_f32) finish_weight(static_cast<float *>(a.out) + at, v, a.d_in - c, a.accumulate);
+  else finish_weight(static_cast<T *>(a.out) + at, v, a.d_in - c, a.accumulate);
 }
 
 constexpr int kUnits = 256;  // compute units

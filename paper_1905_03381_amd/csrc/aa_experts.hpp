@@ -23,7 +23,6 @@ struct ProductArgs {
   int32_t act;
   int32_t out_f32, accumulate;
   int32_t aligned;  // 16-byte chunks of the operands are whole and on 16-byte boundaries
-  int32_t out_vec;  // four neighbouring outputs (and what is read beside them) can be moved at once
   float *partial;   // grad_weight: room for the parts of a split sum
   size_t partial_bytes;
   int32_t parts;    // (chosen at launch) parts a tile's sum over rows comes in

@@ -38,13 +38,13 @@ struct Eight {
 };
 
 template <typename T>
-using Line = T __attribute__((ext_vector_type(8)));
+using Line = T __attribute__((ext_vector_type(8), aligned(sizeof(T))));  // (memory is read and written at any address)
 
-// Columns of which n exist, the others 0; vec: may be moved at once.
+// Columns of which n exist, the others 0.
 template <typename T>
-__device__ __forceinline__ Line<T> load_line(const T *p, int n, bool vec) {
+__device__ __forceinline__ Line<T> load_line(const T *p, int n) {
   Line<T> o;
-  if (vec && n >= 8) {
+  if (n >= 8) {
     o = *reinterpret_cast<const Line<T> *>(p);
   } else {
 #pragma unroll
@@ -57,8 +57,8 @@ __device__ __forceinline__ Line<T> load_line(const T *p, int n, bool vec) {
 }
 
 template <typename T>
-__device__ __forceinline__ Eight load8(const T *p, int n, bool vec) {
-  const Line<T> t = load_line(p, n, vec);
+__device__ __forceinline__ Eight load8(const T *p, int n) {
+  const Line<T> t = load_line(p, n);
   Eight o;
 #pragma unroll
   for (int i = 0; i < 8; ++i) o.v[i] = (float)t[i];
@@ -66,8 +66,8 @@ __device__ __forceinline__ Eight load8(const T *p, int n, bool vec) {
 }
 
 template <typename T>
-__device__ __forceinline__ void store8(T *p, const Eight &o, int n, bool vec) {
-  if (vec && n >= 8) {
+__device__ __forceinline__ void store8(T *p, const Eight &o, int n) {
+  if (n >= 8) {
     Line<T> t;
 #pragma unroll
     for (int i = 0; i < 8; ++i) t[i] = (T)o.v[i];
@@ -123,14 +123,14 @@ __global__ __launch_bounds__(256) void k_dropout(const DropoutArgs a) {
     T *o = static_cast<T *>(a.out) + (int64_t)row * a.ldo;
     for (int c = (threadIdx.x % TPR) * 8; c < a.d; c += TPR * 8) {
       const int n = a.d - c;
-      Eight v = load8(x + c, n, a.vec), add;
-      if (a.residual) add = load8(r + c, n, a.vec);
+      Eight v = load8(x + c, n), add;
+      if (a.residual) add = load8(r + c, n);
       drop8(a.key, row, c, v);
       if (a.residual) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v.v[i] += add.v[i];
       }
-      store8(o + c, v, n, a.vec);
+      store8(o + c, v, n);
     }
   }
 }
@@ -152,7 +152,7 @@ __global__ __launch_bounds__(256) void k_combine(const CombineArgs a) {
       const int n = a.d - c;
       Eight sum = {{0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}};
       Line<T> add;
-      if (a.residual) add = load_line(r + c, n, a.vec);
+      if (a.residual) add = load_line(r + c, n);
       for (int k0 = 0; k0 < K; k0 += kBatch) {
         Line<T> line[kBatch];
         int q[kBatch];
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(256) void k_combine(const CombineArgs a) {
         }
 #pragma unroll
         for (int j = 0; j < kBatch; ++j)
-          if (q[j] >= 0) line[j] = load_line(y + (int64_t)q[j] * a.ldy + c, n, a.vec);
+          if (q[j] >= 0) line[j] = load_line(y + (int64_t)q[j] * a.ldy + c, n);
 #pragma unroll
         for (int j = 0; j < kBatch; ++j) {
           if (q[j] < 0) continue;
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(256) void k_combine(const CombineArgs a) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum.v[i] += (float)add[i];
       }
-      store8(o + c, sum, n, a.vec);
+      store8(o + c, sum, n);
     }
   }
 }
@@ -208,12 +208,12 @@ __global__ __launch_bounds__(256) void k_combine_grad(const CombineArgs a) {
         const T *g_row = static_cast<const T *>(a.dout) + (int64_t)row * a.lddo;
         for (int c = t * 8; c < a.d; c += TPR * 8) {
           const int n = a.d - c;
-          Eight g = load8(g_row + c, n, a.vec);
+          Eight g = load8(g_row + c, n);
           Line<T> line[kBatch];
           if (a.dweights) {
 #pragma unroll
             for (int j = 0; j < kBatch; ++j)
-              if (q[j] >= 0) line[j] = load_line(y + (int64_t)q[j] * a.ldy + c, n, a.vec);
+              if (q[j] >= 0) line[j] = load_line(y + (int64_t)q[j] * a.ldy + c, n);
           }
           drop8(a.key, row, c, g);
 #pragma unroll
@@ -222,7 +222,7 @@ __global__ __launch_bounds__(256) void k_combine_grad(const CombineArgs a) {
             Eight d;
 #pragma unroll
             for (int i = 0; i < 8; ++i) d.v[i] = f[j] * g.v[i];
-            store8(dy + (int64_t)q[j] * a.ldo + c, d, n, a.vec);
+            store8(dy + (int64_t)q[j] * a.ldo + c, d, n);
           }
           if (a.dweights) {
 #pragma unroll

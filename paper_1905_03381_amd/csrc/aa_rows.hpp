@@ -22,7 +22,6 @@ struct DropoutArgs {
   DropKey key;
   void *out;
   int64_t ldo;
-  int32_t vec;  // rows lie on 16-byte boundaries
 };
 
 struct CombineArgs {
@@ -40,7 +39,6 @@ struct CombineArgs {
   void *out;  // combine: out; combine_grad: dy
   int64_t ldo;
   float *dweights;
-  int32_t vec;
 };
 
 hipError_t launch_dropout(const DropoutArgs &a, int32_t dtype, hipStream_t st);
