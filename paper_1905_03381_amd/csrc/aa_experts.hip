@@ -19,8 +19,9 @@
 // (870 to 916), were slower.
 //
 // Operands off 16-byte boundaries or of widths that are no multiples of 8 are read into registers, sixteen bytes at a time at
-// any address, while the slice before is multiplied, and written to LDS from there.  (Two bytes at a time, and waited for
-// where they were asked for: 271 x 6 rows of 8 experts, 1893 x 2808, 179 us; now 56.)
+// any address, while the slice before is multiplied, and written to LDS from there; a chunk in which a row ends is read from
+// as much earlier and moved down.  (271 x 6 rows of 8 experts, 1893 x 2808, forward / grad_input: two bytes at a time, and waited
+// for where they were asked for, 179 us; at once and ahead 56 / 139; ends without single elements 54 / 65.)
 #include "aa_experts.hpp"
 
 #include "aa_route.hpp"
@@ -103,7 +104,11 @@ struct Stage {
   int left[2];
   const int32_t *order;
   int top_k, next[TR && GATHER ? kSlots : 1];
+  // not ALIGNED: what waits for put(); elements by which a slot's chunk (even, odd) was read early, because the row ends
+  // inside it; whether a whole row is shorter than a chunk
   s16x8 held[ALIGNED ? 1 : kSlots];
+  int early[2];
+  bool narrow;
 
   static __device__ int k_row(int it, int t) { return it * kRowsASlot + t / kChunks; }
   static __device__ int chunk(int it, int t) {
@@ -188,9 +193,10 @@ struct Stage {
         load_lds16(src, lds + (it * NT + wave * kWave) * 16);
       } else {
         // elements of the chunk that exist
-        const int n = there ? (TR ? left[it & 1] : k_end - (k + chunk(0, t) * 8)) : 0;
-        held[it] = *there_or_zeros(src, n >= 8);
-        if (n > 0 && n < 8) {
+        const int n = TR ? left[it & 1] : k_end - (k + chunk(0, t) * 8);
+        early[it & 1] = n > 0 && n < 8 && !narrow ? 8 - n : 0;
+        held[it] = *there_or_zeros(src - early[it & 1], there && n > 0 && !narrow);
+        if (narrow && there && n > 0) {
           const short *p = reinterpret_cast<const short *>(src);
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -204,7 +210,17 @@ struct Stage {
 
   __device__ void put(char *lds) {
 #pragma unroll
-    for (int it = 0; it < kSlots; ++it) *reinterpret_cast<s16x8 *>(lds + (it * NT + (int)threadIdx.x) * 16) = held[it];
+    for (int it = 0; it < kSlots; ++it) {
+      s16x8 v = held[it];
+      const int n = early[it & 1];
+      if (n != 0) {  // what was read early leaves at the front, zeros follow
+        const s16x8 none = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (n & 4) v = __builtin_shufflevector(v, none, 4, 5, 6, 7, 8, 8, 8, 8);
+        if (n & 2) v = __builtin_shufflevector(v, none, 2, 3, 4, 5, 6, 7, 8, 8);
+        if (n & 1) v = __builtin_shufflevector(v, none, 1, 2, 3, 4, 5, 6, 7, 8);
+      }
+      *reinterpret_cast<s16x8 *>(lds + (it * NT + (int)threadIdx.x) * 16) = v;
+    }
   }
 };
 
@@ -499,6 +515,8 @@ __global__ __launch_bounds__(WI *WJ *kWave, 2) void k_product(const ProductArgs 
 
   Stage<T, BM, NT, TRP, false, ALIGNED> P;
   Stage<T, BN, NT, TRQ, GATHER && MODE == kGradWeight, ALIGNED> Q;
+  P.narrow = (MODE == kForward ? a.d_in : a.d_out) < 8;
+  Q.narrow = a.d_in < 8;
   constexpr int kReads = FI * (TRP ? 2 : 1) + FJ * (TRQ ? 2 : 1);
   constexpr int kLoads = decltype(P)::kSlots + decltype(Q)::kSlots;
   auto load = [&](char *to, int at, int k_end) __attribute__((always_inline)) {
@@ -948,7 +966,7 @@ hipError_t launch_product(const ProductArgs &a, hipStream_t st) {
       if (rows <= 32 && n128 <= 320)
         return rows <= 16 ? launch_few<T, ACT, 2, 1>(a, st) : launch_few<T, ACT, 2, 2>(a, st);
     }
-    // (what goes through registers: the one tile that has them.  271 x 6 rows, 8 experts of 1893 x 2808: 56 us)
+    // (what goes through registers: the one tile that has them)
     if (!a.aligned) return launch_tiles<T, MODE, ACT, 2, 2, 4, 4, 2, false>(a, st);
     if (t32 < t128 && t32 < t256) return launch_tiles<T, MODE, ACT, 2, 2, 1, 2, 6, true>(a, st);
     if (t128 < t256) return launch_tiles<T, MODE, ACT, 2, 2, 4, 4, 2, true>(a, st);

@@ -816,3 +816,29 @@ def test_boss_block_gradients_against_autograd():
                            ("gate_up", block.grads[1], W1.grad), ("down", block.grads[2], W2.grad)):
         w = ref.detach().numpy()
         assert np.abs(f64(got) - w).max() <= u * np.abs(w).max(), (name, np.abs(f64(got) - w).max(), np.abs(w).max())
+
+
+@pytest.mark.parametrize("dtype", HALVES)
+@pytest.mark.parametrize("offset", [0, 1, 3])
+def test_products_of_every_kind_of_edge(dtype, offset):
+    """Widths that end at every place of a chunk of eight, rows off 16-byte boundaries.  Values -1, 0, 1 and at most 129 of
+    them to add: sums are whole numbers below 256, which both types hold, so the results are exact."""
+    g = torch.Generator().manual_seed(3)
+    ones = lambda *s: torch.randint(-1, 2, s, generator=g).to(dtype)
+    n, E = 129, 2
+    offsets, ends = int_dev([0, 40, n]), [(0, 0, 40), (1, 40, n)]
+    ws = api.ExpertWorkspace(n, 1, E)
+    for d_in, d_out in ((1, 9), (7, 8), (8, 7), (9, 15), (10, 70), (11, 63), (12, 129), (13, 17), (14, 128), (63, 65), (65, 66), (127, 12),
+                        (129, 129), (128, 10)):
+        x, w, dout = ones(n, d_in), ones(E, d_out, d_in), ones(n, d_out)
+        xs, ds = strided(x, d_in + offset, offset), strided(dout, d_out + offset, offset)
+        out, dx = (torch.empty(n, d, dtype=dtype, device="cuda") for d in (d_out, d_in))
+        dw = torch.empty(E, d_out, d_in, dtype=dtype, device="cuda")
+        api.expert_forward(xs, None, 1, offsets, w.cuda(), "none", out)
+        api.expert_grad_input(ds, offsets, w.cuda(), "none", None, dx)
+        api.expert_grad_weight(ds, xs, None, 1, offsets, dw, False, ws)
+        for e, lo, hi in ends:
+            X, W, D = f64(x[lo:hi]), f64(w[e]), f64(dout[lo:hi])
+            assert np.array_equal(f64(out[lo:hi]), X @ W.T), (d_in, d_out, e)
+            assert np.array_equal(f64(dx[lo:hi]), D @ W), (d_in, d_out, e)
+            assert np.array_equal(f64(dw[e]), D.T @ X), (d_in, d_out, e)
