@@ -356,7 +356,11 @@ def _require(ok, what):
         raise AAError(what)
 
 
-def _matrix(t, name, dtype=None, width=None, rows=None):
+# A call of a few rows takes as long as the host needs for it (about 8 us), so the checks look at each property once and
+# put their messages together only where they fail.
+
+
+def _matrix(t, name, dtype=None, width=None, rows=0):
     """(pointer, row stride) of a 2-d CUDA tensor of the given type, width and number of rows (at least)."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 2):
         raise AAError(f"{name}: a 2-d CUDA tensor is needed")
@@ -365,15 +369,15 @@ def _matrix(t, name, dtype=None, width=None, rows=None):
         raise AAError(f"{name}: {t.dtype} where {dtype} is needed")
     if width is not None and d != width:
         raise AAError(f"{name}: {d} columns where {width} are needed")
-    if rows is not None and n < rows:
+    if n < rows:
         raise AAError(f"{name}: {n} rows where {rows} are needed")
     ld, step = t.stride()
-    if d > 1 and step != 1:
+    if step != 1 and d > 1:
         raise AAError(f"{name}: neighbouring columns must be neighbours in memory")
     return t.data_ptr(), ld if n > 1 else d   # (a tensor of one row may state any stride)
 
 
-def _array(t, name, dtype, shape=None, least=None):
+def _array(t, name, dtype, shape=None, least=0):
     """Pointer of a contiguous CUDA tensor; None stays None."""
     if t is None:
         return None
@@ -381,20 +385,31 @@ def _array(t, name, dtype, shape=None, least=None):
         raise AAError(f"{name}: a contiguous {dtype} CUDA tensor is needed")
     if shape is not None and t.shape != shape:
         raise AAError(f"{name}: shape {tuple(t.shape)}, not {tuple(shape)}")
-    if least is not None and t.numel() < least:
+    if least and t.numel() < least:
         raise AAError(f"{name}: {t.numel()} entries where {least} are needed")
     return t.data_ptr()
 
 
 def _type(t, name, products=False):
-    _require(isinstance(t, torch.Tensor) and t.dtype in DTYPES and not (products and t.dtype == torch.float32),
-             f"{name}: its type is not one this call takes")
-    return DTYPES[t.dtype]
+    """The type's code; products: of 16 bits."""
+    code = DTYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
+    if code is None or (products and code == 0):
+        raise AAError(f"{name}: its type is not one this call takes")
+    return code
 
 
 def _name_of(table, name, what):
-    _require(name in table, f"{what}: {name!r} is none of {sorted(table)}")
-    return table[name]
+    code = table.get(name)
+    if code is None:
+        raise AAError(f"{what}: {name!r} is none of {sorted(table)}")
+    return code
+
+
+def _all_weights(w, what):
+    """E, rows, columns of the experts' matrices."""
+    if not (isinstance(w, torch.Tensor) and w.dim() == 3):
+        raise AAError(what)
+    return w.shape
 
 
 class ExpertWorkspace:
@@ -454,47 +469,53 @@ def expert_plan(ids, count, n_experts, offsets, order, slot, ws):
 
 def _grouped_rows(x, order, top_k, rows, name):
     """Rows that a product over `rows` places may read must be there."""
+    n = x.shape[0]
     if order is None:
-        _require(x.shape[0] >= rows, f"{name}: {x.shape[0]} rows where {rows} are needed")
+        if n < rows:
+            raise AAError(f"{name}: {n} rows where {rows} are needed")
         return None
-    _require(top_k >= 1 and x.shape[0] * top_k >= rows, f"{name}: {x.shape[0]} rows for {rows} pairs")
-    return _array(order, "order", torch.int32, least=rows)
+    if top_k < 1 or n * top_k < rows:
+        raise AAError(f"{name}: {n} rows for {rows} pairs")
+    return _array(order, "order", torch.int32, None, rows)
 
 
 def expert_forward(x, order, top_k, offsets, w, act, out, pre=None):
     """Places 0 .. out.shape[0] - 1 at most; order None: place q reads row q of x (top_k is then not used)."""
-    dt, a = _type(x, "x", products=True), _name_of(ACTIVATIONS, act, "act")
-    _require(w.dim() == 3 and w.shape[1] % (2 if act == "gated" else 1) == 0, "w: [E, rows, d_in]")
-    E, d_in, d_out = w.shape[0], w.shape[2], w.shape[1] // (2 if act == "gated" else 1)
+    dt, a = _type(x, "x", True), _name_of(ACTIVATIONS, act, "act")
+    E, d_out, d_in = _all_weights(w, "w: [E, rows, d_in]")
+    if a == 2:
+        _require(d_out % 2 == 0, "w: [E, rows, d_in]")
+        d_out //= 2
+    dtype = x.dtype
+    xp, ldx = _matrix(x, "x", None, d_in)
+    op, ldo = _matrix(out, "out", dtype, d_out)
     rows = out.shape[0]
-    xp, ldx = _matrix(x, "x", width=d_in)
-    op, ldo = _matrix(out, "out", x.dtype, d_out)
-    pp, ldp = (None, 0) if pre is None else _matrix(pre, "pre", x.dtype, 2 * d_out, rows)
+    pp, ldp = (None, 0) if pre is None else _matrix(pre, "pre", dtype, 2 * d_out, rows)
     ordp = _grouped_rows(x, order, top_k, rows, "x")
     _check(lib().aa_expert_forward(xp, dt, ldx, ordp, top_k, _array(offsets, "offsets", torch.int32, (E + 1,)), rows, E,
-                                   d_in, d_out, _array(w, "w", x.dtype), a, op, ldo, pp, ldp, _stream()),
+                                   d_in, d_out, _array(w, "w", dtype), a, op, ldo, pp, ldp, _stream()),
            "aa_expert_forward")
 
 
 def expert_grad_input(dout, offsets, w, act, saved, dx):
-    dt, a = _type(dout, "dout", products=True), _name_of(ACTIVATIONS, act, "act")
-    _require(w.dim() == 3, "w: [E, d_out, d_in]")
-    E, d_out, d_in = w.shape
-    rows, wide = dx.shape[0], d_in * (2 if act == "gated" else 1)
-    gp, ldg = _matrix(dout, "dout", width=d_out, rows=rows)
-    xp, ldx = _matrix(dx, "dx", dout.dtype, wide)
-    sp, lds = (None, 0) if act == "none" else _matrix(saved, "saved", dout.dtype, wide, rows)
+    dt, a = _type(dout, "dout", True), _name_of(ACTIVATIONS, act, "act")
+    E, d_out, d_in = _all_weights(w, "w: [E, d_out, d_in]")
+    dtype, wide = dout.dtype, 2 * d_in if a == 2 else d_in
+    xp, ldx = _matrix(dx, "dx", dtype, wide)
+    rows = dx.shape[0]
+    gp, ldg = _matrix(dout, "dout", None, d_out, rows)
+    sp, lds = (None, 0) if a == 0 else _matrix(saved, "saved", dtype, wide, rows)
     _check(lib().aa_expert_grad_input(gp, dt, ldg, _array(offsets, "offsets", torch.int32, (E + 1,)), rows, E, d_in,
-                                      d_out, _array(w, "w", dout.dtype), a, sp, lds, xp, ldx, _stream()),
+                                      d_out, _array(w, "w", dtype), a, sp, lds, xp, ldx, _stream()),
            "aa_expert_grad_input")
 
 
 def expert_grad_weight(dout, x, order, top_k, offsets, dw, accumulate, ws):
-    dt = _type(dout, "dout", products=True)
-    _require(dw.dim() == 3 and dw.dtype in (dout.dtype, torch.float32), "dw: [E, d_out, d_in] of dout's type or float32")
-    E, d_out, d_in = dw.shape
+    dt = _type(dout, "dout", True)
+    E, d_out, d_in = _all_weights(dw, "dw: [E, d_out, d_in] of dout's type or float32")
+    _require(dw.dtype in (dout.dtype, torch.float32), "dw: [E, d_out, d_in] of dout's type or float32")
+    gp, ldg = _matrix(dout, "dout", None, d_out)
     rows = dout.shape[0]
-    gp, ldg = _matrix(dout, "dout", width=d_out)
     xp, ldx = _matrix(x, "x", dout.dtype, d_in)
     ordp = _grouped_rows(x, order, top_k, rows, "x")
     _check(lib().aa_expert_grad_weight(gp, dt, ldg, xp, ldx, ordp, top_k,
