@@ -14,7 +14,8 @@ class ExpertBlock:
     """out = x + dropout(sum_k weight_k expert_k(x)),  expert(x) = down silu(gate x) * (up x),  bf16 or f16.
 
     Weights: router [1, E, d], gate_up [E, 2 f, d], down [E, d, f]; gradients of the same shapes in fp32.
-    n_max rows at most a step.
+    Rows [0, min(max(count, 0), n_max)) take part in a step; x, out, dout and dx have n_max rows or more, of which those
+    at and beyond n_max are neither read nor written.
     """
 
     def __init__(self, n_max, d, f, n_experts, top_k, dtype=torch.bfloat16, p=0.0, score="softmax", seed=1905,
@@ -42,10 +43,11 @@ class ExpertBlock:
         return [self.router, self.gate_up, self.down]
 
     def forward(self, x, count, step, out, train=True):
-        """Rows [0, count) of x into out; train=False: no dropout, and nothing is kept for backward."""
+        """Rows in use of x into out; train=False: no dropout, and nothing is kept for backward."""
         offsets, order, slot = self.plan
         p = self.p if train else 0.0
-        self.one[1:].copy_(count.clamp(0, x.shape[0]))
+        # (the products go by the group's end alone: it must lie inside the block's own buffers)
+        self.one[1:].copy_(count.clamp(0, self.n_max))
         api.expert_forward(x, None, 1, self.one, self.router, "none", self.logits)
         api.route(self.logits, count, None, self.cfg, self.ids, self.route_weights, self.plan, self.ws)
         api.expert_forward(x, order, self.top_k, offsets, self.gate_up, "gated", self.h, self.pre if train else None)

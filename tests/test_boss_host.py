@@ -1,0 +1,38 @@
+"""ExpertBlock's order of calls and what it hands over, on the CPU: the library's calls are recorded, not made."""
+import pytest
+import torch
+
+from paper_1905_03381_amd import api
+from paper_1905_03381_amd.boss import ExpertBlock
+
+CALLS = ["expert_forward", "route", "expert_combine", "expert_combine_grad", "expert_grad_weight", "expert_grad_input",
+         "route_grad", "dropout"]
+
+
+@pytest.fixture
+def made(monkeypatch):
+    """Names and arguments of the calls made."""
+    calls = []
+    monkeypatch.setattr(api, "ExpertWorkspace", lambda *a, **k: None)
+    for name in CALLS:
+        monkeypatch.setattr(api, name, lambda *a, _name=name: calls.append((_name, a)))
+    return calls
+
+
+def block(n_max=8, **change):
+    return ExpertBlock(n_max, 16, 12, 4, 2, device="cpu", **change)
+
+
+def rows(n, d=16):
+    return torch.zeros(n, d, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("count,rows_of_x,end", [(5, 8, 5), (8, 8, 8), (11, 8, 8), (11, 20, 8), (1 << 30, 64, 8), (0, 8, 0),
+                                                 (-4, 20, 0)])
+def test_the_routers_group_ends_inside_the_buffers(made, count, rows_of_x, end):
+    """The router's product writes as many rows as its group has; its result has n_max."""
+    b, x = block(), rows(rows_of_x)
+    b.forward(x, torch.tensor([count], dtype=torch.int32), 0, torch.zeros_like(x))
+    assert b.one.tolist() == [0, end]
+    name, args = made[0]
+    assert name == "expert_forward" and args[3] is b.one and args[6] is b.logits and b.logits.shape[0] >= end
