@@ -156,6 +156,8 @@ __device__ __forceinline__ double exp_below(double v) {
   return ldexp(p, (int)n);
 }
 
+constexpr float kNoScore = -745.1332f;  // ln 2^-1075: from there down exp_below is 0
+
 // 1 / v for 1 <= v <= 2, by Newton's steps.
 __device__ __forceinline__ double reciprocal(double v) {
   double r = __builtin_amdgcn_rcp(v);
@@ -481,14 +483,19 @@ __global__ __launch_bounds__(256) void k_route_grad(const RouteGradArgs a) {
       const float wk = sum > 0.f ? ek / sum : 0.f;
       v = wk * (d - lanes_sum<LPR>(d * wk));
     } else {
-      const float sk = id < 0 ? 0.f : 1.f / (1.f + expf(-xk));
-      const float rest = id < 0 ? 0.f : 1.f / (1.f + expf(xk));  // 1 - sk, without the cancellation
+      // With t = e^-|x| the score is e^min(x, 0) / (1 + t) and 1 - score, without the cancellation, t / (1 + t) or 1 / (1 + t).
+      const float low = fminf(xk, 0.f), t = expf(-fabsf(xk)), r = 1.f / (1.f + t);
+      const float rest = xk > 0.f ? t * r : r;
       if (renorm) {
+        // Scores relative to the highest choice's e^min(x, 0): in 32 bits those of logits below -88 would all be 0.  (Where
+        // they are 0 in k_route's 64 bits, so are the weights.)
+        const float top = lanes_max<LPR>(low);
+        const float sk = id < 0 ? 0.f : expf(low - top) * r;
         const float sum = lanes_sum<LPR>(sk);
-        const float wk = sum > 0.f ? sk / sum : 0.f;
-        v = sum > 0.f ? wk * rest * (d - lanes_sum<LPR>(d * wk)) : 0.f;
+        const float wk = top > kNoScore ? sk / sum : 0.f;
+        v = wk * rest * (d - lanes_sum<LPR>(d * wk));
       } else {
-        v = d * sk * rest;
+        v = id < 0 ? 0.f : d * (xk > 0.f ? r : t * r) * rest;
       }
     }
     for (int k = 0; k < K; ++k) {
