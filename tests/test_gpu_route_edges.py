@@ -46,3 +46,16 @@ def test_renormalised_sigmoid_beyond_64_bits(dtype):
     api.route(x, None, None, c, ids, weights)
     api.route_grad(x, None, c, ids, normal((3, K), torch.float32, 1).cuda(), out)
     assert (ids.cpu() == torch.arange(K)).all() and (weights == 0).all() and (out == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("n,E", [(5, 2), (300, 37), (70, 200)])
+def test_one_renormalised_choice_has_no_gradient(n, E, kind, dtype):
+    """The weight of a single renormalised choice is the scale whatever the logits are: its gradient is 0, exactly."""
+    x = (normal((n, E), torch.float32, E) * 3).to(dtype).cuda()
+    ids, weights, out = torch.empty(n, 1, dtype=torch.int32, device="cuda"), torch.empty(n, 1, device="cuda"), torch.ones_like(x)
+    c = api.route_config(kind, 1, renormalise=True, scale=2.5)
+    api.route(x, None, None, c, ids, weights)
+    api.route_grad(x, None, c, ids, normal((n, 1), torch.float32, 3).cuda(), out)
+    assert (weights == 2.5).all() and (out == 0).all()
