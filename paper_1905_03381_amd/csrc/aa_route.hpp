@@ -39,7 +39,7 @@ struct PlanArgs {
   const int32_t *count;
   int32_t n_max, top_k, n_experts;
   int32_t *offsets, *order, *slot;
-  int32_t *table;  // [tiles][E] counts
+  int32_t *table;  // [tiles + 1][E]: counts of the tiles (scanned: of all before each, the last row the totals)
 };
 
 inline size_t plan_table_ints(int64_t n_max, int32_t top_k, int32_t n_experts) {
