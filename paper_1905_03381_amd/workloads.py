@@ -402,23 +402,24 @@ def experts(a, torch, api, synth):
     x, out, dout, dx = (z(P, d, t=torch.bfloat16) for _ in range(4))
     row, loss = torch.arange(P, device="cuda"), z(P)
 
-    def generate(t):
+    def generate(step):
+        t = step % steps
         idx = perm[t * P:(t + 1) * P]
-        api.score_shrink(F, idx, P, phi, b, 0.1, 42, t, None, prob, keep, pos, cnt, ws)
+        api.score_shrink(F, idx, P, phi, b, 0.1, 42, step, None, prob, keep, pos, cnt, ws)
         api.gather(Xb, 2 * d, idx, pos, cnt, P, x, ids)
 
-    def forward(t):
-        block.forward(x, cnt, t, out)
+    def forward(step):
+        block.forward(x, cnt, step, out)
         yk, live = yd[ids.long()], row < cnt
         margin = yk * (out.float() @ read)
         loss.copy_(torch.where(live, (1 - margin).clamp(min=0), 0.0))
         slope = torch.where(live & (margin < 1), -yk / cnt.clamp(min=1), 0.0)
         dout.copy_(slope[:, None] * read)
 
-    def backward(t):
-        block.backward(x, cnt, t, dout, dx)
+    def backward(step):
+        block.backward(x, cnt, step, dout, dx)
 
-    def update(t):
+    def update(step):
         for w, m, g in zip(block.weights(), masters, block.grads):
             m.add_(g, alpha=-16.0)
             w.copy_(m)
@@ -426,18 +427,17 @@ def experts(a, torch, api, synth):
         api.assistant_update(F, ids, cnt, P, loss, T, phi, b, 0.1, 0.0, ws)
 
     steps, kept, losses, times = max(1, n // P), [], [], {}
-    for epoch in range(3):
-        for t in range(steps):
-            marks = [torch.cuda.Event(enable_timing=True) for _ in range(5)]
-            marks[0].record()
-            for part, after in zip((generate, forward, backward, update), marks[1:]):
-                part(epoch * steps + t if part in (forward, backward) else t)
-                after.record()
-            if epoch or t:                          # the first step loads the kernels
-                for name, lo, hi in zip(("generate", "forward", "backward", "update"), marks, marks[1:]):
-                    times.setdefault(name, []).append((lo, hi))
-            kept.append(cnt.clone())
-            losses.append(loss.sum() / cnt.clamp(min=1))
+    for step in range(3 * steps):                   # three epochs; keep draws and masks go by the step
+        marks = [torch.cuda.Event(enable_timing=True) for _ in range(5)]
+        marks[0].record()
+        for part, after in zip((generate, forward, backward, update), marks[1:]):
+            part(step)
+            after.record()
+        if step:                                    # the first step loads the kernels
+            for name, lo, hi in zip(("generate", "forward", "backward", "update"), marks, marks[1:]):
+                times.setdefault(name, []).append((lo, hi))
+        kept.append(cnt.clone())
+        losses.append(loss.sum() / cnt.clamp(min=1))
     torch.cuda.synchronize()
     us = {k: float(np.median([lo.elapsed_time(hi) * 1e3 for lo, hi in v])) for k, v in times.items()}
     m = float(torch.stack(kept).float().mean())

@@ -35,3 +35,12 @@ def test_fewer_rows_than_the_block_are_refused():
     block, x = ExpertBlock(40, 64, 48, 8, 2), torch.zeros(39, 64, dtype=BF16, device="cuda")
     with pytest.raises(api.AAError):
         block.forward(x, counted(39), 0, torch.zeros_like(x))
+
+
+def test_every_epoch_of_the_experts_workload_draws_anew(capsys, monkeypatch):
+    """A row's keep draw comes from its position and the step: a step number that comes again would keep the same rows."""
+    from paper_1905_03381_amd import workloads
+    steps, call = [], api.score_shrink
+    monkeypatch.setattr(api, "score_shrink", lambda *a: (steps.append(a[6:8]), call(*a))[1])
+    workloads.main(["experts", "--n", "16384", "--threads", "4"])
+    assert len(steps) == 12 and len(set(steps)) == 12, steps
