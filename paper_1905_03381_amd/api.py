@@ -399,7 +399,7 @@ def _type(t, name, products=False):
 
 
 def _name_of(table, name, what):
-    code = table.get(name)
+    code = table.get(name) if isinstance(name, str) else None
     if code is None:
         raise AAError(f"{what}: {name!r} is none of {sorted(table)}")
     return code
@@ -420,6 +420,12 @@ class ExpertWorkspace:
         self.buf = torch.empty(self.bytes + 256, dtype=torch.uint8, device=device)
         self.ptr = self.buf.data_ptr() + (-self.buf.data_ptr()) % 256
         _check(lib().aa_workspace_init(self.ptr, self.bytes, _stream()), "aa_workspace_init")
+
+
+def _scratch(ws):
+    if ws is None:
+        raise AAError("ws: an ExpertWorkspace is needed")
+    return ws.ptr, ws.bytes
 
 
 def route_config(score, top_k, n_groups=1, top_groups=1, group_best=1, renormalise=False, scale=1.0):
@@ -464,7 +470,7 @@ def expert_plan(ids, count, n_experts, offsets, order, slot, ws):
     n, k = ids.shape
     p = _plan_pointers((offsets, order, slot), n, k, n_experts)
     _check(lib().aa_expert_plan(_array(ids, "ids", torch.int32), _array(count, "count", torch.int32, least=1), n, k,
-                                n_experts, *p, ws.ptr, ws.bytes, _stream()), "aa_expert_plan")
+                                n_experts, *p, *_scratch(ws), _stream()), "aa_expert_plan")
 
 
 def _grouped_rows(x, order, top_k, rows, name):
@@ -520,14 +526,14 @@ def expert_grad_weight(dout, x, order, top_k, offsets, dw, accumulate, ws):
     ordp = _grouped_rows(x, order, top_k, rows, "x")
     _check(lib().aa_expert_grad_weight(gp, dt, ldg, xp, ldx, ordp, top_k,
                                        _array(offsets, "offsets", torch.int32, (E + 1,)), rows, E, d_in, d_out,
-                                       _array(dw, "dw", dw.dtype), DTYPES[dw.dtype], int(bool(accumulate)), ws.ptr,
-                                       ws.bytes, _stream()), "aa_expert_grad_weight")
+                                       _array(dw, "dw", dw.dtype), DTYPES[dw.dtype], int(bool(accumulate)),
+                                       *_scratch(ws), _stream()), "aa_expert_grad_weight")
 
 
 def dropout(x, count, residual, p, seed, step, out):
     dt = _type(x, "x")
-    n, d = x.shape
     xp, ldx = _matrix(x, "x")
+    n, d = x.shape
     rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", x.dtype, d, n)
     op, ldo = _matrix(out, "out", x.dtype, d, n)
     _check(lib().aa_dropout(xp, dt, ldx, _array(count, "count", torch.int32, least=1), n, d, rp, ldr, p, seed, step,
@@ -538,8 +544,8 @@ def expert_combine(y, slot, weights, count, residual, p, seed, step, out):
     dt = _type(y, "y")
     _require(isinstance(slot, torch.Tensor) and slot.dim() == 2, "slot: a 2-d tensor")
     n, k = slot.shape
-    d = y.shape[1]
     yp, ldy = _matrix(y, "y")
+    d = y.shape[1]
     rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", y.dtype, d, n)
     op, ldo = _matrix(out, "out", y.dtype, d, n)
     _check(lib().aa_expert_combine(yp, dt, ldy, _array(slot, "slot", torch.int32),
@@ -553,8 +559,8 @@ def expert_combine_grad(dout, y, slot, weights, count, p, seed, step, dy, dweigh
     dt = _type(dout, "dout")
     _require(isinstance(slot, torch.Tensor) and slot.dim() == 2, "slot: a 2-d tensor")
     n, k = slot.shape
-    d = dout.shape[1]
     gp, ldg = _matrix(dout, "dout", rows=n)
+    d = dout.shape[1]
     _require(y is not None or dweights is None, "y: needed for dweights")
     yp, ldy = (None, d) if y is None else _matrix(y, "y", dout.dtype, d)
     dyp, lddy = _matrix(dy, "dy", dout.dtype, d)

@@ -1,4 +1,5 @@
-"""ExpertBlock's order of calls and what it hands over, on the CPU: the library's calls are recorded, not made."""
+"""ExpertBlock's order of calls and what it hands over, on the CPU, where the library's calls are recorded and not made; and
+wrong arguments of the Python calls, which are refused before anything is launched."""
 import pytest
 import torch
 
@@ -36,3 +37,24 @@ def test_the_routers_group_ends_inside_the_buffers(made, count, rows_of_x, end):
     assert b.one.tolist() == [0, end]
     name, args = made[0]
     assert name == "expert_forward" and args[3] is b.one and args[6] is b.logits and b.logits.shape[0] >= end
+
+
+def wrong(*shape, dtype="bfloat16"):
+    return torch.zeros(*shape, dtype=getattr(torch, dtype))
+
+
+@pytest.mark.parametrize("call", [
+    lambda: api.dropout(wrong(4), None, None, 0.1, 0, 0, wrong(4)),
+    lambda: api.dropout(wrong(2, 2, 2), None, None, 0.1, 0, 0, wrong(4)),
+    lambda: api.dropout(None, None, None, 0.1, 0, 0, wrong(4)),
+    lambda: api.expert_combine(wrong(4), wrong(2, 2, dtype="int32"), None, None, None, 0.0, 0, 0, wrong(4)),
+    lambda: api.expert_combine(wrong(4, 4), None, None, None, None, 0.0, 0, 0, wrong(4)),
+    lambda: api.expert_combine_grad(wrong(4), None, wrong(2, 2, dtype="int32"), None, None, 0.0, 0, 0, wrong(4), None),
+    lambda: api.expert_forward(wrong(2, 2), None, 1, None, wrong(1, 2, 2), ["relu"], wrong(2, 2)),
+    lambda: api.route(wrong(4), None, None, api.route_config("softmax", 1), None, None),
+    lambda: api.route_config(None, 1),
+])
+def test_wrong_arguments_are_this_librarys_error(call):
+    """Tensors of other dimensions, on the host, none at all: AAError, not what Python says about their shapes."""
+    with pytest.raises(api.AAError):
+        call()

@@ -44,3 +44,15 @@ def test_every_epoch_of_the_experts_workload_draws_anew(capsys, monkeypatch):
     monkeypatch.setattr(api, "score_shrink", lambda *a: (steps.append(a[6:8]), call(*a))[1])
     workloads.main(["experts", "--n", "16384", "--threads", "4"])
     assert len(steps) == 12 and len(set(steps)) == 12, steps
+
+
+def test_a_missing_workspace_is_refused():
+    i32 = dict(dtype=torch.int32, device="cuda")
+    ids, plan = torch.zeros(3, 2, **i32), [torch.zeros(5, **i32), torch.zeros(6, **i32), torch.zeros(3, 2, **i32)]
+    x, dw = torch.zeros(6, 8, dtype=BF16, device="cuda"), torch.zeros(4, 8, 8, dtype=BF16, device="cuda")
+    logits, weights = torch.zeros(3, 4, device="cuda"), torch.zeros(3, 2, device="cuda")
+    for call in (lambda: api.expert_plan(ids, None, 4, *plan, None),
+                 lambda: api.expert_grad_weight(x, x, None, 1, plan[0], dw, False, None),
+                 lambda: api.route(logits, None, None, api.route_config("softmax", 2), ids, weights, plan, None)):
+        with pytest.raises(api.AAError):
+            call()
