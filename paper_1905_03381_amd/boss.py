@@ -37,15 +37,20 @@ class ExpertBlock:
         self.dy, self.dpre, self.dx_pairs = z(R, d), z(R, 2 * f), z(R, d)
         self.dweights, self.dlogits = z(n_max, top_k, t=f32), z(n_max, E)
         self.dx_router = z(n_max, d)
+        # whether the buffers hold what backward needs (who replays a forward from a graph and calls backward outside it
+        # sets this)
+        self.kept = False
         self.ws = api.ExpertWorkspace(n_max, top_k, E, device=device)
 
     def weights(self):
         return [self.router, self.gate_up, self.down]
 
     def forward(self, x, count, step, out, train=True):
-        """Rows in use of x into out; train=False: no dropout, and nothing is kept for backward."""
+        """Rows in use of x into out; train=False: no dropout, and nothing is kept for backward (what an earlier
+        call kept is gone, too)."""
         offsets, order, slot = self.plan
         p = self.p if train else 0.0
+        self.kept = False
         # (the products go by the group's end alone: it must lie inside the block's own buffers)
         self.one[1:].copy_(count.clamp(0, self.n_max))
         api.expert_forward(x, None, 1, self.one, self.router, "none", self.logits)
@@ -53,9 +58,13 @@ class ExpertBlock:
         api.expert_forward(x, order, self.top_k, offsets, self.gate_up, "gated", self.h, self.pre if train else None)
         api.expert_forward(self.h, None, 1, offsets, self.down, "none", self.y)
         api.expert_combine(self.y, slot, self.route_weights, count, x, p, self.seed, step, out)
+        self.kept = train
 
     def backward(self, x, count, step, dout, dx):
-        """Gradients of the last forward(train=True) of the same x, count and step: self.grads, and of x into dx."""
+        """Gradients of the last forward of the same x, count and step, which was one with train=True: self.grads, and of x
+        into dx."""
+        if not self.kept:
+            raise api.AAError("backward: what the last forward kept is needed, and it ran without train=True or not at all")
         offsets, order, slot = self.plan
         d_router, d_gate_up, d_down = self.grads
         api.expert_combine_grad(dout, self.y, slot, self.route_weights, count, self.p, self.seed, step, self.dy,

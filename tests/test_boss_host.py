@@ -39,6 +39,23 @@ def test_the_routers_group_ends_inside_the_buffers(made, count, rows_of_x, end):
     assert name == "expert_forward" and args[3] is b.one and args[6] is b.logits and b.logits.shape[0] >= end
 
 
+def test_backward_needs_the_last_forward_to_have_trained(made):
+    """A forward without training takes the buffers: what an earlier one kept is no longer there, and gradients of it
+    would mix the two."""
+    b, x, count = block(p=0.1), rows(8), torch.tensor([8], dtype=torch.int32)
+    out, dx = torch.zeros_like(x), torch.zeros_like(x)
+    with pytest.raises(api.AAError):
+        b.backward(x, count, 0, x, dx)
+    b.forward(x, count, 0, out)
+    b.backward(x, count, 0, x, dx)
+    b.backward(x, count, 0, x, dx)
+    b.forward(x, count, 0, out, train=False)
+    made.clear()
+    with pytest.raises(api.AAError):
+        b.backward(x, count, 0, x, dx)
+    assert not made
+
+
 def wrong(*shape, dtype="bfloat16"):
     return torch.zeros(*shape, dtype=getattr(torch, dtype))
 
