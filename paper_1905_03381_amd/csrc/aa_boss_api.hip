@@ -46,7 +46,8 @@ int32_t check_words(const void *p, bool needed) {
 bool rows_on_16(const void *p, int64_t ld, int bytes) { return on(p, 16) && ld * bytes % 16 == 0; }
 
 // What the kernels that move 16 bytes at a time address with 32 bits a lane: rows by their place in units of 16
-// bytes; rows that run along the result by their place among 31.
+// bytes (gathered ones, of which there may be more than rows_max, by 64 bits); rows that run along the result by their place
+// among 31.
 bool in_reach(const void *p, int64_t rows, int64_t ld) {
   return rows_on_16(p, ld, 2) && (rows == 0 || ld / 8 < (1ll << 32) / rows);
 }
@@ -202,7 +203,8 @@ int32_t aa_expert_forward(const void *x, int32_t dtype, int64_t ldx, const int32
   a.pre = pre;
   a.ldpre = ldpre;
   a.act = act;
-  a.aligned = d_in % 8 == 0 && in_reach(x, rows_max, ldx) && in_reach(w, 2 * (int64_t)d_out, d_in);
+  a.aligned = d_in % 8 == 0 && (order ? rows_on_16(x, ldx, 2) : in_reach(x, rows_max, ldx)) &&
+              in_reach(w, 2 * (int64_t)d_out, d_in);
   return hip_status(launch_expert_forward(a, dtype == AA_F16, as_stream(stream)));
 }
 

@@ -68,11 +68,12 @@ __device__ __forceinline__ void load_lds16(const void *src, char *dst) {
 
 // A value the compiler shall not keep derived values of over the turns of a loop (it would run out of registers): for
 // all it knows this one changes with k.
-__device__ __forceinline__ uint32_t fresh(uint32_t v, int k) {
+template <typename V>
+__device__ __forceinline__ V fresh(V v, int k) {
   asm("" : "+v"(v) : "s"(k));
   return v;
 }
-__device__ __forceinline__ int fresh_thread(int k) { return (int)fresh(threadIdx.x, k); }
+__device__ __forceinline__ int fresh_thread(int k) { return (int)fresh((uint32_t)threadIdx.x, k); }
 
 // Permutation of the 32-byte units of a transposed operand's row r: the rows that one half of a wave
 // reads at once (r % 4 and r / 8 % 2 vary) fall into different banks.
@@ -96,8 +97,10 @@ struct Stage {
 
   const T *base;
   int64_t ld;
-  // not transposed: where each slot's row begins, in units of 16 bytes (not ALIGNED: the row's number)
-  uint32_t row_at[TR ? 1 : kSlots];
+  // not transposed: where each slot's row begins, in units of 16 bytes (not ALIGNED: the row's number).  Gathered rows may lie
+  // anywhere, also where there are few of them, and take 64 bits.
+  typedef typename std::conditional<GATHER && ALIGNED, uint64_t, uint32_t>::type Place;
+  Place row_at[TR ? 1 : kSlots];
   // transposed: a thread's place in a slot's rows, in bytes (slots of odd number may permute differently), and the
   // columns left from there on; the rows of the next slice when they are gathered
   uint32_t at[2];
@@ -127,7 +130,7 @@ struct Stage {
 #pragma unroll
     for (int it = 0; it < kSlots; ++it) {
       const uint32_t row = row_of((it * NT + t) / kChunks);
-      row_at[it] = ALIGNED ? (uint32_t)((uint64_t)row * (uint64_t)(ld / 8)) + (uint32_t)chunk(0, t) : row;
+      row_at[it] = ALIGNED ? (Place)((uint64_t)row * (uint64_t)(ld / 8)) + (uint32_t)chunk(0, t) : row;
     }
   }
 
@@ -513,7 +516,7 @@ __global__ __launch_bounds__(WI *WJ *kWave, 2) void k_product(const ProductArgs 
     return turn * blocks + (turn & 1 ? blocks - 1 - place : place);
   };
 
-  Stage<T, BM, NT, TRP, false, ALIGNED> P;
+  Stage<T, BM, NT, TRP, GATHER && MODE == kForward, ALIGNED> P;
   Stage<T, BN, NT, TRQ, GATHER && MODE == kGradWeight, ALIGNED> Q;
   P.narrow = (MODE == kForward ? a.d_in : a.d_out) < 8;
   Q.narrow = a.d_in < 8;
