@@ -13,7 +13,9 @@ from . import api
 class ExpertBlock:
     """out = x + dropout(sum_k weight_k expert_k(x)),  expert(x) = down silu(gate x) * (up x),  bf16 or f16.
 
-    Weights: router [1, E, d], gate_up [E, 2 f, d], down [E, d, f]; gradients of the same shapes in fp32.
+    Weights: router [1, E, d], gate_up [E, 2 f, d], down [E, d, f]; gradients of the same shapes in fp32.  seed makes the first
+    weights and, with the step, the masks: blocks of one model take seeds of their own.  Logits are rounded to dtype before
+    they are routed: those that tie in it go to the lowest index.
     Rows [0, min(max(count, 0), n_max)) take part in a step; x, out, dout and dx have n_max rows or more, of which those
     at and beyond n_max are neither read nor written.
     """
