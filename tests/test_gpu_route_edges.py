@@ -59,3 +59,35 @@ def test_one_renormalised_choice_has_no_gradient(n, E, kind, dtype):
     api.route(x, None, None, c, ids, weights)
     api.route_grad(x, None, c, ids, normal((n, 1), torch.float32, 3).cuda(), out)
     assert (weights == 2.5).all() and (out == 0).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("high,low", [(0.5, None), (0.5, -10_000.0), (float("inf"), 0.25), (300.0, -500.0)])
+@pytest.mark.parametrize("E,K", [(6, 2), (40, 5), (200, 9), (300, 20)])
+def test_renormalised_softmax_of_choices_without_a_score(E, K, high, low, dtype):
+    """A bias may choose masked experts alone: their scores are 0 beside the row's others, in 64 bits, so are their weights
+    (there is nothing to divide by), and the gradient of those is 0.  low None: the type's lowest value."""
+    if low is None:
+        low = torch.finfo(dtype).min
+    x = torch.full((4, E), low, dtype=dtype)
+    x[:, ::3] = high
+    x[0] = low                               # all alike: K equal weights, whose gradients are not 0
+    x[2, 1] = high                           # one of the choices has a score
+    bias = torch.zeros(E)
+    bias[[e for e in range(E) if e % 3][:K]] = 3.0
+    ids = torch.empty(4, K, dtype=torch.int32, device="cuda")
+    weights, out = torch.empty(4, K, device="cuda"), torch.full((4, E), 7.0, dtype=dtype, device="cuda")
+    c, dw = api.route_config("softmax", K, renormalise=True), normal((4, K), torch.float32, 5)
+    api.route(x.cuda(), None, bias.cuda(), c, ids, weights)
+    api.route_grad(x.cuda(), None, c, ids, dw.cuda(), out)
+    ids, weights, got = ids.cpu().numpy(), f64(weights), f64(out)
+    for t in range(4):
+        want_ids, want_weights = R.choose(f64(x)[t], "softmax", K, bias.numpy(), renorm=True)
+        assert ids[t].tolist() == want_ids
+        check(weights[t], np.array(want_weights), 4 * U32, f"weights of row {t}")
+    assert (weights[[1, 3]] == 0).all() and (got[[1, 3]] == 0).all()
+    want = np.zeros(E)
+    want[ids[0]] = (dw[0].double().numpy() - dw[0].double().mean().item()) / K
+    mag = np.abs(dw[0].double().numpy()).sum()
+    check(got[0], want, half_step(dtype) * np.abs(want) + 64 * U32 * mag + tiny(dtype), "row 0")
+    assert (weights[2] > 0).sum() == 1 and (np.abs(got[2]) <= 64 * U32 * np.abs(dw[2].numpy()).sum()).all()
