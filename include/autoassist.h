@@ -502,6 +502,33 @@ int32_t aa_expert_combine_grad(const void *dout, int32_t dtype, int64_t lddo, co
                                int32_t n_max, int32_t top_k, int32_t d, float p, uint64_t seed,
                                uint64_t step, void *dy, int64_t lddy, float *dweights, void *stream);
 
+/* ---- Around a Boss block of experts -----------------------------------------
+ * What a deep Boss needs beside its experts when it is trained: layer norm, the dense
+ * product with its epilogue, the router's balance loss, and the optimizer.  Conventions as for the block of
+ * experts (count, dtype, strides, rounding, reproducibility); vectors of one row (gamma, beta, bias) and
+ * all sums over rows are fp32.  This library's definitions: the paper leaves the Boss to its framework. */
+
+/* Scratch of the calls below that take ws, for rows of up to d_max columns (aa_linear_grad with AA_ACT_GATED: 2 d_out;
+ * aa_balance: n_experts); 256-byte aligned, prepared once with aa_workspace_init(). */
+size_t aa_layer_workspace_bytes(int32_t d_max);
+
+/* Layer norm: out[t] = (x[t] - mean_t) rstd_t gamma + beta over the d columns of a row, mean_t = sum x / d,
+ * rstd_t = 1 / sqrt(sum (x - mean_t)^2 / d + eps).  gamma, beta: [d] (NULL: 1 and 0).  mean, rstd: [n_max], what
+ * the backward pass needs (NULL: not written).  eps >= 0, finite.  out may be x. */
+int32_t aa_layer_norm(const void *x, int32_t dtype, int64_t ldx, const int32_t *count, int32_t n_max, int32_t d,
+                      const float *gamma, const float *beta, float eps, void *out, int64_t ldo, float *mean,
+                      float *rstd, void *stream);
+
+/* Its gradient: with xh = (x - mean) rstd and g = dout gamma
+ *   dx[t] = residual[t] + rstd (g - sum g / d - xh sum (g xh) / d)   (residual == NULL: without)
+ *   dgamma = sum over the rows in use of dout xh,  dbeta = of dout   (either may be NULL; accumulate != 0 adds
+ * to what they hold; no rows: zeros, or nothing).  mean, rstd as aa_layer_norm wrote them.  dx may be dout, x
+ * or residual.  ws is needed where dgamma or dbeta is. */
+int32_t aa_layer_norm_grad(const void *dout, int32_t dtype, int64_t lddo, const void *x, int64_t ldx,
+                           const int32_t *count, int32_t n_max, int32_t d, const float *gamma, const float *mean,
+                           const float *rstd, const void *residual, int64_t ldr, void *dx, int64_t lddx,
+                           float *dgamma, float *dbeta, int32_t accumulate, void *ws, size_t ws_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

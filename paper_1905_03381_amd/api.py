@@ -32,6 +32,7 @@ SYMBOLS = [
     "aa_expert_workspace_bytes", "aa_route", "aa_route_grad", "aa_expert_plan", "aa_expert_forward",
     "aa_expert_grad_input", "aa_expert_grad_weight", "aa_expert_combine", "aa_expert_combine_grad",
     "aa_dropout",
+    "aa_layer_workspace_bytes", "aa_layer_norm", "aa_layer_norm_grad",
 ]
 
 
@@ -110,6 +111,10 @@ def lib():
         "aa_expert_combine_grad": (i32, [vp, i32, i64, vp, i64, vp, vp, vp, i32, i32, i32, f32, u64, u64, vp, i64,
                                          vp, vp]),
         "aa_dropout": (i32, [vp, i32, i64, vp, i32, i32, vp, i64, f32, u64, u64, vp, i64, vp]),
+        "aa_layer_workspace_bytes": (sz, [i32]),
+        "aa_layer_norm": (i32, [vp, i32, i64, vp, i32, i32, vp, vp, f32, vp, i64, vp, vp, vp]),
+        "aa_layer_norm_grad": (i32, [vp, i32, i64, vp, i64, vp, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, i32,
+                                     vp, sz, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -416,15 +421,20 @@ class ExpertWorkspace:
     """Device scratch of route / expert_plan (with a plan) and expert_grad_weight."""
 
     def __init__(self, n_max, top_k, n_experts, device="cuda"):
-        self.bytes = int(lib().aa_expert_workspace_bytes(n_max, top_k, n_experts))
-        self.buf = torch.empty(self.bytes + 256, dtype=torch.uint8, device=device)
-        self.ptr = self.buf.data_ptr() + (-self.buf.data_ptr()) % 256
-        _check(lib().aa_workspace_init(self.ptr, self.bytes, _stream()), "aa_workspace_init")
+        _take(self, int(lib().aa_expert_workspace_bytes(n_max, top_k, n_experts)), device)
 
 
-def _scratch(ws):
+def _take(ws, size, device):
+    """Prepared scratch of `size` bytes for the workspace object ws."""
+    ws.bytes = size
+    ws.buf = torch.empty(size + 256, dtype=torch.uint8, device=device)
+    ws.ptr = ws.buf.data_ptr() + (-ws.buf.data_ptr()) % 256
+    _check(lib().aa_workspace_init(ws.ptr, ws.bytes, _stream()), "aa_workspace_init")
+
+
+def _scratch(ws, kind="an ExpertWorkspace"):
     if ws is None:
-        raise AAError("ws: an ExpertWorkspace is needed")
+        raise AAError(f"ws: {kind} is needed")
     return ws.ptr, ws.bytes
 
 
@@ -569,3 +579,47 @@ def expert_combine_grad(dout, y, slot, weights, count, p, seed, step, dy, dweigh
                                         _array(count, "count", torch.int32, least=1), n, k, d, p, seed, step, dyp, lddy,
                                         _array(dweights, "dweights", torch.float32, (n, k)), _stream()),
            "aa_expert_combine_grad")
+
+
+# ---- around a Boss block of experts: layer norm, dense product, balance loss, optimizer ----
+
+
+class LayerWorkspace:
+    """Device scratch of layer_norm_grad, linear_grad and balance for rows of up to d_max columns (gated layers: twice d_out;
+    balance: the experts)."""
+
+    def __init__(self, d_max, device="cuda"):
+        _take(self, int(lib().aa_layer_workspace_bytes(d_max)), device)
+
+
+def _count(count):
+    return _array(count, "count", torch.int32, least=1)
+
+
+def layer_norm(x, gamma, beta, eps, count, out, mean=None, rstd=None):
+    """gamma, beta: float32 [d] or None (1 and 0); mean, rstd: float32 [n], for the backward pass."""
+    dt = _type(x, "x")
+    xp, ldx = _matrix(x, "x")
+    n, d = x.shape
+    op, ldo = _matrix(out, "out", x.dtype, d, n)
+    _check(lib().aa_layer_norm(xp, dt, ldx, _count(count), n, d, _array(gamma, "gamma", torch.float32, (d,)),
+                               _array(beta, "beta", torch.float32, (d,)), eps, op, ldo,
+                               _array(mean, "mean", torch.float32, (n,)), _array(rstd, "rstd", torch.float32, (n,)),
+                               _stream()), "aa_layer_norm")
+
+
+def layer_norm_grad(dout, x, gamma, mean, rstd, residual, count, dx, dgamma, dbeta, accumulate, ws):
+    """residual: what is added to dx, or None; dgamma, dbeta: either may be None, and ws where both are."""
+    dt = _type(dout, "dout")
+    gp, ldg = _matrix(dout, "dout")
+    n, d = dout.shape
+    xp, ldx = _matrix(x, "x", dout.dtype, d, n)
+    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", dout.dtype, d, n)
+    op, ldo = _matrix(dx, "dx", dout.dtype, d, n)
+    scratch = (None, 0) if dgamma is None and dbeta is None else _scratch(ws, "a LayerWorkspace")
+    _check(lib().aa_layer_norm_grad(gp, dt, ldg, xp, ldx, _count(count), n, d,
+                                    _array(gamma, "gamma", torch.float32, (d,)), _array(mean, "mean", torch.float32, (n,)),
+                                    _array(rstd, "rstd", torch.float32, (n,)), rp, ldr, op, ldo,
+                                    _array(dgamma, "dgamma", torch.float32, (d,)),
+                                    _array(dbeta, "dbeta", torch.float32, (d,)), int(bool(accumulate)), *scratch,
+                                    _stream()), "aa_layer_norm_grad")

@@ -84,6 +84,11 @@ __device__ __forceinline__ bool keep_decision(float u, float g, float gamma, flo
 
 __device__ __forceinline__ float sigmoidf_(float s) { return 1.0f / (1.0f + expf(-s)); }
 
+// Rows of an operator that take part: *count of n_max (count == NULL: all).
+__device__ __forceinline__ int rows_in_use(const int32_t *count, int n_max) {
+  return count ? min(max(*count, 0), n_max) : n_max;
+}
+
 // ---- wave64 primitives -----------------------------------------------------
 // Butterfly sum over aligned groups of WIDTH lanes; every lane gets the total.
 template <int WIDTH>

@@ -21,10 +21,6 @@ __device__ __forceinline__ void wave_sync() {
   __builtin_amdgcn_wave_barrier();
 }
 
-__device__ __forceinline__ int rows_in_use(const int32_t *count, int n_max) {
-  return count ? min(max(*count, 0), n_max) : n_max;
-}
-
 // Largest value and sum over aligned groups of LPR (16 or 64) lanes, every lane gets it: inside a row of 16 lanes
 // quad swaps, half mirror, mirror; across rows exchanges with the lanes 16 and 32 away.  No LDS.
 template <int CTRL>

@@ -6,78 +6,13 @@
 // gradient 117 us, 4.9 TB/s.
 #include "aa_rows.hpp"
 
+#include "aa_lines.hpp"
+
 #include <type_traits>
 
 namespace aa {
 
 namespace {
-
-__device__ __forceinline__ int rows_in_use(const int32_t *count, int n_max) {
-  return count ? min(max(*count, 0), n_max) : n_max;
-}
-
-// All four words of Philox4x32-10 (Salmon et al., SC'11).
-__device__ __forceinline__ uint4 philox_words(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3, uint32_t k0,
-                                              uint32_t k1) {
-#pragma unroll
-  for (int r = 0; r < 10; ++r) {
-    const uint64_t p0 = (uint64_t)0xD2511F53u * c0, p1 = (uint64_t)0xCD9E8D57u * c2;
-    const uint32_t n0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0, n2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
-    c0 = n0;
-    c1 = (uint32_t)p1;
-    c2 = n2;
-    c3 = (uint32_t)p0;
-    k0 += 0x9E3779B9u;
-    k1 += 0xBB67AE85u;
-  }
-  return make_uint4(c0, c1, c2, c3);
-}
-
-struct Eight {
-  float v[8];
-};
-
-template <typename T>
-using Line = T __attribute__((ext_vector_type(8), aligned(sizeof(T))));  // (memory is read and written at any address)
-
-// Columns of which n exist, the others 0.
-template <typename T>
-__device__ __forceinline__ Line<T> load_line(const T *p, int n) {
-  Line<T> o;
-  if (n >= 8) {
-    o = *reinterpret_cast<const Line<T> *>(p);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const T v = p[i < n ? i : 0];  // (no branch: all are asked for at once)
-      o[i] = i < n ? v : (T)0.f;
-    }
-  }
-  return o;
-}
-
-template <typename T>
-__device__ __forceinline__ Eight load8(const T *p, int n) {
-  const Line<T> t = load_line(p, n);
-  Eight o;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) o.v[i] = (float)t[i];
-  return o;
-}
-
-template <typename T>
-__device__ __forceinline__ void store8(T *p, const Eight &o, int n) {
-  if (n >= 8) {
-    Line<T> t;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = (T)o.v[i];
-    *reinterpret_cast<Line<T> *>(p) = t;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < n) p[i] = (T)o.v[i];
-  }
-}
 
 // Columns c .. c + 7 (c a multiple of 8) of a row; what is dropped is 0 whatever it was.
 __device__ __forceinline__ void drop8(const DropKey &k, int row, int c, Eight &x) {
@@ -92,18 +27,6 @@ __device__ __forceinline__ void drop8(const DropKey &k, int row, int c, Eight &x
 }
 
 constexpr int kBatch = 8;  // choices of a row whose lines are asked for together
-
-// Sum over aligned groups of W (8 to 64) lanes; every lane gets it.
-template <int W>
-__device__ __forceinline__ float lanes_sum(float v, int lane) {
-  if constexpr (W >= 16) {
-    return row_group_sum<W>(v, lane);
-  } else {
-    v = dpp_add<0xB1>(v);     // quad_perm [1,0,3,2]
-    v = dpp_add<0x4E>(v);     // quad_perm [2,3,0,1]
-    return dpp_add<0x141>(v);  // row_half_mirror
-  }
-}
 
 // TPR threads a row, 256 / TPR rows a turn of the block.  A wave that has one row knows it for all its lanes.
 template <int TPR>

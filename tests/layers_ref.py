@@ -1,0 +1,102 @@
+"""References in 64 bits of the operators around a Boss block of experts, and helpers their tests share.  Nothing here
+calls the package."""
+import numpy as np
+import torch
+
+U32 = 2.0 ** -23  # (2^-23 rather than 2^-24 for adders that cut instead of rounding)
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+TYPES = [F32, BF16, F16]
+HALVES = [BF16, F16]
+
+
+def half_step(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def tiny(dtype):
+    """Half a step below the smallest normal number."""
+    return torch.finfo(dtype).smallest_normal * torch.finfo(dtype).eps / 2
+
+
+def normal(shape, dtype, seed, scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g, dtype=torch.float64) * scale).to(dtype)
+
+
+def strided(t, ld, offset=0):
+    """t's values on the GPU as rows `ld` elements apart, the first `offset` elements into its storage; NaN between."""
+    n, d = t.shape
+    store = torch.full((offset + max(n, 1) * ld + 8,), float("nan"), dtype=t.dtype, device="cuda")
+    v = store[offset:offset + n * ld].view(n, ld)[:, :d] if n else store[:0].view(0, ld)[:, :d]
+    v.copy_(t)
+    return v
+
+
+def f64(t):
+    return t.detach().cpu().to(torch.float64).numpy()
+
+
+def device_count(count):
+    return None if count is None else torch.tensor([count], dtype=torch.int32, device="cuda")
+
+
+def in_use(count, n):
+    return n if count is None else min(max(count, 0), n)
+
+
+def check(got, want, bound, what):
+    got, want = f64(got) if isinstance(got, torch.Tensor) else got, np.asarray(want)
+    with np.errstate(invalid="ignore"):
+        err = np.abs(got - want)
+    same = (got == want) | (np.isnan(got) & np.isnan(want))
+    bad = ~same & ~(err <= bound)
+    assert not bad.any(), (what, int(bad.sum()), got[bad][:3], want[bad][:3], np.broadcast_to(bound, got.shape)[bad][:3])
+
+
+# ---------------------------------------------------------------------------
+# layer norm
+
+# Additions that a term of a row's sum passes through: 16 of its thread, 6 between the lanes, 16 between the waves, and the
+# division.
+ROW_DEPTH = 40
+
+
+def norm(x, gamma, beta, eps):
+    """out, mean, rstd"""
+    mean = x.mean(1, keepdims=True)
+    rstd = 1 / np.sqrt(((x - mean) ** 2).mean(1, keepdims=True) + eps)
+    return (x - mean) * rstd * gamma + beta, mean[:, 0], rstd[:, 0]
+
+
+def norm_bounds(x, gamma, beta, eps, dtype):
+    """How far out, mean and rstd may be off.  The mean is off by at most e = ROW_DEPTH U mean|x|; the squares around it sum
+    to d (var + e^2) at most, with ROW_DEPTH + 4 roundings; the root halves what is relative, and adds a few."""
+    out, mean, rstd = norm(x, gamma, beta, eps)
+    xh = (x - mean[:, None]) * rstd[:, None]
+    e = ROW_DEPTH * U32 * np.abs(x).mean(1)
+    of_rstd = (ROW_DEPTH + 4) / 2 * U32 + 4 * U32 + (e * rstd) ** 2
+    of_out = np.abs(gamma) * ((rstd * e)[:, None] + np.abs(xh) * (of_rstd + 4 * U32)[:, None])
+    of_out = of_out + 2 * U32 * (np.abs(xh * gamma) + np.abs(beta))
+    of_out += half_step(dtype) * (np.abs(out) + of_out) + tiny(dtype)
+    return of_out, e, rstd * of_rstd
+
+
+def norm_grad(dout, x, gamma, mean, rstd, residual):
+    """dx, dgamma, dbeta"""
+    xh = (x - mean[:, None]) * rstd[:, None]
+    g = dout * gamma
+    dx = rstd[:, None] * (g - g.mean(1, keepdims=True) - xh * (g * xh).mean(1, keepdims=True)) + residual
+    return dx, (dout * xh).sum(0), dout.sum(0)
+
+
+def norm_grad_bounds(dout, x, gamma, mean, rstd, residual, dtype):
+    """xh is off by 2 roundings, g by one, their sums by ROW_DEPTH more; the sums over n rows by n (blocks, parts and their
+    joining: at most 64 more) of their terms' magnitudes."""
+    dx = norm_grad(dout, x, gamma, mean, rstd, residual)[0]
+    xh = np.abs(x - mean[:, None]) * rstd[:, None]
+    g = np.abs(dout * gamma)
+    s1, s2 = g.mean(1, keepdims=True), (g * xh).mean(1, keepdims=True)
+    of_dx = rstd[:, None] * U32 * (5 * g + (ROW_DEPTH + 6) * s1 + (ROW_DEPTH + 10) * xh * s2) + 2 * U32 * np.abs(residual)
+    of_dx += half_step(dtype) * (np.abs(dx) + of_dx) + tiny(dtype)
+    rows = len(x) + 64
+    return of_dx, (rows + 3) * U32 * (np.abs(dout) * xh).sum(0), rows * U32 * np.abs(dout).sum(0)

@@ -1,0 +1,68 @@
+"""Refusals of the operators around a Boss block of experts: every one is decided on the host before anything is
+launched, so these run without a GPU.  The pointers handed over are never read."""
+import pytest
+
+from paper_1905_03381_amd import api
+
+OK, NULL, SHAPE, ALIGN, WORKSPACE = 0, -1, -2, -3, -4
+P = 0x10000  # stands for a device pointer, aligned to everything
+F32, BF16, F16 = 0, 1, 2
+BIG = 1 << 40
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def L():
+    import os
+    if not os.path.exists(api.LIB_PATH):
+        from paper_1905_03381_amd import build
+        build.build(force=False)
+    return api.lib()
+
+
+NORM = dict(x=P, dtype=BF16, ldx=32, count=None, n_max=8, d=32, gamma=P, beta=P, eps=1e-5, out=P, ldo=32, mean=P, rstd=P,
+            stream=None)
+NORM_GRAD = dict(dout=P, dtype=BF16, lddo=32, x=P, ldx=32, count=None, n_max=8, d=32, gamma=P, mean=P, rstd=P,
+                 residual=None, ldr=0, dx=P, lddx=32, dgamma=P, dbeta=P, accumulate=0, ws=P, ws_bytes=BIG, stream=None)
+
+REFUSED = [
+    ("aa_layer_norm", NORM, [
+        (dict(x=None), NULL), (dict(out=None), NULL), (dict(dtype=3), SHAPE), (dict(dtype=-1), SHAPE),
+        (dict(n_max=-1), SHAPE), (dict(d=0), SHAPE), (dict(d=(1 << 24) + 1, ldx=BIG, ldo=BIG), SHAPE),
+        (dict(ldx=31), SHAPE), (dict(ldo=31), SHAPE), (dict(ldx=BIG + 1), SHAPE), (dict(eps=-1e-9), SHAPE),
+        (dict(eps=NAN), SHAPE), (dict(eps=INF), SHAPE), (dict(x=P + 1), ALIGN), (dict(out=P + 1), ALIGN),
+        (dict(dtype=F32, x=P + 2), ALIGN), (dict(gamma=P + 2), ALIGN), (dict(beta=P + 2), ALIGN),
+        (dict(mean=P + 2), ALIGN), (dict(rstd=P + 2), ALIGN), (dict(count=P + 2), ALIGN)]),
+    ("aa_layer_norm_grad", NORM_GRAD, [
+        (dict(dout=None), NULL), (dict(x=None), NULL), (dict(dx=None), NULL), (dict(mean=None), NULL),
+        (dict(rstd=None), NULL), (dict(dtype=7), SHAPE), (dict(n_max=-1), SHAPE), (dict(d=0), SHAPE),
+        (dict(lddo=31), SHAPE), (dict(ldx=31), SHAPE), (dict(lddx=31), SHAPE), (dict(residual=P, ldr=31), SHAPE),
+        (dict(dout=P + 1), ALIGN), (dict(residual=P + 1, ldr=32), ALIGN), (dict(gamma=P + 1), ALIGN),
+        (dict(dgamma=P + 2), ALIGN), (dict(dbeta=P + 2), ALIGN), (dict(ws=None), WORKSPACE),
+        (dict(ws=P + 128), WORKSPACE), (dict(ws_bytes=256), WORKSPACE), (dict(ws=None, dgamma=None), WORKSPACE)]),
+]
+
+
+@pytest.mark.parametrize("name,args,change,want",
+                         [(n, a, c, w) for n, a, cases in REFUSED for c, w in cases],
+                         ids=lambda v: v if isinstance(v, str) else ",".join(v) if isinstance(v, dict) and len(v) < 4 else None)
+def test_refused(L, name, args, change, want):
+    call = dict(args)
+    assert set(change) <= set(call), change
+    call.update(change)
+    assert getattr(L, name)(*call.values()) == want
+
+
+def test_workspace_grows_with_the_columns(L):
+    sizes = [L.aa_layer_workspace_bytes(d) for d in (0, 1, 64, 8192, 1 << 16, 1 << 24)]
+    assert sizes[0] == sizes[1] and all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[-1] < 1 << 28
+    assert all(s % 256 == 0 for s in sizes)
+
+
+def test_python_refusals():
+    import torch
+    t = torch.zeros(4, 8)  # (not a CUDA tensor)
+    with pytest.raises(api.AAError):
+        api.layer_norm(t, None, None, 1e-5, None, t)
+    with pytest.raises(api.AAError):
+        api.layer_norm_grad(t, t, None, None, None, None, None, t, None, None, False, None)
