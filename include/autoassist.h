@@ -529,6 +529,26 @@ int32_t aa_layer_norm_grad(const void *dout, int32_t dtype, int64_t lddo, const 
                            const float *rstd, const void *residual, int64_t ldr, void *dx, int64_t lddx,
                            float *dgamma, float *dbeta, int32_t accumulate, void *ws, size_t ws_bytes, void *stream);
 
+/* Balance of a router: with the ids that aa_route wrote, c_e the choices of expert e among the m top_k of the rows
+ * in use, and p_te = s_te / sum_e s_te the share that expert e has of row t's scores (cfg->score as in aa_route; 0 for
+ * experts that are not free; worked out relative to the row's highest, so that low logits have shares too):
+ *   counts[E]  c_e (ids outside [0, E) are no choices),   share[E]  P_e = sum_t p_te / m (NULL: not written)
+ *   loss[2]    coef E / (m top_k) sum_e c_e P_e  and  z_coef / m sum_t lse_t^2   (NULL: not written)
+ * lse_t = log sum exp of the row's free logits, whatever the score; a row whose lse is not finite adds nothing.  No
+ * rows: zeros.  Of cfg, score and top_k are used; all of it is checked.  coef and z_coef are finite. */
+int32_t aa_balance(const void *logits, int32_t dtype, int64_t ld, const int32_t *count, int32_t n_max,
+                   int32_t n_experts, const aa_route_config *cfg, const int32_t *ids, float coef, float z_coef,
+                   int32_t *counts, float *share, float *loss, void *ws, size_t ws_bytes, void *stream);
+
+/* Its gradient, the counts held fixed, times *dloss (device scalar; NULL: 1), and with dweights != NULL the
+ * gradient of aa_route_grad added to it (ids and dweights as there), in one pass with one rounding:
+ *   dlogits[t][e] = *dloss (coef E / (m^2 top_k) p_te w_te (c_e - sum_e p_te c_e) + 2 z_coef / m lse_t softmax_te)
+ * with w = 1 (softmax) or 1 - s_te (sigmoid).  ids is not read where dweights is NULL. */
+int32_t aa_balance_grad(const void *logits, int32_t dtype, int64_t ld, const int32_t *count, int32_t n_max,
+                        int32_t n_experts, const aa_route_config *cfg, const int32_t *ids, const float *dweights,
+                        const int32_t *counts, float coef, float z_coef, const float *dloss, void *dlogits,
+                        int64_t ld_out, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

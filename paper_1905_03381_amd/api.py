@@ -32,7 +32,7 @@ SYMBOLS = [
     "aa_expert_workspace_bytes", "aa_route", "aa_route_grad", "aa_expert_plan", "aa_expert_forward",
     "aa_expert_grad_input", "aa_expert_grad_weight", "aa_expert_combine", "aa_expert_combine_grad",
     "aa_dropout",
-    "aa_layer_workspace_bytes", "aa_layer_norm", "aa_layer_norm_grad",
+    "aa_layer_workspace_bytes", "aa_layer_norm", "aa_layer_norm_grad", "aa_balance", "aa_balance_grad",
 ]
 
 
@@ -115,6 +115,8 @@ def lib():
         "aa_layer_norm": (i32, [vp, i32, i64, vp, i32, i32, vp, vp, f32, vp, i64, vp, vp, vp]),
         "aa_layer_norm_grad": (i32, [vp, i32, i64, vp, i64, vp, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, i32,
                                      vp, sz, vp]),
+        "aa_balance": (i32, [vp, i32, i64, vp, i32, i32, RP, vp, f32, f32, vp, vp, vp, vp, sz, vp]),
+        "aa_balance_grad": (i32, [vp, i32, i64, vp, i32, i32, RP, vp, vp, vp, f32, f32, vp, vp, i64, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -623,3 +625,29 @@ def layer_norm_grad(dout, x, gamma, mean, rstd, residual, count, dx, dgamma, dbe
                                     _array(dgamma, "dgamma", torch.float32, (d,)),
                                     _array(dbeta, "dbeta", torch.float32, (d,)), int(bool(accumulate)), *scratch,
                                     _stream()), "aa_layer_norm_grad")
+
+
+def balance(logits, count, cfg, ids, coef, z_coef, counts, share, loss, ws):
+    """counts: int32 [E]; share: float32 [E] or None; loss: float32 [2] or None; ws: a LayerWorkspace of E columns."""
+    dt = _type(logits, "logits")
+    x, ld = _matrix(logits, "logits")
+    n, E = logits.shape
+    _require(counts is not None, "counts: needed")
+    _check(lib().aa_balance(x, dt, ld, _count(count), n, E, C.byref(cfg), _array(ids, "ids", torch.int32, (n, cfg.top_k)),
+                            coef, z_coef, _array(counts, "counts", torch.int32, (E,)),
+                            _array(share, "share", torch.float32, (E,)), _array(loss, "loss", torch.float32, (2,)),
+                            *_scratch(ws, "a LayerWorkspace"), _stream()), "aa_balance")
+
+
+def balance_grad(logits, count, cfg, ids, dweights, counts, coef, z_coef, dloss, dlogits):
+    """dweights None: the balance loss alone (ids is then not read and may be None); dloss: a float32 tensor of one, or None."""
+    dt = _type(logits, "logits")
+    x, ld = _matrix(logits, "logits")
+    n, E = logits.shape
+    out, ld_out = _matrix(dlogits, "dlogits", logits.dtype, E, n)
+    _check(lib().aa_balance_grad(x, dt, ld, _count(count), n, E, C.byref(cfg),
+                                 _array(ids, "ids", torch.int32, (n, cfg.top_k)),
+                                 _array(dweights, "dweights", torch.float32, (n, cfg.top_k)),
+                                 _array(counts, "counts", torch.int32, (E,)), coef, z_coef,
+                                 _array(dloss, "dloss", torch.float32, least=1), out, ld_out, _stream()),
+           "aa_balance_grad")

@@ -30,7 +30,12 @@ __host__ __device__ inline int column_parts(int64_t d) {
   const int64_t p = (4ll << 20) / (d > 0 ? d : 1);
   return (int)(p < 1 ? 1 : p > kColumnPartsMost ? kColumnPartsMost : p);
 }
-inline size_t column_bytes(int64_t d) { return align_up((size_t)column_parts(d) * 2 * d * sizeof(float), 256); }
+// The workspace: control words, kLayerHead bytes of what blocks have one of, then the columns' parts.
+constexpr size_t kLayerHead = 4096;
+inline size_t layer_bytes(int64_t d) {
+  const size_t parts = align_up((size_t)column_parts(d) * 2 * d * sizeof(float), 256);
+  return kLayerHead + (parts > 16384 ? parts : 16384);
+}
 
 hipError_t launch_layer_norm(const NormArgs &a, int32_t dtype, hipStream_t st);
 hipError_t launch_layer_norm_grad(const NormArgs &a, int32_t dtype, hipStream_t st);

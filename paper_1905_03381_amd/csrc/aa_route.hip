@@ -421,26 +421,245 @@ __global__ __launch_bounds__(256) void k_route(const RouteArgs a) {
   }
 }
 
+// ---- balance loss ---------------------------------------------------------------------------------------
+// With c_e the choices of expert e among the m K of the rows in use, p_te = s_te / sum_e s_te and q_t the softmax of a row:
+//   loss = coef E / (m K) sum_e c_e P_e + z / m sum_t lse_t^2,   P_e = sum_t p_te / m,  lse_t = log sum_e exp x_te
+//   d/dx_te = coef E / (m^2 K) p_te w_te (c_e - sum_e p_te c_e) + 2 z / m lse_t q_te,   w = 1 (softmax) or 1 - s_te (sigmoid).
+// c_e may be counted from the mean of all: both c_e - sum p c then lose fewer digits.
+
+// What a row's EPL logits a lane come to: the shares of the sum of scores (sigmoid: with the scores' complements), the
+// softmax and log sum exp (0 where there is none that is finite).
+template <int LPR, int EPL>
+__device__ __forceinline__ void row_shares(const float (&x)[EPL], bool softmax, float (&p)[EPL], float (&rest)[EPL],
+                                           float (&q)[EPL], float *lse) {
+  float top = kNegInf, sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) top = fmaxf(top, x[i]);
+  top = lanes_max<LPR>(top);
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    q[i] = !(x[i] > kNegInf) ? 0.f : x[i] == top ? 1.f : __expf(x[i] - top);
+    sum += q[i];
+  }
+  sum = lanes_sum<LPR>(sum);
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) q[i] *= inv;
+  *lse = fabsf(top) < -kNegInf ? top + __logf(sum) : 0.f;
+  if (softmax) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      p[i] = q[i];
+      rest[i] = 1.f;
+    }
+    return;
+  }
+  // scores relative to the highest: in 32 bits those of low logits would all be 0
+  const float low = fminf(top, 0.f);
+  float all = 0.f;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    const float t = __expf(-fabsf(x[i])), r = 1.f / (1.f + t);
+    p[i] = x[i] > kNegInf ? __expf(fminf(x[i], 0.f) - low) * r : 0.f;
+    rest[i] = x[i] > 0.f ? t * r : r;
+    all += p[i];
+  }
+  all = lanes_sum<LPR>(all);
+  const float part = all > 0.f ? 1.f / all : 0.f;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) p[i] *= part;
+}
+
+// The experts' choices, counted from their mean, and the factors of the two terms.
+template <int LPR, int EPL>
+__device__ __forceinline__ void balance_scales(const RouteGradArgs &a, int rows, int e0, float (&counts)[EPL],
+                                               float *scale, float *z_scale) {
+  int sum = 0, c[EPL];
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) {
+    c[i] = e0 + i < a.n_experts ? a.counts[e0 + i] : 0;
+    sum += c[i];
+  }
+  const double mean = lanes_sum<LPR>((double)sum) / a.n_experts;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) counts[i] = (float)((double)c[i] - mean);
+  const double m = rows, up = a.dloss ? *a.dloss : 1.f;
+  *scale = (float)(up * a.coef * a.n_experts / (m * m * a.cfg.top_k));
+  *z_scale = (float)(up * 2.0 * a.z_coef / m);
+}
+
+template <int LPR, int EPL>
+__device__ __forceinline__ void balance_terms(const float (&x)[EPL], bool softmax, const float (&counts)[EPL],
+                                              float scale, float z_scale, float (&out)[EPL]) {
+  float p[EPL], rest[EPL], q[EPL], lse, dot = 0.f;
+  row_shares<LPR, EPL>(x, softmax, p, rest, q, &lse);
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) dot += p[i] * counts[i];
+  dot = lanes_sum<LPR>(dot);
+  lse *= z_scale;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) out[i] = scale * p[i] * rest[i] * (counts[i] - dot) + lse * q[i];
+}
+
+constexpr int kBalanceThreads = 1024;
+
+// (sixteen experts a lane take more registers than sixteen waves leave)
+template <int EPL>
+constexpr int kRowsThreads = EPL > 8 ? 512 : kBalanceThreads;
+
+// Shares and choices of the rows that a block takes, a lane's experts in registers; what the block's waves have is added
+// up in LDS, half of them at a time.
+template <int LPR, int EPL>
+__global__ __launch_bounds__(kRowsThreads<EPL>) void k_balance_rows(const BalanceArgs a) {
+  constexpr int kRows = kWave / LPR, kThreads = kRowsThreads<EPL>, kWaves = kThreads / kWave;
+  __shared__ float room[kWaves / 2][EPL][kWave];
+  __shared__ int hist[LPR * EPL];
+  __shared__ float z_room[kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % LPR, e0 = sub * EPL;
+  const int rows = rows_in_use(a.count, a.n_max), E = a.n_experts, K = a.cfg.top_k;
+  const bool softmax = a.cfg.score == AA_SCORE_SOFTMAX;
+  for (int e = threadIdx.x; e < LPR * EPL; e += kThreads) hist[e] = 0;
+  __syncthreads();
+  float sums[EPL], z = 0.f;
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) sums[i] = 0.f;
+  for (int64_t base = ((int64_t)blockIdx.x * kWaves + wave) * kRows; base < rows; base += (int64_t)gridDim.x * kWaves * kRows) {
+    const int64_t row = base + lane / LPR;
+    const bool live = row < rows;
+    float x[EPL];
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) x[i] = kNegInf;
+    if (live) load_logits<EPL>(a.logits, a.dtype, row * a.ld, e0, E, a.vec, x);
+    if (live && sub < K) {
+      const int id = a.ids[row * K + sub];
+      if (id >= 0 && id < E) atomicAdd(&hist[id], 1);
+    }
+    float p[EPL], rest[EPL], q[EPL], lse;
+    row_shares<LPR, EPL>(x, softmax, p, rest, q, &lse);
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) sums[i] += p[i];
+    z += sub == 0 ? lse * lse : 0.f;
+  }
+  if constexpr (LPR == 16) {  // the wave's rows
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) {
+      float u, v;
+      exchange<false>(sums[i], &u, &v);
+      exchange<true>(u + v, &u, &v);
+      sums[i] = u + v;
+    }
+  }
+  z = lanes_sum<64>(z);
+  if (lane == 0) z_room[wave] = z;
+#pragma unroll
+  for (int half = kWaves / 2; half >= 1; half /= 2) {
+    if (wave >= half && wave < 2 * half) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) room[wave - half][i][lane] = sums[i];
+    }
+    __syncthreads();
+    if (wave < half) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) sums[i] += room[wave][i][lane];
+    }
+    __syncthreads();
+  }
+  const int wide = (E + 3) & ~3;
+  float *part = a.part + (size_t)blockIdx.x * 2 * wide;
+  int *choices = reinterpret_cast<int *>(part + wide);
+  if (wave == 0 && lane < LPR) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i)
+      if (e0 + i < wide) part[e0 + i] = e0 + i < E ? sums[i] : 0.f;
+  }
+  for (int e = threadIdx.x; e < wide; e += kThreads) choices[e] = e < LPR * EPL ? hist[e] : 0;
+  if (threadIdx.x == 0) {
+    float all = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) all += z_room[w];
+    a.z_part[blockIdx.x] = all;
+  }
+}
+
+// The blocks' parts, added up in their order by one block, four experts a thread.
+__global__ __launch_bounds__(kBalanceThreads) void k_balance_join(const BalanceArgs a, int blocks) {
+  typedef int i4 __attribute__((ext_vector_type(4)));
+  __shared__ f4 room_p[kBalanceThreads];
+  __shared__ i4 room_c[kBalanceThreads];
+  __shared__ double terms[kBalanceThreads / kWave], squares[kBalanceThreads / kWave];
+  const int rows = rows_in_use(a.count, a.n_max), E = a.n_experts, wide = (E + 3) & ~3, quads = wide / 4;
+  const int shares = kBalanceThreads / quads, quad = threadIdx.x % quads, share = threadIdx.x / quads;
+  f4 p = {0.f, 0.f, 0.f, 0.f};
+  i4 c = {0, 0, 0, 0};
+  if (share < shares) {
+    const int each = (blocks + shares - 1) / shares, from = min(share * each, blocks), to = min(from + each, blocks);
+    const float *at = a.part + quad * 4;
+#pragma unroll 8
+    for (int b = from; b < to; ++b) {
+      p += *reinterpret_cast<const f4 *>(at + (size_t)b * 2 * wide);
+      c += *reinterpret_cast<const i4 *>(at + (size_t)b * 2 * wide + wide);
+    }
+  }
+  room_p[threadIdx.x] = p;
+  room_c[threadIdx.x] = c;
+  __syncthreads();
+  double term = 0.0, square = (int)threadIdx.x < blocks ? (double)a.z_part[threadIdx.x] : 0.0;
+  if ((int)threadIdx.x < quads) {
+    for (int s = 1; s < shares; ++s) {
+      p += room_p[s * quads + threadIdx.x];
+      c += room_c[s * quads + threadIdx.x];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = threadIdx.x * 4 + i;
+      if (e >= E) continue;
+      const double mean = rows > 0 ? (double)p[i] / rows : 0.0;
+      term += (double)c[i] * mean;
+      a.counts[e] = c[i];
+      if (a.share) a.share[e] = (float)mean;
+    }
+  }
+  term = lanes_sum<64>(term);
+  square = lanes_sum<64>(square);
+  if ((threadIdx.x & 63) == 0) {
+    terms[threadIdx.x / kWave] = term;
+    squares[threadIdx.x / kWave] = square;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0 || !a.loss) return;
+  term = square = 0.0;
+  for (int w = 0; w < kBalanceThreads / kWave; ++w) {
+    term += terms[w];
+    square += squares[w];
+  }
+  a.loss[0] = rows > 0 ? (float)(term * a.coef * E / ((double)rows * a.cfg.top_k)) : 0.f;
+  a.loss[1] = rows > 0 ? (float)(square * a.z_coef / rows) : 0.f;
+}
+
+// ---- gradient of the routing ----------------------------------------------------------------------------
 // LPR lanes a row, EPL neighbouring experts each; lane k keeps choice k.  With v the score of the choices and
 // a = scale dweights:
 //   renormalised   ds_k = (a_k - sum a v / S) / S,  S = sum v
 //   sigmoid        dlogit_k = ds_k v_k (1 - v_k), 0 elsewhere
 //   softmax        dlogit_e = s_e (ds_e - sum ds v); renormalised: the softmax over the choices alone.
-template <int LPR, int EPL>
+// BALANCE: the gradient of the balance loss (below) is added to it.
+template <int LPR, int EPL, bool BALANCE>
 __global__ __launch_bounds__(256) void k_route_grad(const RouteGradArgs a) {
   constexpr int kRows = kWave / LPR;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % LPR, e0 = sub * EPL;
   const int rows = rows_in_use(a.count, a.n_max);
   const int E = a.n_experts, K = a.cfg.top_k;
   const bool softmax = a.cfg.score == AA_SCORE_SOFTMAX, renorm = a.cfg.renormalise != 0;
+  float counts[EPL], scale = 0.f, z_scale = 0.f;
+  if constexpr (BALANCE) balance_scales<LPR, EPL>(a, rows, e0, counts, &scale, &z_scale);
   for (int64_t base = ((int64_t)blockIdx.x * 4 + wave) * kRows; base < rows; base += (int64_t)gridDim.x * 4 * kRows) {
     const int64_t row = base + lane / LPR;
     const bool live = row < rows;
     float x[EPL];
-    if (live && softmax) load_logits<EPL>(a.logits, a.dtype, row * a.ld, e0, E, a.vec, x);
+    if (live && (softmax || BALANCE)) load_logits<EPL>(a.logits, a.dtype, row * a.ld, e0, E, a.vec, x);
     int id = -1;
     float d = 0.f, xk = kNegInf;
-    if (live && sub < K) {
+    if (live && sub < K && !(BALANCE && !a.dweights)) {
       id = a.ids[row * K + sub];
       d = a.dweights[row * K + sub] * a.cfg.scale;
       if (id < 0 || id >= E) id = -1;
@@ -452,11 +671,13 @@ __global__ __launch_bounds__(256) void k_route_grad(const RouteGradArgs a) {
 #pragma unroll
     for (int i = 0; i < EPL; ++i) base_[i] = 0.f;
     float top = kNegInf;  // of the row
-    if (softmax) {
-      if (!live) {
+    if ((softmax || BALANCE) && !live) {
 #pragma unroll
-        for (int i = 0; i < EPL; ++i) x[i] = kNegInf;
-      }
+      for (int i = 0; i < EPL; ++i) x[i] = kNegInf;
+    }
+    float balance[EPL];
+    if constexpr (BALANCE) balance_terms<LPR, EPL>(x, softmax, counts, scale, z_scale, balance);
+    if (softmax) {
 #pragma unroll
       for (int i = 0; i < EPL; ++i) top = fmaxf(top, x[i]);
       top = lanes_max<LPR>(top);
@@ -505,6 +726,10 @@ __global__ __launch_bounds__(256) void k_route_grad(const RouteGradArgs a) {
 #pragma unroll
       for (int i = 0; i < EPL; ++i)
         if (at == i) base_[i] = vk;
+    }
+    if constexpr (BALANCE) {
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) base_[i] += balance[i];
     }
     if (live) {
       const int64_t to = row * a.ld_out;
@@ -772,9 +997,38 @@ hipError_t launch_route_grad(const RouteGradArgs &args, hipStream_t st) {
     constexpr int LPR = decltype(lpr)::value, EPL = decltype(epl)::value;
     a.vec = whole_lanes(a.logits, a.ld, a.n_experts, EPL, a.dtype) &&
             whole_lanes(a.dlogits, a.ld_out, a.n_experts, EPL, a.dtype);
-    hipLaunchKernelGGL((k_route_grad<LPR, EPL>), blocks_for(a.n_max, 4 * (kWave / LPR)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_route_grad<LPR, EPL, false>), blocks_for(a.n_max, 4 * (kWave / LPR)), dim3(256), 0, st, a);
     return hipGetLastError();
   });
+}
+
+hipError_t launch_balance_grad(const RouteGradArgs &args, hipStream_t st) {
+  RouteGradArgs a = args;
+  if (a.n_max == 0) return hipSuccess;
+  return by_width(a.n_experts, a.cfg.top_k, 128, [&](auto lpr, auto epl) {
+    constexpr int LPR = decltype(lpr)::value, EPL = decltype(epl)::value;
+    a.vec = whole_lanes(a.logits, a.ld, a.n_experts, EPL, a.dtype) &&
+            whole_lanes(a.dlogits, a.ld_out, a.n_experts, EPL, a.dtype);
+    const dim3 want = blocks_for(a.n_max, 4 * (kWave / LPR));
+    hipLaunchKernelGGL((k_route_grad<LPR, EPL, true>), want, dim3(256), 0, st, a);
+    return hipGetLastError();
+  });
+}
+
+hipError_t launch_balance(const BalanceArgs &args, hipStream_t st) {
+  BalanceArgs a = args;
+  int blocks = 0;
+  const hipError_t e = by_width(a.n_experts, a.cfg.top_k, 128, [&](auto lpr, auto epl) {
+    constexpr int LPR = decltype(lpr)::value, EPL = decltype(epl)::value, kThreads = kRowsThreads<EPL>, kRows = kThreads / LPR;
+    const int64_t want = ((int64_t)a.n_max + kRows - 1) / kRows;
+    blocks = (int)(want < 1 ? 1 : want < kBalanceBlocks ? want : kBalanceBlocks);
+    a.vec = whole_lanes(a.logits, a.ld, a.n_experts, EPL, a.dtype);
+    hipLaunchKernelGGL((k_balance_rows<LPR, EPL>), dim3(blocks), dim3(kThreads), 0, st, a);
+    return hipGetLastError();
+  });
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(k_balance_join, dim3(1), dim3(kBalanceThreads), 0, st, a, blocks);
+  return hipGetLastError();
 }
 
 hipError_t launch_expert_plan(const PlanArgs &a, hipStream_t st) {

@@ -32,7 +32,28 @@ struct RouteGradArgs {
   const float *dweights;
   void *dlogits;
   int64_t ld_out;
+  // with the gradient of the balance loss (dweights may then be NULL)
+  const int32_t *counts;
+  float coef, z_coef;
+  const float *dloss;
 };
+
+struct BalanceArgs {
+  const void *logits;
+  int32_t dtype, vec;
+  int64_t ld;
+  const int32_t *count;
+  int32_t n_max, n_experts;
+  aa_route_config cfg;
+  const int32_t *ids;
+  float coef, z_coef;
+  int32_t *counts;
+  float *share, *loss;
+  float *z_part;  // [blocks]
+  float *part;    // [blocks][2][E up to a multiple of 4]: shares, then (int32) choices
+};
+
+constexpr int kBalanceBlocks = 256;
 
 struct PlanArgs {
   const int32_t *ids;
@@ -50,6 +71,8 @@ inline size_t plan_table_ints(int64_t n_max, int32_t top_k, int32_t n_experts) {
 // plan: made in the same call (may be NULL)
 hipError_t launch_route(const RouteArgs &a, const PlanArgs *plan, hipStream_t st);
 hipError_t launch_route_grad(const RouteGradArgs &a, hipStream_t st);
+hipError_t launch_balance(const BalanceArgs &a, hipStream_t st);
+hipError_t launch_balance_grad(const RouteGradArgs &a, hipStream_t st);
 hipError_t launch_expert_plan(const PlanArgs &a, hipStream_t st);
 
 }  // namespace aa

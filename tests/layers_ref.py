@@ -100,3 +100,54 @@ def norm_grad_bounds(dout, x, gamma, mean, rstd, residual, dtype):
     of_dx += half_step(dtype) * (np.abs(dx) + of_dx) + tiny(dtype)
     rows = len(x) + 64
     return of_dx, (rows + 3) * U32 * (np.abs(dout) * xh).sum(0), rows * U32 * np.abs(dout).sum(0)
+
+
+# ---------------------------------------------------------------------------
+# balance of a router
+
+
+def shares(x, kind):
+    """p, softmax, log sum exp (0 where it is not finite) and 1 - score of float64 logits; -inf and NaN are not free."""
+    free = x > -np.inf  # (False for NaN)
+    x = np.where(free, x, -np.inf)
+    top = x.max(1, keepdims=True)
+    with np.errstate(invalid="ignore", over="ignore"):
+        e = np.where(free, np.where(x == top, 1.0, np.exp(x - np.where(np.isfinite(top), top, 0.0))), 0.0)
+        e = np.where(np.isinf(top) & (x < top), 0.0, e)
+    total = e.sum(1, keepdims=True)
+    q = np.where(total > 0, e / np.where(total > 0, total, 1.0), 0.0)
+    finite = np.isfinite(top[:, 0])
+    lse = np.where(finite, np.where(finite, top[:, 0], 0.0) + np.log(np.where(total[:, 0] > 0, total[:, 0], 1.0)), 0.0)
+    if kind == "softmax":
+        return q, q, lse, np.ones_like(q)
+    with np.errstate(over="ignore"):
+        t = np.exp(-np.abs(x))
+    low = np.minimum(x, 0.0)
+    best = np.where(np.isfinite(low.max(1, keepdims=True)), low.max(1, keepdims=True), 0.0)
+    s = np.where(free, np.exp(low - best) / (1 + t), 0.0)  # (relative to the row's highest)
+    total = s.sum(1, keepdims=True)
+    rest = np.where(x > 0, t / (1 + t), 1 / (1 + t))
+    return np.where(total > 0, s / np.where(total > 0, total, 1.0), 0.0), q, lse, rest
+
+
+def choices(ids, n_experts):
+    ids = ids[(ids >= 0) & (ids < n_experts)]
+    return np.bincount(ids.reshape(-1), minlength=n_experts)
+
+
+def balance(x, kind, ids, coef, z_coef):
+    """counts, shares, losses"""
+    m, E = x.shape
+    counts = choices(ids, E)
+    if m == 0:
+        return counts, np.zeros(E), np.zeros(2)
+    p, _, lse, _ = shares(x, kind)
+    share = p.sum(0) / m
+    return counts, share, np.array([coef * E / (m * ids.shape[1]) * (counts * share).sum(), z_coef / m * (lse ** 2).sum()])
+
+
+def balance_grad(x, kind, counts, top_k, coef, z_coef, up=1.0):
+    m, E = x.shape
+    p, q, lse, rest = shares(x, kind)
+    d = coef * E / (m * m * top_k) * p * rest * (counts - (p * counts).sum(1, keepdims=True))
+    return up * (d + 2 * z_coef / m * lse[:, None] * q)

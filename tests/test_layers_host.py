@@ -25,7 +25,32 @@ NORM = dict(x=P, dtype=BF16, ldx=32, count=None, n_max=8, d=32, gamma=P, beta=P,
 NORM_GRAD = dict(dout=P, dtype=BF16, lddo=32, x=P, ldx=32, count=None, n_max=8, d=32, gamma=P, mean=P, rstd=P,
                  residual=None, ldr=0, dx=P, lddx=32, dgamma=P, dbeta=P, accumulate=0, ws=P, ws_bytes=BIG, stream=None)
 
+
+def cfg(**change):
+    c = api.route_config("softmax", 4)
+    for k, v in change.items():
+        setattr(c, k, v)
+    return c
+
+
+BALANCE = dict(logits=P, dtype=BF16, ld=16, count=None, n_max=8, n_experts=16, cfg=cfg(), ids=P, coef=0.1, z_coef=0.1,
+               counts=P, share=P, loss=P, ws=P, ws_bytes=BIG, stream=None)
+BALANCE_GRAD = dict(logits=P, dtype=BF16, ld=16, count=None, n_max=8, n_experts=16, cfg=cfg(), ids=P, dweights=P, counts=P,
+                    coef=0.1, z_coef=0.1, dloss=None, dlogits=P, ld_out=16, stream=None)
+OF_BOTH = [(dict(logits=None), NULL), (dict(cfg=None), NULL), (dict(dtype=3), SHAPE), (dict(n_max=-1), SHAPE),
+           (dict(n_experts=0), SHAPE), (dict(n_experts=1025, ld=1025), SHAPE), (dict(ld=15), SHAPE),
+           (dict(cfg=cfg(top_k=0)), SHAPE), (dict(cfg=cfg(top_k=17)), SHAPE), (dict(cfg=cfg(score=2)), SHAPE),
+           (dict(cfg=cfg(scale=INF)), SHAPE), (dict(coef=NAN), SHAPE), (dict(z_coef=INF), SHAPE),
+           (dict(logits=P + 1), ALIGN), (dict(count=P + 2), ALIGN), (dict(ids=P + 2), ALIGN), (dict(ids=None), NULL),
+           (dict(counts=None), NULL), (dict(counts=P + 2), ALIGN)]
+
 REFUSED = [
+    ("aa_balance", BALANCE, OF_BOTH + [
+        (dict(share=P + 2), ALIGN), (dict(loss=P + 2), ALIGN), (dict(ws=None), WORKSPACE), (dict(ws_bytes=4096), WORKSPACE),
+        (dict(ws=P + 64), WORKSPACE)]),
+    ("aa_balance_grad", BALANCE_GRAD, OF_BOTH + [
+        (dict(dlogits=None), NULL), (dict(ld_out=15), SHAPE), (dict(dlogits=P + 1), ALIGN), (dict(dloss=P + 2), ALIGN),
+        (dict(dweights=P + 2), ALIGN)]),
     ("aa_layer_norm", NORM, [
         (dict(x=None), NULL), (dict(out=None), NULL), (dict(dtype=3), SHAPE), (dict(dtype=-1), SHAPE),
         (dict(n_max=-1), SHAPE), (dict(d=0), SHAPE), (dict(d=(1 << 24) + 1, ldx=BIG, ldo=BIG), SHAPE),
