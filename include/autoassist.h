@@ -549,6 +549,63 @@ int32_t aa_balance_grad(const void *logits, int32_t dtype, int64_t ld, const int
                         const int32_t *counts, float coef, float z_coef, const float *dloss, void *dlogits,
                         int64_t ld_out, void *stream);
 
+/* ---- AdamW over many tensors at once -------------------------------------------
+ * One update of all tensors in one launch:
+ *   g = grad *grad_factor,  m = beta1 m + (1 - beta1) g,  v = beta2 v + (1 - beta2) g^2,  t = *t + 1,
+ *   param = param (1 - lr weight_decay decay) - lr m / (1 - beta1^t) / (sqrt(v / (1 - beta2^t)) + eps),
+ * lr = cfg->lr *lr_factor; parameters are fp32, `copy` receives them rounded, for the products.
+ * States are fp32 (state_bits 32), or of 8 bits: elements [256 b, 256 b + 256) of a tensor share the scales m_scale[b] and
+ * v_scale[b] (a power of two that brings the largest into [128, 256), 0 for zeros), and m is held as code m_scale,
+ * v as (code v_scale)^2, the codes of one byte in the OCP format e4m3.  The update uses the new m and v before they are
+ * rounded.  Rounding is at random: with a the value in units of the scale and s = 2^max(floor(log2 a) - 3, -9) a step of
+ * the format there, the code is s floor(a / s + draw / 65536) (v's: at least one step if a > 0), the draw being the 16-bit
+ * draw i % 8 of Philox4x32-10(counter = (i / 8, 2^31 + the tensor's number, t, 0), key = cfg->seed) for element i (halves
+ * as in aa_dropout), the same for m and v.  What is not finite is held as NaN, and the others' scale does not see it.
+ * Zeroed states (and scales) are those of a start. */
+#define AA_STATE_BLOCK 256
+
+typedef struct aa_adamw_tensor {
+  float *param;
+  const void *grad;
+  void *copy;             /* NULL: none */
+  void *m, *v;            /* float[n], or uint8_t[n] with state_bits 8 */
+  float *m_scale, *v_scale; /* [ceil(n / 256)] with state_bits 8 */
+  int64_t n;              /* elements, 0 to 2^35 */
+  int32_t grad_dtype;     /* AA_F32, AA_BF16 or AA_F16 */
+  int32_t copy_dtype;     /* AA_BF16 or AA_F16, where copy is */
+  int32_t state_bits;     /* 32 or 8 */
+  float decay;            /* factor of the weight decay: 0 for vectors that take none */
+} aa_adamw_tensor;
+
+typedef struct aa_adamw_config {
+  float lr, beta1, beta2, eps, weight_decay; /* 0 <= beta < 1, eps > 0, lr and weight_decay >= 0 */
+  int32_t reserved;
+  uint64_t seed; /* of the rounding of 8-bit states */
+} aa_adamw_config;
+
+/* The list of the tensors on the device: made once, used by every step as long as the tensors stay where they are.
+ * `tensors` is a HOST array of n_tensors (1 to 65536); no element belongs to two of them.  aa_adamw_chunks: how many chunks they are cut
+ * into, or a negative AA_ERR_* if the list is refused.  `table`: device memory of aa_adamw_table_bytes(n_tensors, n_chunks)
+ * bytes, 256-byte aligned; it must not be used by two calls that may overlap in time. */
+int64_t aa_adamw_chunks(const aa_adamw_tensor *tensors, int32_t n_tensors);
+size_t aa_adamw_table_bytes(int32_t n_tensors, int64_t n_chunks);
+int32_t aa_adamw_table(const aa_adamw_tensor *tensors, int32_t n_tensors, void *table, size_t table_bytes,
+                       void *stream);
+
+/* Norm of all gradients together, and the factor that an update takes them with:
+ *   out[0] = |s| sqrt(sum g^2),  out[1] = s min(1, max_norm / out[0]),  s = *scale (device scalar; NULL: 1).
+ * Sums are held in 64 bits.  out[1] is NaN if the norm is not finite: aa_adamw_step then leaves everything as it is.
+ * max_norm > 0 (infinity: no clipping). */
+int32_t aa_grad_norm(void *table, size_t table_bytes, int32_t n_tensors, int64_t n_chunks, float max_norm,
+                     const float *scale, float *out, void *stream);
+
+/* The update.  lr_factor, grad_factor: device scalars (NULL: 1).  t: device counter of the updates made, one more after
+ * the call.  Nothing changes, t included, if count != NULL and *count <= 0 (an empty batch) or if *grad_factor is not
+ * finite. */
+int32_t aa_adamw_step(void *table, size_t table_bytes, int32_t n_tensors, int64_t n_chunks,
+                      const aa_adamw_config *cfg, const float *lr_factor, const float *grad_factor,
+                      const int32_t *count, int32_t *t, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

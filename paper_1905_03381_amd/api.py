@@ -33,6 +33,7 @@ SYMBOLS = [
     "aa_expert_grad_input", "aa_expert_grad_weight", "aa_expert_combine", "aa_expert_combine_grad",
     "aa_dropout",
     "aa_layer_workspace_bytes", "aa_layer_norm", "aa_layer_norm_grad", "aa_balance", "aa_balance_grad",
+    "aa_adamw_chunks", "aa_adamw_table_bytes", "aa_adamw_table", "aa_grad_norm", "aa_adamw_step",
 ]
 
 
@@ -58,6 +59,17 @@ class aa_route_config(C.Structure):
                 ("scale", C.c_float), ("reserved", C.c_int32)]
 
 
+class aa_adamw_tensor(C.Structure):
+    _fields_ = [("param", C.c_void_p), ("grad", C.c_void_p), ("copy", C.c_void_p), ("m", C.c_void_p), ("v", C.c_void_p),
+                ("m_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n", C.c_int64), ("grad_dtype", C.c_int32),
+                ("copy_dtype", C.c_int32), ("state_bits", C.c_int32), ("decay", C.c_float)]
+
+
+class aa_adamw_config(C.Structure):
+    _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
+                ("weight_decay", C.c_float), ("reserved", C.c_int32), ("seed", C.c_uint64)]
+
+
 _lib = None
 
 
@@ -72,6 +84,7 @@ def lib():
     L = C.CDLL(LIB_PATH)
     vp, i32, i64, u64, f32, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_uint64, C.c_float, C.c_size_t
     FP, CP, RP = C.POINTER(aa_features), C.POINTER(aa_step_config), C.POINTER(aa_route_config)
+    TP, AP = C.POINTER(aa_adamw_tensor), C.POINTER(aa_adamw_config)
     sig = {
         "aa_version": (i32, []),
         "aa_status_string": (C.c_char_p, [i32]),
@@ -117,6 +130,11 @@ def lib():
                                      vp, sz, vp]),
         "aa_balance": (i32, [vp, i32, i64, vp, i32, i32, RP, vp, f32, f32, vp, vp, vp, vp, sz, vp]),
         "aa_balance_grad": (i32, [vp, i32, i64, vp, i32, i32, RP, vp, vp, vp, f32, f32, vp, vp, i64, vp]),
+        "aa_adamw_chunks": (i64, [TP, i32]),
+        "aa_adamw_table_bytes": (sz, [i32, i64]),
+        "aa_adamw_table": (i32, [TP, i32, vp, sz, vp]),
+        "aa_grad_norm": (i32, [vp, sz, i32, i64, f32, vp, vp, vp]),
+        "aa_adamw_step": (i32, [vp, sz, i32, i64, AP, vp, vp, vp, vp, vp]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -651,3 +669,71 @@ def balance_grad(logits, count, cfg, ids, dweights, counts, coef, z_coef, dloss,
                                  _array(counts, "counts", torch.int32, (E,)), coef, z_coef,
                                  _array(dloss, "dloss", torch.float32, least=1), out, ld_out, _stream()),
            "aa_balance_grad")
+
+
+STATE_BLOCK = 256   # AA_STATE_BLOCK
+
+
+def adamw_tensor(param, grad, m, v, copy=None, m_scale=None, v_scale=None, decay=1.0):
+    """One tensor of an update.  param float32, grad of any of the three types, copy bfloat16 or float16; all of the same number of
+    elements, contiguous.  m, v: float32, or float8_e4m3fn with m_scale, v_scale float32 (one for 256 neighbours)."""
+    _require(isinstance(param, torch.Tensor), "param: a tensor")
+    n, bits8 = param.numel(), isinstance(m, torch.Tensor) and m.dtype == torch.float8_e4m3fn
+    code = _type(grad, "grad")
+    state = torch.float8_e4m3fn if bits8 else torch.float32
+
+    def flat(t, name, dtype, size=n):
+        p = _array(t, name, dtype)
+        _require(p is not None and t.numel() == size, f"{name}: {size} elements are needed")
+        return p
+
+    copy_code = 0 if copy is None else _type(copy, "copy", products=True)
+    blocks = -(-n // STATE_BLOCK)
+    out = aa_adamw_tensor(
+        flat(param, "param", torch.float32), flat(grad, "grad", grad.dtype),
+        None if copy is None else flat(copy, "copy", copy.dtype), flat(m, "m", state), flat(v, "v", state),
+        flat(m_scale, "m_scale", torch.float32, blocks) if bits8 else None,
+        flat(v_scale, "v_scale", torch.float32, blocks) if bits8 else None,
+        n, code, copy_code, 8 if bits8 else 32, decay)
+    out._tensors = (param, grad, copy, m, v, m_scale, v_scale)
+    return out
+
+
+class AdamWTable:
+    """The tensors of an optimizer's steps, listed on the device once.  Holds references to them: they stay where they are."""
+
+    def __init__(self, tensors, device="cuda"):
+        self._tensors = [t._tensors for t in tensors]
+        self.n = len(tensors)
+        _require(self.n > 0, "tensors: at least one")
+        listed = (aa_adamw_tensor * self.n)(*tensors)
+        self.chunks = int(lib().aa_adamw_chunks(listed, self.n))
+        _check(min(self.chunks, 0), "aa_adamw_chunks")
+        self.bytes = int(lib().aa_adamw_table_bytes(self.n, self.chunks))
+        self.buf = torch.empty(self.bytes + 256, dtype=torch.uint8, device=device)
+        self.ptr = self.buf.data_ptr() + (-self.buf.data_ptr()) % 256
+        _check(lib().aa_adamw_table(listed, self.n, self.ptr, self.bytes, _stream()), "aa_adamw_table")
+
+
+def adamw_config(lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0):
+    return aa_adamw_config(lr, beta1, beta2, eps, weight_decay, 0, seed)
+
+
+def _scalar(t, name, dtype=torch.float32):
+    return _array(t, name, dtype, least=1)
+
+
+def grad_norm(table, max_norm, scale, out):
+    """out: float32 [2], the norm of all gradients and the factor for adamw_step; scale: a float32 tensor of one, or None."""
+    _require(out is not None, "out: needed")
+    _check(lib().aa_grad_norm(table.ptr, table.bytes, table.n, table.chunks, max_norm, _scalar(scale, "scale"),
+                              _array(out, "out", torch.float32, least=2), _stream()), "aa_grad_norm")
+
+
+def adamw_step(table, cfg, lr_factor, grad_factor, count, t):
+    """lr_factor, grad_factor: float32 tensors of one, or None (1); count: an int32 tensor of one, or None; t: the int32 tensor of
+    one that counts the updates."""
+    _require(t is not None, "t: needed")
+    _check(lib().aa_adamw_step(table.ptr, table.bytes, table.n, table.chunks, C.byref(cfg),
+                               _scalar(lr_factor, "lr_factor"), _scalar(grad_factor, "grad_factor"), _count(count),
+                               _scalar(t, "t", torch.int32), _stream()), "aa_adamw_step")

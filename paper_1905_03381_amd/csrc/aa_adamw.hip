@@ -1,0 +1,351 @@
+// One AdamW update of many tensors, and the norm of all their gradients.
+//
+// The tensors are cut into chunks of 2048 elements, listed once in a table on the device; a launch walks all of them, each block a
+// run of neighbouring chunks, eight neighbouring elements a thread.  Bound by memory: 28 to 30 bytes an element with
+// states in 32 bits, 16 to 18 with states in 8.
+//
+// States in 8 bits: 256 neighbours share a power of two that brings their largest into [128, 256), and each is held
+// as an e4m3 number (steps of an eighth to a sixteenth of it, down to 2^-17 of the largest).  v is held as its root, so
+// that its range is twice that, and never as 0 where it is above: the denominator then errs to the safe side.  A
+// state moves by 1 - beta a step, for v a thousandth, far less than half a step of the format: rounded to the nearest it would
+// stay where it is for good.  So it is rounded at random, up as often as the fraction says, with 16-bit draws of the generator
+// the keep draws use; its mean is then right.  m and v of an element share a draw.
+#include "aa_adamw.hpp"
+
+#include "aa_lines.hpp"
+
+#include <type_traits>
+
+namespace aa {
+
+namespace {
+
+constexpr int kUnits = 256;  // compute units
+constexpr int kBatch = 32;   // entries that travel as arguments of one launch
+
+struct EntryBatch {
+  TensorEntry e[kBatch];
+};
+
+// Entries [first, first + gridDim.x) of the table and the chunks that belong to them.
+__global__ __launch_bounds__(256) void k_adamw_table(char *table, int64_t map, int64_t n_chunks, int32_t first,
+                                                     const EntryBatch batch) {
+  const TensorEntry e = batch.e[blockIdx.x];
+  const int32_t tensor = first + (int32_t)blockIdx.x;
+  if (threadIdx.x == 0) reinterpret_cast<TensorEntry *>(table + kTableEntries)[tensor] = e;
+  if (tensor == 0 && threadIdx.x < 64) reinterpret_cast<int32_t *>(table)[threadIdx.x] = threadIdx.x == 2 ? (int32_t)n_chunks : 0;
+  int32_t *of = reinterpret_cast<int32_t *>(table + map) + e.first_chunk;
+  const int64_t chunks = (e.n + kChunk - 1) / kChunk;
+  for (int64_t c = threadIdx.x; c < chunks; c += 256) of[c] = tensor;
+}
+
+// Gradients i .. i + 7 of a tensor, of which n (at least one) exist.
+__device__ __forceinline__ Eight load_grad(const TensorEntry &e, int64_t i, int n) {
+  if (e.grad_dtype == AA_BF16) return load8(static_cast<const __bf16 *>(e.grad) + i, n);
+  if (e.grad_dtype == AA_F16) return load8(static_cast<const _Float16 *>(e.grad) + i, n);
+  return load8(static_cast<const float *>(e.grad) + i, n);
+}
+
+// The chunks of this block: a run of neighbouring ones.
+struct Run {
+  int64_t from, to;
+};
+__device__ __forceinline__ Run chunks_of_block(const AdamWArgs &a) {
+  const int64_t listed = reinterpret_cast<const int32_t *>(a.table)[2], all = a.n_chunks < listed ? a.n_chunks : listed;
+  return {all * blockIdx.x / gridDim.x, all * (blockIdx.x + 1) / gridDim.x};
+}
+
+__device__ __forceinline__ int tensor_of(const AdamWArgs &a, int64_t chunk) {
+  return __builtin_amdgcn_readfirstlane(reinterpret_cast<const int32_t *>(a.table + a.map)[chunk]);
+}
+
+// Whether this block is the last of the grid to come here (its thread 0 only); the word is 0 again then.  ORDERED: what the
+// others' threads 0 wrote before is seen after.
+template <bool ORDERED>
+__device__ __forceinline__ bool last_block(int32_t *word) {
+  const int before = __hip_atomic_fetch_add(word, 1, ORDERED ? __ATOMIC_ACQ_REL : __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (before != (int)gridDim.x - 1) return false;
+  __hip_atomic_store(word, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+  for (int off = kWave / 2; off > 0; off >>= 1) v += __shfl_xor(v, off, kWave);
+  return v;
+}
+
+// Sum of squares in 64 bits (32 would end at gradients of 1.8e19).  Each block's part, and the last block adds them
+// up in their order.
+__global__ __launch_bounds__(256) void k_grad_norm(const AdamWArgs a) {
+  __shared__ double room[4];
+  __shared__ int last;
+  const Run run = chunks_of_block(a);
+  const TensorEntry *entries = reinterpret_cast<const TensorEntry *>(a.table + kTableEntries);
+  double *parts = reinterpret_cast<double *>(a.table + kTableParts);
+  double sum = 0.0;
+  for (int64_t c = run.from; c < run.to; ++c) {
+    const TensorEntry &e = entries[tensor_of(a, c)];
+    const int64_t i = (c - e.first_chunk) * kChunk + threadIdx.x * 8;
+    if (i >= e.n) continue;
+    const int64_t left = e.n - i;
+    const Eight g = load_grad(e, i, left < 8 ? (int)left : 8);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sum = fma((double)g.v[k], (double)g.v[k], sum);
+  }
+  sum = wave_sum(sum);
+  const int wave = threadIdx.x / kWave;
+  if ((threadIdx.x & 63) == 0) room[wave] = sum;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    __hip_atomic_store(parts + blockIdx.x, room[0] + room[1] + room[2] + room[3], __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+    last = last_block<true>(reinterpret_cast<int32_t *>(a.table));
+  }
+  __syncthreads();
+  if (!last) return;
+  sum = 0.0;
+#pragma unroll
+  for (int k = 0; k < kNormBlocks / 256; ++k) {
+    const int b = k * 256 + (int)threadIdx.x;
+    if (b < (int)gridDim.x) sum += __hip_atomic_load(parts + b, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  sum = wave_sum(sum);
+  if ((threadIdx.x & 63) == 0) room[wave] = sum;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  const float scale = a.scale ? *a.scale : 1.f;
+  const float norm = (float)(sqrt(room[0] + room[1] + room[2] + room[3]) * fabs((double)scale));
+  a.out[0] = norm;
+  a.out[1] = !(norm < __builtin_inff()) ? __builtin_nanf("") : norm > a.max_norm ? scale * (a.max_norm / norm) : scale;
+}
+
+// What all elements of an update have in common.
+struct Step {
+  float beta1, beta2, eps, factor, rate, root, shrink;
+  uint32_t k0, k1, t;
+};
+
+// The new m and v (its root in r) of eight elements, and their parameters.
+__device__ __forceinline__ void update8(const Step &s, const Eight &g, Eight &m, Eight &v, Eight &r, Eight &p, float shrink) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const float d = g.v[k] * s.factor;
+    m.v[k] = s.beta1 * m.v[k] + (1.f - s.beta1) * d;
+    v.v[k] = s.beta2 * v.v[k] + (1.f - s.beta2) * (d * d);
+    r.v[k] = sqrtf(v.v[k]);
+    p.v[k] = p.v[k] * shrink - s.rate * m.v[k] / (r.v[k] * s.root + s.eps);
+  }
+}
+
+__device__ __forceinline__ void store_param(const TensorEntry &e, int64_t i, int n, const Eight &p) {
+  store8(e.param + i, p, n);
+  if (!e.copy) return;
+  if (e.copy_dtype == AA_BF16) store8(static_cast<__bf16 *>(e.copy) + i, p, n);
+  else store8(static_cast<_Float16 *>(e.copy) + i, p, n);
+}
+
+struct Codes {
+  uint32_t w[2];
+};
+typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
+
+__device__ __forceinline__ Codes load_codes(const uint8_t *p, int n) {
+  Codes c = {{0u, 0u}};
+  if (n >= 8) {
+    const u32x2_any v = *reinterpret_cast<const u32x2_any *>(p);
+    c.w[0] = v[0];
+    c.w[1] = v[1];
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < n) c.w[k / 4] |= (uint32_t)p[k] << (k % 4 * 8);
+  }
+  return c;
+}
+
+__device__ __forceinline__ void store_codes(uint8_t *p, int n, const Codes &c) {
+  if (n >= 8) {
+    u32x2_any v;
+    v[0] = c.w[0];
+    v[1] = c.w[1];
+    *reinterpret_cast<u32x2_any *>(p) = v;
+  } else {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (k < n) p[k] = (uint8_t)(c.w[k / 4] >> (k % 4 * 8));
+  }
+}
+
+__device__ __forceinline__ Eight decode(const Codes &c, float scale) {
+  Eight o;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.w[h], false);
+    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c.w[h], true);
+    o.v[h * 4 + 0] = lo[0] * scale;
+    o.v[h * 4 + 1] = lo[1] * scale;
+    o.v[h * 4 + 2] = hi[0] * scale;
+    o.v[h * 4 + 3] = hi[1] * scale;
+  }
+  return o;
+}
+
+// Largest value of 32 neighbouring lanes.
+__device__ __forceinline__ float block_max(float v) {
+  const auto move = [](float x, auto ctrl) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xF, 0xF, true));
+  };
+  v = fmaxf(v, move(v, std::integral_constant<int, 0xB1>()));
+  v = fmaxf(v, move(v, std::integral_constant<int, 0x4E>()));
+  v = fmaxf(v, move(v, std::integral_constant<int, 0x141>()));
+  v = fmaxf(v, move(v, std::integral_constant<int, 0x140>()));
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
+
+// Codes and scale of the block's states.  A step of the format at a is 2^max(exponent - 3, -9); a in steps plus the draw's
+// part of one, cut, is the rounding.  What is not finite is held as NaN and takes no part in the scale.
+template <bool AT_LEAST_ONE>
+__device__ __forceinline__ Codes encode(const Eight &x, const uint4 &draws, float *scale) {
+  float most = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x.v[k]) < __builtin_inff() ? fabsf(x.v[k]) : 0.f);
+  most = block_max(most);
+  const int e = max((int)(__float_as_uint(most) >> 23) - 126 - 8, -126);
+  *scale = most > 0.f ? power_of_two(e) : 0.f;
+  const float inv = power_of_two(-e);
+  const uint32_t words[4] = {draws.x, draws.y, draws.z, draws.w};
+  float y[8];
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    const uint32_t draw = k & 1 ? words[k >> 1] >> 16 : words[k >> 1] & 0xFFFFu;
+    const float a = fabsf(x.v[k]) * inv;
+    const int s = max((int)(__float_as_uint(a) >> 23) - 130, -9);
+    float q = floorf(a * power_of_two(-s) + (float)draw * 0x1p-16f);
+    if (AT_LEAST_ONE && a > 0.f) q = fmaxf(q, 1.f);
+    y[k] = copysignf(q * power_of_two(s), x.v[k]);
+    if (!(fabsf(x.v[k]) < __builtin_inff())) y[k] = __builtin_nanf("");
+  }
+  Codes c;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[h * 4], y[h * 4 + 1], 0, false);
+    c.w[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[h * 4 + 2], y[h * 4 + 3], w, true);
+  }
+  return c;
+}
+
+__global__ __launch_bounds__(256) void k_adamw_step(const AdamWArgs a) {
+  const int32_t before = *a.t;
+  const float factor = a.grad_factor ? *a.grad_factor : 1.f;
+  // an empty batch, or gradients that are not finite: nothing changes
+  const bool skip = (a.count && *a.count <= 0) || !(fabsf(factor) < __builtin_inff());
+  if (!skip) {
+    const float lr = a.cfg.lr * (a.lr_factor ? *a.lr_factor : 1.f);
+    const float t = (float)before + 1.f;
+    Step s;
+    s.beta1 = a.cfg.beta1;
+    s.beta2 = a.cfg.beta2;
+    s.eps = a.cfg.eps;
+    s.factor = factor;
+    s.rate = lr / -expm1f(t * a.log_beta1);
+    s.root = 1.f / sqrtf(-expm1f(t * a.log_beta2));
+    s.shrink = lr * a.cfg.weight_decay;
+    s.k0 = (uint32_t)a.cfg.seed;
+    s.k1 = (uint32_t)(a.cfg.seed >> 32);
+    s.t = (uint32_t)before + 1u;
+    const Run run = chunks_of_block(a);
+    const TensorEntry *entries = reinterpret_cast<const TensorEntry *>(a.table + kTableEntries);
+    for (int64_t c = run.from; c < run.to; ++c) {
+      const int tensor = tensor_of(a, c);
+      const TensorEntry &e = entries[tensor];
+      const int64_t i = (c - e.first_chunk) * kChunk + threadIdx.x * 8, left = e.n - i;
+      const int n = left < 8 ? (int)left : 8;
+      const float shrink = 1.f - s.shrink * e.decay;
+      Eight r;
+      if (e.bits == 32) {
+        if (n <= 0) continue;
+        float *pm = static_cast<float *>(e.m) + i, *pv = static_cast<float *>(e.v) + i;
+        const Eight g = load_grad(e, i, n);
+        Eight p = load8(e.param + i, n), m = load8(pm, n), v = load8(pv, n);
+        update8(s, g, m, v, r, p, shrink);
+        store_param(e, i, n, p);
+        store8(pm, m, n);
+        store8(pv, v, n);
+      } else {
+        Eight m, v, p;
+        uint8_t *pm = static_cast<uint8_t *>(e.m) + i, *pv = static_cast<uint8_t *>(e.v) + i;
+        float *ms = e.m_scale + i / kStateBlock, *vs = e.v_scale + i / kStateBlock;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) m.v[k] = r.v[k] = 0.f;
+        if (n > 0) {
+          const Eight g = load_grad(e, i, n);
+          p = load8(e.param + i, n);
+          m = decode(load_codes(pm, n), *ms);
+          v = decode(load_codes(pv, n), *vs);
+#pragma unroll
+          for (int k = 0; k < 8; ++k) v.v[k] *= v.v[k];
+          update8(s, g, m, v, r, p, shrink);
+          store_param(e, i, n, p);
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (k >= n) m.v[k] = r.v[k] = 0.f;
+        }
+        const uint4 draws = philox_words((uint32_t)(i / 8), 0x80000000u | (uint32_t)tensor, s.t, 0u, s.k0, s.k1);
+        float m_scale, v_scale;
+        const Codes cm = encode<false>(m, draws, &m_scale), cv = encode<true>(r, draws, &v_scale);
+        if (n > 0) {
+          store_codes(pm, n, cm);
+          store_codes(pv, n, cv);
+          if (threadIdx.x % (kStateBlock / 8) == 0) {
+            *ms = m_scale;
+            *vs = v_scale;
+          }
+        }
+      }
+    }
+  }
+  // every block has read the counter before it is counted here
+  __syncthreads();
+  if (threadIdx.x == 0 && last_block<false>(reinterpret_cast<int32_t *>(a.table) + 1) && !skip) *a.t = before + 1;
+}
+
+}  // namespace
+
+hipError_t launch_adamw_table(const aa_adamw_tensor *tensors, int32_t n, char *table, hipStream_t st) {
+  const int64_t map = (int64_t)table_map(n);
+  int64_t n_chunks = 0;
+  for (int32_t k = 0; k < n; ++k) n_chunks += (tensors[k].n + kChunk - 1) / kChunk;
+  int64_t chunk = 0;
+  for (int32_t first = 0; first < n; first += kBatch) {
+    EntryBatch batch = {};
+    const int here = n - first < kBatch ? n - first : kBatch;
+    for (int k = 0; k < here; ++k) {
+      const aa_adamw_tensor &t = tensors[first + k];
+      batch.e[k] = {t.param, t.grad,       t.copy,       t.m,          t.v,     t.m_scale, t.v_scale,
+                    t.n,     chunk,        t.grad_dtype, t.copy_dtype, t.state_bits, t.decay};
+      chunk += (t.n + kChunk - 1) / kChunk;
+    }
+    hipLaunchKernelGGL(k_adamw_table, dim3(here), dim3(256), 0, st, table, map, n_chunks, first, batch);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+hipError_t launch_grad_norm(const AdamWArgs &a, hipStream_t st) {
+  const int64_t blocks = a.n_chunks < 1 ? 1 : a.n_chunks < kNormBlocks ? a.n_chunks : kNormBlocks;
+  hipLaunchKernelGGL(k_grad_norm, dim3((uint32_t)blocks), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_adamw_step(const AdamWArgs &a, hipStream_t st) {
+  const int64_t most = kUnits * 8, blocks = a.n_chunks < 1 ? 1 : a.n_chunks < most ? a.n_chunks : most;
+  hipLaunchKernelGGL(k_adamw_step, dim3((uint32_t)blocks), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace aa

@@ -1,6 +1,7 @@
 // C ABI of the operators around a Boss block of experts: argument checks and the choice of kernels.
 #include "../../include/autoassist.h"
 
+#include "aa_adamw.hpp"
 #include "aa_checks.hpp"
 #include "aa_norm.hpp"
 #include "aa_route.hpp"
@@ -26,6 +27,25 @@ int32_t check_balance(const void *logits, int32_t dtype, int64_t ld, const int32
   if (type_bytes(dtype) == 0 || !isfinite(coef) || !isfinite(z_coef)) return AA_ERR_SHAPE;
   AA_TRY(check_rows(logits, n_max, ld, n_experts, type_bytes(dtype)));
   return check_words(count, false);
+}
+
+// One tensor of an update.
+int32_t check_tensor(const aa_adamw_tensor &t) {
+  if (t.n < 0 || t.n > (1ll << 35) || type_bytes(t.grad_dtype) == 0 || !isfinite(t.decay)) return AA_ERR_SHAPE;
+  if (t.state_bits != 32 && t.state_bits != 8) return AA_ERR_SHAPE;
+  if (t.copy && t.copy_dtype != AA_BF16 && t.copy_dtype != AA_F16) return AA_ERR_SHAPE;
+  if (t.n > 0 && (!t.param || !t.grad || !t.m || !t.v)) return AA_ERR_NULL;
+  if (t.n > 0 && t.state_bits == 8 && (!t.m_scale || !t.v_scale)) return AA_ERR_NULL;
+  const size_t state = t.state_bits / 8;
+  const bool fits = on(t.param, 4) && on(t.grad, type_bytes(t.grad_dtype)) && on(t.copy, 2) && on(t.m, state) &&
+                    on(t.v, state) && on(t.m_scale, 4) && on(t.v_scale, 4);
+  return fits ? AA_OK : AA_ERR_ALIGN;
+}
+
+// A table as aa_adamw_table made it.
+int32_t check_table(const void *table, size_t bytes, int32_t n_tensors, int64_t n_chunks) {
+  if (n_tensors < 1 || n_tensors > 65536 || n_chunks < 0 || n_chunks > kMaxPairs) return AA_ERR_SHAPE;
+  return check_ws(table, bytes, table_bytes(n_tensors, n_chunks));
 }
 
 }  // namespace
@@ -154,6 +174,72 @@ int32_t aa_balance_grad(const void *logits, int32_t dtype, int64_t ld, const int
   a.z_coef = z_coef;
   a.dloss = dloss;
   return hip_status(launch_balance_grad(a, as_stream(stream)));
+}
+
+int64_t aa_adamw_chunks(const aa_adamw_tensor *tensors, int32_t n_tensors) {
+  if (n_tensors < 1 || n_tensors > 65536) return AA_ERR_SHAPE;
+  if (!tensors) return AA_ERR_NULL;
+  int64_t chunks = 0;
+  for (int32_t k = 0; k < n_tensors; ++k) {
+    AA_TRY(check_tensor(tensors[k]));
+    chunks += (tensors[k].n + kChunk - 1) / kChunk;
+  }
+  return chunks <= kMaxPairs ? chunks : (int64_t)AA_ERR_SHAPE;
+}
+
+size_t aa_adamw_table_bytes(int32_t n_tensors, int64_t n_chunks) {
+  return table_bytes(n_tensors > 0 ? n_tensors : 1, n_chunks > 0 ? n_chunks : 0);
+}
+
+int32_t aa_adamw_table(const aa_adamw_tensor *tensors, int32_t n_tensors, void *table, size_t table_bytes_,
+                       void *stream) {
+  const int64_t chunks = aa_adamw_chunks(tensors, n_tensors);
+  if (chunks < 0) return (int32_t)chunks;
+  AA_TRY(check_table(table, table_bytes_, n_tensors, chunks));
+  return hip_status(launch_adamw_table(tensors, n_tensors, static_cast<char *>(table), as_stream(stream)));
+}
+
+int32_t aa_grad_norm(void *table, size_t table_bytes_, int32_t n_tensors, int64_t n_chunks, float max_norm,
+                     const float *scale, float *out, void *stream) {
+  AA_TRY(check_table(table, table_bytes_, n_tensors, n_chunks));
+  if (!(max_norm > 0.0f)) return AA_ERR_SHAPE;
+  AA_TRY(check_words(scale, false));
+  AA_TRY(check_words(out, true));
+  AdamWArgs a{};
+  a.table = static_cast<char *>(table);
+  a.map = (int64_t)table_map(n_tensors);
+  a.n_chunks = n_chunks;
+  a.max_norm = max_norm;
+  a.scale = scale;
+  a.out = out;
+  return hip_status(launch_grad_norm(a, as_stream(stream)));
+}
+
+int32_t aa_adamw_step(void *table, size_t table_bytes_, int32_t n_tensors, int64_t n_chunks,
+                      const aa_adamw_config *cfg, const float *lr_factor, const float *grad_factor,
+                      const int32_t *count, int32_t *t, void *stream) {
+  if (!cfg) return AA_ERR_NULL;
+  AA_TRY(check_table(table, table_bytes_, n_tensors, n_chunks));
+  const auto beta = [](float b) { return b >= 0.0f && b < 1.0f; };
+  const auto size = [](float v) { return v >= 0.0f && isfinite(v); };
+  if (!beta(cfg->beta1) || !beta(cfg->beta2) || !size(cfg->lr) || !size(cfg->weight_decay)) return AA_ERR_SHAPE;
+  if (!size(cfg->eps) || cfg->eps == 0.0f) return AA_ERR_SHAPE;
+  AA_TRY(check_words(lr_factor, false));
+  AA_TRY(check_words(grad_factor, false));
+  AA_TRY(check_words(count, false));
+  AA_TRY(check_words(t, true));
+  AdamWArgs a{};
+  a.table = static_cast<char *>(table);
+  a.map = (int64_t)table_map(n_tensors);
+  a.n_chunks = n_chunks;
+  a.cfg = *cfg;
+  a.log_beta1 = (float)log((double)cfg->beta1);
+  a.log_beta2 = (float)log((double)cfg->beta2);
+  a.lr_factor = lr_factor;
+  a.grad_factor = grad_factor;
+  a.count = count;
+  a.t = t;
+  return hip_status(launch_adamw_step(a, as_stream(stream)));
 }
 
 }  // extern "C"

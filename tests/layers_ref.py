@@ -151,3 +151,70 @@ def balance_grad(x, kind, counts, top_k, coef, z_coef, up=1.0):
     p, q, lse, rest = shares(x, kind)
     d = coef * E / (m * m * top_k) * p * rest * (counts - (p * counts).sum(1, keepdims=True))
     return up * (d + 2 * z_coef / m * lse[:, None] * q)
+
+
+# ---------------------------------------------------------------------------
+# AdamW
+
+BLOCK = 256
+
+
+def e4m3(codes):
+    """Values of bytes in the OCP format e4m3 (no infinities, NaN with all bits set)."""
+    c = codes.astype(np.int64)
+    e, f = (c >> 3) & 15, c & 7
+    v = np.where(e == 0, f * 2.0 ** -9, (8 + f) * 2.0 ** (e - 10.0))
+    v = np.where((c & 127) == 127, np.nan, v)
+    return np.where(c & 128, -v, v)
+
+
+def philox_words(c0, c1, c2, c3, seed):
+    """Philox4x32-10 (Salmon et al., SC'11) on arrays of counters."""
+    c = [np.asarray(v, np.uint64) + np.zeros_like(np.asarray(c0, np.uint64)) for v in (c0, c1, c2, c3)]
+    k0, k1, low = seed & 0xFFFFFFFF, seed >> 32, np.uint64(0xFFFFFFFF)
+    for _ in range(10):
+        p0, p1 = c[0] * np.uint64(0xD2511F53), c[2] * np.uint64(0xCD9E8D57)
+        c = [(p1 >> np.uint64(32)) ^ c[1] ^ np.uint64(k0), p1 & low, (p0 >> np.uint64(32)) ^ c[3] ^ np.uint64(k1), p0 & low]
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    return c
+
+
+def draws(n, tensor, t, seed):
+    """The 16-bit draws of elements 0 .. n - 1 of a tensor at update t."""
+    group = np.arange((n + 7) // 8)
+    words = philox_words(group, (1 << 31) + tensor, t & 0xFFFFFFFF, 0, seed)
+    halves = [h for w in words for h in (w & np.uint64(0xFFFF), w >> np.uint64(16))]
+    return np.stack(halves, 1).reshape(-1)[:n].astype(np.float64)
+
+
+def blocks(x):
+    """x in blocks of 256, zeros behind its end."""
+    return np.pad(x, (0, -len(x) % BLOCK)).reshape(-1, BLOCK)
+
+
+def scales(x):
+    most = np.where(np.isfinite(blocks(x)), np.abs(blocks(x)), 0.0).max(1)
+    _, e = np.frexp(most)
+    return np.where(most > 0, np.ldexp(1.0, np.maximum(e - 8, -126)), 0.0)
+
+
+def rounded(x, scale, draw, at_least_one):
+    """Values of the codes, and the place of a in steps (to tell how near a border it was)."""
+    s = np.repeat(scale, BLOCK)[:len(x)]
+    a = np.abs(x) / np.where(s > 0, s, 1.0)
+    _, e = np.frexp(a)
+    step = np.ldexp(1.0, np.maximum(e - 4, -9))
+    place = a / step + draw / 65536
+    q = np.floor(place)
+    if at_least_one:
+        q = np.where(a > 0, np.maximum(q, 1), q)
+    return np.sign(x) * q * step, step, place
+
+
+def adamw(p, g, m, v, t, cfg, decay, factor=1.0, lr_factor=1.0):
+    """p, m, v after update t (counted from 1); cfg: (lr, beta1, beta2, eps, weight_decay) as 32-bit values."""
+    lr, b1, b2, eps, wd = cfg
+    lr, g = lr * lr_factor, g * factor
+    m, v = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+    step = m / (1 - b1 ** t) / (np.sqrt(v / (1 - b2 ** t)) + eps)
+    return p * (1 - lr * wd * decay) - lr * step, m, v

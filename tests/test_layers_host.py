@@ -44,7 +44,59 @@ OF_BOTH = [(dict(logits=None), NULL), (dict(cfg=None), NULL), (dict(dtype=3), SH
            (dict(logits=P + 1), ALIGN), (dict(count=P + 2), ALIGN), (dict(ids=P + 2), ALIGN), (dict(ids=None), NULL),
            (dict(counts=None), NULL), (dict(counts=P + 2), ALIGN)]
 
+
+def tensors(*changes):
+    """A host array of good tensors with changes."""
+    out = (api.aa_adamw_tensor * len(changes))()
+    for t, change in zip(out, changes):
+        for k, v in dict(dict(param=P, grad=P, copy=None, m=P, v=P, m_scale=None, v_scale=None, n=5000, grad_dtype=BF16,
+                              copy_dtype=BF16, state_bits=32, decay=1.0), **change).items():
+            setattr(t, k, v)
+    return out
+
+
+def opt(**change):
+    c = api.adamw_config(1e-3)
+    for k, v in change.items():
+        setattr(c, k, v)
+    return c
+
+
+GOOD = tensors({}, {})
+ONE_BAD = lambda **change: tensors({}, change)
+CHUNKS = dict(tensors=GOOD, n_tensors=2)
+TABLE = dict(tensors=GOOD, n_tensors=2, table=P, table_bytes=BIG, stream=None)
+OF_LIST = [
+    (dict(tensors=None), NULL), (dict(n_tensors=0), SHAPE), (dict(n_tensors=-1), SHAPE), (dict(n_tensors=65537), SHAPE),
+    (dict(tensors=ONE_BAD(n=-1)), SHAPE), (dict(tensors=ONE_BAD(n=(1 << 35) + 1)), SHAPE),
+    (dict(tensors=ONE_BAD(grad_dtype=3)), SHAPE), (dict(tensors=ONE_BAD(copy=P, copy_dtype=F32)), SHAPE),
+    (dict(tensors=ONE_BAD(state_bits=16)), SHAPE), (dict(tensors=ONE_BAD(decay=NAN)), SHAPE),
+    (dict(tensors=ONE_BAD(param=None)), NULL), (dict(tensors=ONE_BAD(grad=None)), NULL), (dict(tensors=ONE_BAD(m=None)), NULL),
+    (dict(tensors=ONE_BAD(v=None)), NULL), (dict(tensors=ONE_BAD(state_bits=8)), NULL),
+    (dict(tensors=ONE_BAD(state_bits=8, m_scale=P)), NULL), (dict(tensors=ONE_BAD(param=P + 2)), ALIGN),
+    (dict(tensors=ONE_BAD(grad=P + 1)), ALIGN), (dict(tensors=ONE_BAD(grad=P + 2, grad_dtype=F32)), ALIGN),
+    (dict(tensors=ONE_BAD(copy=P + 1)), ALIGN), (dict(tensors=ONE_BAD(m=P + 1)), ALIGN), (dict(tensors=ONE_BAD(v=P + 2)), ALIGN),
+    (dict(tensors=ONE_BAD(state_bits=8, m_scale=P + 2, v_scale=P)), ALIGN)]
+GRAD_NORM = dict(table=P, table_bytes=BIG, n_tensors=2, n_chunks=6, max_norm=1.0, scale=None, out=P, stream=None)
+STEP = dict(table=P, table_bytes=BIG, n_tensors=2, n_chunks=6, cfg=opt(), lr_factor=None, grad_factor=None, count=None,
+            t=P, stream=None)
+OF_TABLE = [(dict(table=None), WORKSPACE), (dict(table=P + 128), WORKSPACE), (dict(table_bytes=8192), WORKSPACE),
+            (dict(n_tensors=0), SHAPE), (dict(n_tensors=65537), SHAPE), (dict(n_chunks=-1), SHAPE),
+            (dict(n_chunks=1 << 31), SHAPE)]
+
 REFUSED = [
+    ("aa_adamw_chunks", CHUNKS, OF_LIST),
+    ("aa_adamw_table", TABLE, OF_LIST + [(dict(table=None), WORKSPACE), (dict(table=P + 64), WORKSPACE),
+                                         (dict(table_bytes=8192), WORKSPACE)]),
+    ("aa_grad_norm", GRAD_NORM, OF_TABLE + [
+        (dict(max_norm=0.0), SHAPE), (dict(max_norm=-1.0), SHAPE), (dict(max_norm=NAN), SHAPE), (dict(out=None), NULL),
+        (dict(out=P + 2), ALIGN), (dict(scale=P + 1), ALIGN)]),
+    ("aa_adamw_step", STEP, OF_TABLE + [
+        (dict(cfg=None), NULL), (dict(cfg=opt(beta1=1.0)), SHAPE), (dict(cfg=opt(beta1=-0.1)), SHAPE),
+        (dict(cfg=opt(beta2=NAN)), SHAPE), (dict(cfg=opt(eps=0.0)), SHAPE), (dict(cfg=opt(eps=INF)), SHAPE),
+        (dict(cfg=opt(lr=-1.0)), SHAPE), (dict(cfg=opt(lr=INF)), SHAPE), (dict(cfg=opt(weight_decay=-1.0)), SHAPE),
+        (dict(t=None), NULL), (dict(t=P + 2), ALIGN), (dict(lr_factor=P + 2), ALIGN), (dict(grad_factor=P + 2), ALIGN),
+        (dict(count=P + 2), ALIGN)]),
     ("aa_balance", BALANCE, OF_BOTH + [
         (dict(share=P + 2), ALIGN), (dict(loss=P + 2), ALIGN), (dict(ws=None), WORKSPACE), (dict(ws_bytes=4096), WORKSPACE),
         (dict(ws=P + 64), WORKSPACE)]),
@@ -91,3 +143,11 @@ def test_python_refusals():
         api.layer_norm(t, None, None, 1e-5, None, t)
     with pytest.raises(api.AAError):
         api.layer_norm_grad(t, t, None, None, None, None, None, t, None, None, False, None)
+
+
+def test_chunks_of_tensors(L):
+    n = lambda *sizes: L.aa_adamw_chunks(tensors(*(dict(n=k) for k in sizes)), len(sizes))
+    assert n(0) == 0 and n(1) == 1 and n(2048) == 1 and n(2049, 0, 5) == 3 and n(1 << 35) == 1 << 24
+    assert L.aa_adamw_table_bytes(3, 100) % 256 == 0 and L.aa_adamw_table_bytes(3, 100) < L.aa_adamw_table_bytes(300, 10_000)
+    # a tensor without elements needs no memory
+    assert L.aa_adamw_chunks(tensors(dict(n=0, param=None, grad=None, m=None, v=None)), 1) == 0
