@@ -392,6 +392,8 @@ int32_t aa_train_epoch_stale(const aa_features *F, const float *y, const int32_t
 #define AA_ACT_NONE 0
 #define AA_ACT_RELU 1
 #define AA_ACT_GATED 2 /* silu(gate) * up */
+#define AA_ACT_SILU 3  /* h sigmoid(h); aa_linear and its gradient only */
+#define AA_ACT_GELU 4  /* h sigmoid(2 sqrt(2 / pi) (h + 0.044715 h^3)); aa_linear and its gradient only */
 
 #define AA_MAX_EXPERTS 1024
 #define AA_MAX_CHOICES 64
@@ -528,6 +530,25 @@ int32_t aa_layer_norm_grad(const void *dout, int32_t dtype, int64_t lddo, const 
                            const int32_t *count, int32_t n_max, int32_t d, const float *gamma, const float *mean,
                            const float *rstd, const void *residual, int64_t ldr, void *dx, int64_t lddx,
                            float *dgamma, float *dbeta, int32_t accumulate, void *ws, size_t ws_bytes, void *stream);
+
+/* Dense layer (dtype AA_BF16 or AA_F16, sums in fp32): for the rows in use
+ *   h = w x[t] + bias,   out[t] = residual[t] + act(h)
+ * with w [d_out][d_in] and bias [d_out], with AA_ACT_GATED [2 d_out][d_in] and [2 d_out] (gate rows, then up rows),
+ * contiguous.  bias, residual: NULL for none.  pre (NULL: not written) receives h, [n_max][d_out] or
+ * [n_max][2 d_out], for the backward pass.  act: any AA_ACT_*.  out may be residual, but neither x nor pre. */
+int32_t aa_linear(const void *x, int32_t dtype, int64_t ldx, const int32_t *count, int32_t n_max, int32_t d_in,
+                  int32_t d_out, const void *w, const float *bias, int32_t act, const void *residual, int64_t ldr,
+                  void *out, int64_t ldo, void *pre, int64_t ldpre, void *stream);
+
+/* Its gradient as far as h: dpre[t] = dout[t] act'(pre[t]) (AA_ACT_GATED: the gate's, then up's, 2 d_out wide), and
+ * dbias = the sum of dpre over the rows in use, before it is rounded (accumulate != 0 adds to what dbias
+ * holds; no rows: zeros, or nothing).  dpre or dbias may be NULL, not both; pre is not read with AA_ACT_NONE.
+ * dpre may be pre, and but for AA_ACT_GATED dout.  ws is needed where dbias is (d_max: dbias' columns).  The
+ * gradients of x and w are those of a block of one expert: aa_expert_grad_input and aa_expert_grad_weight of dpre
+ * with offsets {0, m}; that of residual is dout. */
+int32_t aa_linear_grad(const void *dout, int32_t dtype, int64_t lddo, const int32_t *count, int32_t n_max,
+                       int32_t d_out, int32_t act, const void *pre, int64_t ldpre, void *dpre, int64_t lddp,
+                       float *dbias, int32_t accumulate, void *ws, size_t ws_bytes, void *stream);
 
 /* Balance of a router: with the ids that aa_route wrote, c_e the choices of expert e among the m top_k of the rows
  * in use, and p_te = s_te / sum_e s_te the share that expert e has of row t's scores (cfg->score as in aa_route; 0 for

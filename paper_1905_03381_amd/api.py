@@ -19,6 +19,7 @@ AA_DENSE, AA_CSR = 0, 1
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}   # AA_F32, AA_BF16, AA_F16
 SCORES = {"softmax": 0, "sigmoid": 1}
 ACTIVATIONS = {"none": 0, "relu": 1, "gated": 2}
+DENSE_ACTIVATIONS = dict(ACTIVATIONS, silu=3, gelu=4)   # of linear and linear_grad
 
 SYMBOLS = [
     "aa_version", "aa_status_string", "aa_workspace_bytes", "aa_workspace_init", "aa_profile_hook",
@@ -32,7 +33,7 @@ SYMBOLS = [
     "aa_expert_workspace_bytes", "aa_route", "aa_route_grad", "aa_expert_plan", "aa_expert_forward",
     "aa_expert_grad_input", "aa_expert_grad_weight", "aa_expert_combine", "aa_expert_combine_grad",
     "aa_dropout",
-    "aa_layer_workspace_bytes", "aa_layer_norm", "aa_layer_norm_grad", "aa_balance", "aa_balance_grad",
+    "aa_layer_workspace_bytes", "aa_layer_norm", "aa_layer_norm_grad", "aa_linear", "aa_linear_grad", "aa_balance", "aa_balance_grad",
     "aa_adamw_chunks", "aa_adamw_table_bytes", "aa_adamw_table", "aa_grad_norm", "aa_adamw_step",
 ]
 
@@ -128,6 +129,8 @@ def lib():
         "aa_layer_norm": (i32, [vp, i32, i64, vp, i32, i32, vp, vp, f32, vp, i64, vp, vp, vp]),
         "aa_layer_norm_grad": (i32, [vp, i32, i64, vp, i64, vp, i32, i32, vp, vp, vp, vp, i64, vp, i64, vp, vp, i32,
                                      vp, sz, vp]),
+        "aa_linear": (i32, [vp, i32, i64, vp, i32, i32, i32, vp, vp, i32, vp, i64, vp, i64, vp, i64, vp]),
+        "aa_linear_grad": (i32, [vp, i32, i64, vp, i32, i32, i32, vp, i64, vp, i64, vp, i32, vp, sz, vp]),
         "aa_balance": (i32, [vp, i32, i64, vp, i32, i32, RP, vp, f32, f32, vp, vp, vp, vp, sz, vp]),
         "aa_balance_grad": (i32, [vp, i32, i64, vp, i32, i32, RP, vp, vp, vp, f32, f32, vp, vp, i64, vp]),
         "aa_adamw_chunks": (i64, [TP, i32]),
@@ -643,6 +646,38 @@ def layer_norm_grad(dout, x, gamma, mean, rstd, residual, count, dx, dgamma, dbe
                                     _array(dgamma, "dgamma", torch.float32, (d,)),
                                     _array(dbeta, "dbeta", torch.float32, (d,)), int(bool(accumulate)), *scratch,
                                     _stream()), "aa_layer_norm_grad")
+
+
+def linear(x, w, bias, act, residual, count, out, pre=None):
+    """w [d_out, d_in] (gated: [2 d_out, d_in]) and bias (float32, or None) for all rows; pre: what the activation is taken
+    of, for the backward pass."""
+    dt, a = _type(x, "x", True), _name_of(DENSE_ACTIVATIONS, act, "act")
+    xp, ldx = _matrix(x, "x")
+    n, d_in = x.shape
+    _require(isinstance(w, torch.Tensor) and w.dim() == 2 and w.shape[1] == d_in, "w: [rows, d_in]")
+    wide, dtype = w.shape[0], x.dtype
+    _require(a != 2 or wide % 2 == 0, "w: [rows, d_in]")
+    d_out = wide // 2 if a == 2 else wide
+    op, ldo = _matrix(out, "out", dtype, d_out, n)
+    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", dtype, d_out, n)
+    pp, ldp = (None, 0) if pre is None else _matrix(pre, "pre", dtype, wide, n)
+    _check(lib().aa_linear(xp, dt, ldx, _count(count), n, d_in, d_out, _array(w, "w", dtype),
+                           _array(bias, "bias", torch.float32, (wide,)), a, rp, ldr, op, ldo, pp, ldp, _stream()),
+           "aa_linear")
+
+
+def linear_grad(dout, act, pre, count, dpre, dbias, accumulate, ws):
+    """pre: not needed without an activation; dpre or dbias may be None, and ws where dbias is."""
+    dt, a = _type(dout, "dout", True), _name_of(DENSE_ACTIVATIONS, act, "act")
+    gp, ldg = _matrix(dout, "dout")
+    (n, d), dtype = dout.shape, dout.dtype
+    wide = 2 * d if a == 2 else d
+    pp, ldp = (None, 0) if a == 0 else _matrix(pre, "pre", dtype, wide, n)
+    op, ldo = (None, 0) if dpre is None else _matrix(dpre, "dpre", dtype, wide, n)
+    scratch = (None, 0) if dbias is None else _scratch(ws, "a LayerWorkspace")
+    _check(lib().aa_linear_grad(gp, dt, ldg, _count(count), n, d, a, pp, ldp, op, ldo,
+                                _array(dbias, "dbias", torch.float32, (wide,)), int(bool(accumulate)), *scratch,
+                                _stream()), "aa_linear_grad")
 
 
 def balance(logits, count, cfg, ids, coef, z_coef, counts, share, loss, ws):

@@ -12,17 +12,6 @@ using namespace aa;
 
 namespace {
 
-// Rows of `width` elements can be moved 16 bytes at a time, but for a shorter end.
-bool rows_on_16(const void *p, int64_t ld, int bytes) { return on(p, 16) && ld * bytes % 16 == 0; }
-
-// What the kernels that move 16 bytes at a time address with 32 bits a lane: rows by their place in units of 16
-// bytes (gathered ones, of which there may be more than rows_max, by 64 bits); rows that run along the result by their place
-// among 31.
-bool in_reach(const void *p, int64_t rows, int64_t ld) {
-  return rows_on_16(p, ld, 2) && (rows == 0 || ld / 8 < (1ll << 32) / rows);
-}
-bool columns_in_reach(const void *p, int64_t ld) { return rows_on_16(p, ld, 2) && ld < (1ll << 25); }
-
 size_t plan_bytes(int64_t n_max, int32_t top_k, int32_t n_experts) {
   return align_up(plan_table_ints(n_max, top_k, n_experts) * sizeof(int32_t), 256);
 }

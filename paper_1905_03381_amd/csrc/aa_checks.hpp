@@ -38,6 +38,17 @@ inline int32_t check_words(const void *p, bool needed) {
     if (rc_ != AA_OK) return rc_;       \
   } while (0)
 
+// Rows of `width` elements can be moved 16 bytes at a time, but for a shorter end.
+inline bool rows_on_16(const void *p, int64_t ld, int bytes) { return on(p, 16) && ld * bytes % 16 == 0; }
+
+// What the kernels that move 16 bytes at a time address with 32 bits a lane: rows by their place in units of 16
+// bytes (gathered ones, of which there may be more than rows_max, by 64 bits); rows that run along the result by their place
+// among 31.
+inline bool in_reach(const void *p, int64_t rows, int64_t ld) {
+  return rows_on_16(p, ld, 2) && (rows == 0 || ld / 8 < (1ll << 32) / rows);
+}
+inline bool columns_in_reach(const void *p, int64_t ld) { return rows_on_16(p, ld, 2) && ld < (1ll << 25); }
+
 inline int32_t check_ws(const void *ws, size_t ws_bytes, size_t need) {
   return !ws || !on(ws, 256) || ws_bytes < need ? AA_ERR_WORKSPACE : AA_OK;
 }

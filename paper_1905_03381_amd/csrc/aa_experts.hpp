@@ -26,6 +26,11 @@ struct ProductArgs {
   float *partial;   // grad_weight: room for the parts of a split sum
   size_t partial_bytes;
   int32_t parts;    // (chosen at launch) parts a tile's sum over rows comes in
+  // dense layer: one group, rows [0, m) by count; the rows' bias and residual (NULL: none)
+  const int32_t *count;
+  const float *bias;
+  const void *residual;
+  int64_t ldres;
 };
 
 hipError_t launch_expert_forward(const ProductArgs &a, bool f16, hipStream_t st);

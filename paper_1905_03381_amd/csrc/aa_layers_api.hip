@@ -3,6 +3,7 @@
 
 #include "aa_adamw.hpp"
 #include "aa_checks.hpp"
+#include "aa_linear.hpp"
 #include "aa_norm.hpp"
 #include "aa_route.hpp"
 
@@ -17,6 +18,15 @@ float *body(void *ws) { return reinterpret_cast<float *>(static_cast<char *>(ws)
 // Rows that a layer norm reads or writes.
 int32_t check_norm(int32_t dtype, int32_t n_max, int32_t d, const int32_t *count) {
   if (type_bytes(dtype) == 0 || n_max < 0 || d < 1 || d > kMaxWidth) return AA_ERR_SHAPE;
+  return check_words(count, false);
+}
+
+bool is_dense_act(int32_t act) { return act >= AA_ACT_NONE && act <= AA_ACT_GELU; }
+
+// Rows of a dense layer.
+int32_t check_linear(int32_t dtype, const int32_t *count, int32_t n_max, int32_t d_out, int32_t act) {
+  if (dtype != AA_BF16 && dtype != AA_F16) return AA_ERR_SHAPE;
+  if (n_max < 0 || n_max > kMaxPairs || d_out < 1 || d_out > kMaxWidth || !is_dense_act(act)) return AA_ERR_SHAPE;
   return check_words(count, false);
 }
 
@@ -117,6 +127,68 @@ int32_t aa_layer_norm_grad(const void *dout, int32_t dtype, int64_t lddo, const 
   a.accumulate = accumulate != 0;
   a.part = dgamma || dbeta ? body(ws) : nullptr;
   return hip_status(launch_layer_norm_grad(a, dtype, as_stream(stream)));
+}
+
+int32_t aa_linear(const void *x, int32_t dtype, int64_t ldx, const int32_t *count, int32_t n_max, int32_t d_in,
+                  int32_t d_out, const void *w, const float *bias, int32_t act, const void *residual, int64_t ldr,
+                  void *out, int64_t ldo, void *pre, int64_t ldpre, void *stream) {
+  AA_TRY(check_linear(dtype, count, n_max, d_out, act));
+  if (d_in < 1 || d_in > kMaxWidth) return AA_ERR_SHAPE;
+  const int64_t wide = act == AA_ACT_GATED ? 2 * (int64_t)d_out : d_out;
+  AA_TRY(check_rows(x, n_max, ldx, d_in, 2));
+  AA_TRY(check_rows(out, n_max, ldo, d_out, 2));
+  if (residual) AA_TRY(check_rows(residual, n_max, ldr, d_out, 2));
+  if (pre) AA_TRY(check_rows(pre, n_max, ldpre, wide, 2));
+  AA_TRY(check_rows(w, 1, d_in, d_in, 2));
+  AA_TRY(check_words(bias, false));
+  ProductArgs a{};
+  a.rows = x;
+  a.ld_rows = ldx;
+  a.mat = w;
+  a.top_k = 1;
+  a.rows_max = n_max;
+  a.n_experts = 1;
+  a.d_in = d_in;
+  a.d_out = d_out;
+  a.out = out;
+  a.ldo = ldo;
+  a.pre = pre;
+  a.ldpre = ldpre;
+  a.act = act;
+  a.aligned = d_in % 8 == 0 && in_reach(x, n_max, ldx) && in_reach(w, wide, d_in);
+  a.count = count;
+  a.bias = bias;
+  a.residual = residual;
+  a.ldres = ldr;
+  return hip_status(launch_linear(a, dtype == AA_F16, as_stream(stream)));
+}
+
+int32_t aa_linear_grad(const void *dout, int32_t dtype, int64_t lddo, const int32_t *count, int32_t n_max,
+                       int32_t d_out, int32_t act, const void *pre, int64_t ldpre, void *dpre, int64_t lddp,
+                       float *dbias, int32_t accumulate, void *ws, size_t ws_bytes, void *stream) {
+  AA_TRY(check_linear(dtype, count, n_max, d_out, act));
+  if (!dpre && !dbias) return AA_ERR_NULL;
+  const int64_t wide = act == AA_ACT_GATED ? 2 * (int64_t)d_out : d_out;
+  AA_TRY(check_rows(dout, n_max, lddo, d_out, 2));
+  if (act != AA_ACT_NONE) AA_TRY(check_rows(pre, n_max, ldpre, wide, 2));
+  if (dpre) AA_TRY(check_rows(dpre, n_max, lddp, wide, 2));
+  AA_TRY(check_words(dbias, false));
+  if (dbias) AA_TRY(check_ws(ws, ws_bytes, layer_bytes(wide)));
+  ActGradArgs a{};
+  a.dout = dout;
+  a.lddo = lddo;
+  a.count = count;
+  a.n_max = n_max;
+  a.d = d_out;
+  a.act = act;
+  a.pre = pre;
+  a.ldpre = ldpre;
+  a.dpre = dpre;
+  a.lddp = lddp;
+  a.dbias = dbias;
+  a.accumulate = accumulate != 0;
+  a.part = dbias ? body(ws) : nullptr;
+  return hip_status(launch_linear_grad(a, dtype == AA_F16, as_stream(stream)));
 }
 
 int32_t aa_balance(const void *logits, int32_t dtype, int64_t ld, const int32_t *count, int32_t n_max,

@@ -391,12 +391,12 @@ __global__ __launch_bounds__(256) void k_layer_norm_columns(const NormArgs a, in
   store8(a.part + (int64_t)part * 2 * d + d + c, db, d - c);
 }
 
-// first[c], second[c] (+)= the sum over the parts of part[.][0][c], part[.][1][c]: 64 columns a block, 16 shares of
-// the parts, joined in their order.
+// first[c], second[c] (+)= the sum over the parts (`stride` apart) of their columns c and d + c: 64 columns a block, 16
+// shares of the parts, joined in their order.
 constexpr int kJoinShares = 16;
 
-__global__ __launch_bounds__(kJoinShares *kWave) void k_join_columns(const float *part, int parts, int d, float *first,
-                                                                      float *second, int accumulate) {
+__global__ __launch_bounds__(kJoinShares *kWave) void k_join_columns(const float *part, int parts, int64_t stride, int d,
+                                                                      float *first, float *second, int accumulate) {
   __shared__ float sums[kJoinShares][kWave];
   float *out = blockIdx.y == 0 ? first : second;
   if (!out) return;
@@ -406,7 +406,7 @@ __global__ __launch_bounds__(kJoinShares *kWave) void k_join_columns(const float
   const int each = (parts + kJoinShares - 1) / kJoinShares, from = min(share * each, parts), to = min(from + each, parts);
   float sum = 0.f;
 #pragma unroll 8
-  for (int i = from; i < to; ++i) sum += p[(int64_t)i * 2 * d];
+  for (int i = from; i < to; ++i) sum += p[i * stride];
   sums[share][lane] = sum;
   __syncthreads();
   if (share > 0 || c >= d) return;
@@ -418,11 +418,7 @@ __global__ __launch_bounds__(kJoinShares *kWave) void k_join_columns(const float
 }
 
 hipError_t join_columns(const NormArgs &a, int parts, hipStream_t st) {
-  if (!a.dgamma && !a.dbeta) return hipSuccess;
-  const dim3 grid((uint32_t)(((int64_t)a.d + kWave - 1) / kWave), 2);
-  hipLaunchKernelGGL(k_join_columns, grid, dim3(kJoinShares * kWave), 0, st, a.part, parts, a.d, a.dgamma, a.dbeta,
-                     a.accumulate);
-  return hipGetLastError();
+  return launch_join_columns(a.part, parts, 2 * (int64_t)a.d, a.d, a.dgamma, a.dbeta, a.accumulate, st);
 }
 
 // Threads of a row and lines of eight columns each of them holds.
@@ -493,13 +489,21 @@ __global__ void k_clear_columns(float *first, float *second, int d) {
   if (second) second[c] = 0.f;
 }
 
-hipError_t clear_columns(float *first, float *second, int32_t d, bool accumulate, hipStream_t st) {
-  if (accumulate || (!first && !second)) return hipSuccess;
+}  // namespace
+
+hipError_t launch_clear_columns(float *first, float *second, int32_t d, hipStream_t st) {
+  if (!first && !second) return hipSuccess;
   hipLaunchKernelGGL(k_clear_columns, dim3((uint32_t)(((int64_t)d + 255) / 256)), dim3(256), 0, st, first, second, d);
   return hipGetLastError();
 }
 
-}  // namespace
+hipError_t launch_join_columns(const float *part, int parts, int64_t stride, int32_t d, float *first, float *second,
+                               int32_t accumulate, hipStream_t st) {
+  if (!first && !second) return hipSuccess;
+  const dim3 grid((uint32_t)(((int64_t)d + kWave - 1) / kWave), 2);
+  hipLaunchKernelGGL(k_join_columns, grid, dim3(kJoinShares * kWave), 0, st, part, parts, stride, d, first, second, accumulate);
+  return hipGetLastError();
+}
 
 hipError_t launch_layer_norm(const NormArgs &a, int32_t dtype, hipStream_t st) {
   if (a.n_max == 0) return hipSuccess;
@@ -511,7 +515,7 @@ hipError_t launch_layer_norm(const NormArgs &a, int32_t dtype, hipStream_t st) {
 }
 
 hipError_t launch_layer_norm_grad(const NormArgs &a, int32_t dtype, hipStream_t st) {
-  if (a.n_max == 0) return clear_columns(a.dgamma, a.dbeta, a.d, a.accumulate != 0, st);
+  if (a.n_max == 0) return a.accumulate ? hipSuccess : launch_clear_columns(a.dgamma, a.dbeta, a.d, st);
   switch (dtype) {
     case AA_BF16: return layer_norm_grad<__bf16>(a, st);
     case AA_F16: return layer_norm_grad<_Float16>(a, st);

@@ -37,6 +37,12 @@ inline size_t layer_bytes(int64_t d) {
   return kLayerHead + (parts > 16384 ? parts : 16384);
 }
 
+// first[c], second[c] (+)= the sum over the parts, `stride` floats apart, of their columns c and d + c (either may be NULL);
+// zeros.
+hipError_t launch_join_columns(const float *part, int parts, int64_t stride, int32_t d, float *first, float *second,
+                               int32_t accumulate, hipStream_t st);
+hipError_t launch_clear_columns(float *first, float *second, int32_t d, hipStream_t st);
+
 hipError_t launch_layer_norm(const NormArgs &a, int32_t dtype, hipStream_t st);
 hipError_t launch_layer_norm_grad(const NormArgs &a, int32_t dtype, hipStream_t st);
 

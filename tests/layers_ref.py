@@ -218,3 +218,79 @@ def adamw(p, g, m, v, t, cfg, decay, factor=1.0, lr_factor=1.0):
     m, v = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
     step = m / (1 - b1 ** t) / (np.sqrt(v / (1 - b2 ** t)) + eps)
     return p * (1 - lr * wd * decay) - lr * step, m, v
+
+
+# ---------------------------------------------------------------------------
+# dense layer
+
+ACTS = ["none", "relu", "silu", "gelu", "gated"]
+GELU = 2 * np.sqrt(2 / np.pi)
+
+
+def sigmoid(x):
+    with np.errstate(over="ignore"):
+        return 1 / (1 + np.exp(-x))
+
+
+def activate(h, act):
+    """The activation, and how far it is off for h exact, in units of U: |value| (2 |argument| (1 - z) + 8) for those with an
+    exponential of the argument."""
+    if act == "none":
+        return h, 0 * h
+    if act == "relu":
+        return np.where(h < 0, 0.0, h), 0 * h
+    gate, up = (h, 1.0) if act != "gated" else (h[:, :h.shape[1] // 2], h[:, h.shape[1] // 2:])
+    arg = GELU * (gate + 0.044715 * gate ** 3) if act == "gelu" else gate
+    z = sigmoid(arg)
+    out = gate * z * up
+    return out, np.abs(out) * (4 * np.abs(arg) * (1 - z) + 8)
+
+
+def slopes(h, act):
+    """(d out / d h, d out / d up) and the size of the terms the first is a sum of."""
+    if act == "none":
+        return np.ones_like(h), None, np.ones_like(h)
+    if act == "relu":
+        return (h > 0).astype(np.float64), None, (h > 0).astype(np.float64)
+    gate, up = (h, 1.0) if act != "gated" else (h[:, :h.shape[1] // 2], h[:, h.shape[1] // 2:])
+    arg = GELU * (gate + 0.044715 * gate ** 3) if act == "gelu" else gate
+    inner = GELU * (1 + 3 * 0.044715 * gate ** 2) if act == "gelu" else 1.0
+    z = sigmoid(arg)
+    first, second = z, gate * z * (1 - z) * inner
+    return (first + second) * up, gate * z if act == "gated" else None, (np.abs(first) + np.abs(second)) * np.abs(up)
+
+
+def linear(x, w, bias, act, residual):
+    h = x @ w.T + bias
+    return activate(h, act)[0] + residual, h
+
+
+def linear_bounds(x, w, bias, act, residual, dtype):
+    """A sum of d_in products and the bias in 32 bits is off by (d_in + 3) U of its terms' magnitudes; the activations' slopes
+    are at most 1.13."""
+    h = x @ w.T + bias
+    of_h = (x.shape[1] + 3) * U32 * (np.abs(x) @ np.abs(w).T + np.abs(bias))
+    out, rel = activate(h, act)
+    if act == "gated":
+        f = out.shape[1]
+        gate = np.abs(h[:, :f]) * sigmoid(h[:, :f])
+        b = 1.13 * of_h[:, :f] * (np.abs(h[:, f:]) + of_h[:, f:]) + of_h[:, f:] * gate
+    else:
+        b = 1.13 * of_h
+    b = b + rel * U32 + 2 * U32 * np.abs(residual)
+    out = out + residual
+    return b + half_step(dtype) * (np.abs(out) + b) + tiny(dtype), of_h + half_step(dtype) * (np.abs(h) + of_h) + tiny(dtype)
+
+
+def linear_grad(dout, h, act):
+    """dpre, its error, dbias, its error's terms (sum of magnitudes)."""
+    s, u, size = slopes(h, act)
+    d = dout * s
+    with np.errstate(over="ignore"):
+        arg = np.abs(h if act != "gated" else h[:, :h.shape[1] // 2])
+    # (beyond 20 the slopes are 0 or 1)
+    off = np.abs(dout) * size * (4 * np.minimum(1.6 * arg * (1 + 0.045 * arg ** 2), 120) + 16) * U32
+    off = off * (act not in ("none", "relu"))
+    if act == "gated":
+        d, off = np.concatenate([d, dout * u], 1), np.concatenate([off, np.abs(dout * u) * (4 * np.minimum(arg, 120) + 16) * U32], 1)
+    return d, off

@@ -1,0 +1,262 @@
+"""The dense layer and the gradient through its epilogue on the GPU against the references in 64 bits (layers_ref.py, with
+the tolerances)."""
+import numpy as np
+import pytest
+import torch
+
+import layers_ref as R
+from layers_ref import ACTS, BF16, F16, F32, HALVES, U32, check, device_count, f64, half_step, in_use, normal, strided, tiny
+from paper_1905_03381_amd import api
+
+pytestmark = pytest.mark.gpu
+
+
+class Layer:
+    def __init__(self, n, d_in, d_out, act, dtype, bias=True, residual=False, seed=0, spread=0, count=None):
+        self.act, self.count, self.wide = act, count, d_out * (2 if act == "gated" else 1)
+        self.x = strided(normal((n, d_in), dtype, seed + 1), d_in + spread, spread // 2)
+        self.w = normal((self.wide, d_in), dtype, seed + 2, d_in ** -0.5).cuda()
+        self.bias = normal((self.wide,), F32, seed + 3).cuda() if bias else None
+        self.residual = strided(normal((n, d_out), dtype, seed + 4), d_out + spread, spread // 3) if residual else None
+        self.d_out = d_out
+
+    def run(self, pre=True, out=None):
+        n, dt = self.x.shape[0], self.x.dtype
+        out = torch.full((n, self.d_out), 77.0, dtype=dt, device="cuda") if out is None else out
+        pre = torch.full((n, self.wide), 77.0, dtype=dt, device="cuda") if pre else None
+        api.linear(self.x, self.w, self.bias, self.act, self.residual, device_count(self.count), out, pre)
+        return out, pre
+
+    def check(self, out, pre, residual=None):
+        m, dt = in_use(self.count, self.x.shape[0]), self.x.dtype
+        residual = self.residual if residual is None else residual
+        args = (f64(self.x)[:m], f64(self.w), 0.0 if self.bias is None else f64(self.bias), self.act,
+                0.0 if residual is None else f64(residual)[:m])
+        want, bounds = R.linear(*args), R.linear_bounds(*args, dt)
+        check(out[:m], want[0], bounds[0], "out")
+        assert (f64(out[m:]) == 77.0).all()
+        if pre is not None:
+            check(pre[:m], want[1], bounds[1], "pre")
+            assert (f64(pre[m:]) == 77.0).all()
+
+
+# A few rows (16 and 32 at a time), tiles of 32 x 64, 128 x 128 and 256 x 256, and operands that are moved through registers.
+SIZES = [(1, 64, 48), (1, 2048, 520), (5, 8, 8), (16, 136, 40), (17, 1000, 333), (32, 512, 1024), (33, 64, 64),
+         (100, 256, 520), (300, 512, 264), (700, 320, 1000), (1100, 200, 2900), (4100, 128, 2568), (60, 7, 30),
+         (129, 65, 129), (500, 100, 77), (40, 1, 1), (3, 3, 5), (1, 1, 1), (2, 4095, 17), (130, 513, 256)]
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("n,d_in,d_out", SIZES)
+def test_sizes(n, d_in, d_out, act):
+    for i, dtype in enumerate(HALVES):
+        layer = Layer(n, d_in, d_out, act, dtype, bias=True, residual=i == 0, seed=n + d_in)
+        layer.check(*layer.run(pre=i == 1))
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("pre", [False, True])
+def test_what_is_left_out(act, bias, residual, pre):
+    for n, d_in, d_out in ((4, 96, 70), (200, 128, 136)):
+        layer = Layer(n, d_in, d_out, act, BF16, bias, residual)
+        layer.check(*layer.run(pre))
+
+
+@pytest.mark.parametrize("spread", [1, 3, 8, 24])
+@pytest.mark.parametrize("n", [7, 150])
+@pytest.mark.parametrize("act", ["gelu", "gated"])
+def test_strides_and_places(n, spread, act):
+    layer = Layer(n, 104, 88, act, F16, residual=True, spread=spread)
+    out = strided(torch.full((n, 88), 77.0, dtype=F16), 88 + spread, spread // 2)
+    pre = strided(torch.full((n, layer.wide), 77.0, dtype=F16), layer.wide + spread, 1)
+    api.linear(layer.x, layer.w, layer.bias, act, layer.residual, None, out, pre)
+    layer.check(out, pre)
+
+
+@pytest.mark.parametrize("n,count", [(5, 0), (5, -3), (5, 9), (300, 0), (300, 1), (300, 129), (3000, 2500), (0, None)])
+@pytest.mark.parametrize("act", ["none", "gated"])
+def test_rows_in_use(n, count, act):
+    layer = Layer(n, 128, 192, act, BF16, residual=True, count=count)
+    layer.check(*layer.run())
+
+
+@pytest.mark.parametrize("n", [8, 400])
+def test_residual_in_place(n):
+    layer = Layer(n, 128, 192, "silu", BF16, residual=True)
+    kept = layer.residual.clone()
+    out = layer.residual
+    layer.run(pre=False, out=out)
+    layer.check(out, None, kept)
+
+
+@pytest.mark.parametrize("n", [3, 200])
+def test_a_row_that_is_not_finite_stays_alone(n):
+    layer = Layer(n, 64, 96, "relu", BF16)
+    layer.x[1, 5] = float("nan")
+    out, pre = layer.run()
+    assert np.isnan(f64(out)[1]).all()
+    keep = np.arange(n) != 1
+    assert np.isfinite(f64(out)[keep]).all()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gated"])
+def test_far_arguments(act):
+    """Activations of what is far from 0: the bias alone."""
+    layer = Layer(2, 8, 64, act, BF16)
+    layer.x.zero_()
+    layer.bias.copy_(torch.linspace(-300, 300, layer.wide))
+    layer.check(*layer.run())
+    layer.bias.fill_(1e30)
+    assert np.isfinite(f64(Layer.run(layer)[1])).all()
+
+
+def run_grad(dout, act, pre, count, dpre="new", dbias=True, accumulate=False):
+    n, d = dout.shape
+    wide = 2 * d if act == "gated" else d
+    if isinstance(dpre, str):
+        dpre = torch.full((n, wide), 77.0, dtype=dout.dtype, device="cuda")
+    dbias = torch.full((wide,), 0.25, device="cuda") if dbias else None
+    api.linear_grad(dout, act, pre, device_count(count), dpre, dbias, accumulate,
+                    api.LayerWorkspace(wide) if dbias is not None else None)
+    return dpre, dbias
+
+
+def check_grad(dout, act, pre, count, got, accumulate=False, sums=True):
+    m, dt = in_use(count, dout.shape[0]), dout.dtype
+    want, off = R.linear_grad(f64(dout)[:m], None if pre is None else f64(pre)[:m], act) if act != "none" else \
+        (f64(dout)[:m], 0.0 * f64(dout)[:m])
+    if got[0] is not None:
+        check(got[0][:m], want, off + half_step(dt) * (np.abs(want) + off) + tiny(dt), "dpre")
+    if sums:
+        total = want.sum(0) + (0.25 if accumulate else 0.0)
+        check(got[1], total, off.sum(0) + (m + 64) * U32 * (np.abs(want).sum(0) + 0.25) * 1.01, "dbias")
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("n,d", [(1, 1), (1, 128), (9, 7), (40, 129), (300, 512), (100, 1000), (3000, 90), (2500, 1537), (6, 70_001)])
+def test_grad_sizes(n, d, act):
+    wide = 2 * d if act == "gated" else d
+    for i, dtype in enumerate(HALVES):
+        dout = strided(normal((n, d), dtype, 1), d + 3 * i, i)
+        pre = None if act == "none" else strided(normal((n, wide), dtype, 2, 2.0), wide + 5 * i, 2 * i)
+        got = run_grad(dout, act, pre, None, accumulate=i == 1)
+        check_grad(dout, act, pre, None, got, accumulate=i == 1)
+
+
+@pytest.mark.parametrize("count", [0, -1, 1, 77, 500])
+@pytest.mark.parametrize("act", ["none", "gelu", "gated"])
+def test_grad_rows_in_use(count, act):
+    n, d = 120, 300
+    dout, pre = normal((n, d), BF16, 1).cuda(), normal((n, 2 * d if act == "gated" else d), BF16, 2).cuda()
+    got = run_grad(dout, act, pre, count)
+    check_grad(dout, act, pre, count, got)
+    assert (f64(got[0][in_use(count, n):]) == 77.0).all()
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_grad_in_place_and_left_out(act):
+    n, d = 50, 200
+    wide = 2 * d if act == "gated" else d
+    dout, pre = normal((n, d), F16, 1).cuda(), normal((n, wide), F16, 2).cuda()
+    got = run_grad(dout, act, pre, None, dbias=False)
+    check_grad(dout, act, pre, None, got, sums=False)
+    check_grad(dout, act, pre, None, run_grad(dout, act, pre, None, dpre=None))
+    same = pre.clone()
+    check_grad(dout, act, pre, None, run_grad(dout, act, same if act != "none" else None, None, dpre=same))
+    if act != "gated":
+        same = dout.clone()
+        check_grad(dout, act, pre, None, run_grad(same, act, pre, None, dpre=same))
+
+
+def test_grad_of_no_rows():
+    dout, pre = torch.zeros(0, 8, dtype=BF16, device="cuda"), torch.zeros(0, 16, dtype=BF16, device="cuda")
+    assert (f64(run_grad(dout, "gated", pre, None)[1]) == 0).all()
+    assert (f64(run_grad(dout, "gated", pre, None, accumulate=True)[1]) == 0.25).all()
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+def test_grad_far_from_0(act):
+    pre = torch.tensor([[-1e30, -1e4, -300.0, -25.0, 25.0, 300.0, 1e4, 1e30]], dtype=BF16, device="cuda")
+    dout = torch.ones(1, 8, dtype=BF16, device="cuda")
+    got = f64(run_grad(dout, act, pre, None)[0])[0]
+    assert (np.abs(got[:4]) < 1e-6).all() and (got[4:] == 1).all()
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_gradients_of_the_whole_layer(act):
+    """x, w and bias against differences of the reference's loss: dpre, then the products of one group."""
+    n, d_in, d_out, h = 6, 24, 16, 1e-5
+    layer = Layer(n, d_in, d_out, act, BF16, residual=True)
+    _, pre = layer.run()
+    dout = normal((n, d_out), BF16, 9).cuda()
+    dpre, dbias = run_grad(dout, act, pre, None)
+    group = torch.tensor([0, n], dtype=torch.int32, device="cuda")
+    dx, dw = torch.zeros_like(layer.x), torch.zeros(1, layer.wide, d_in, device="cuda")
+    api.expert_grad_input(dpre, group, layer.w[None], "none", None, dx)
+    api.expert_grad_weight(dpre, layer.x, None, 1, group, dw, False, api.ExpertWorkspace(n, 1, 1))
+    x, w, b, g = f64(layer.x), f64(layer.w), f64(layer.bias), f64(dout)
+    loss = lambda x, w, b: (R.linear(x, w, b, act, 0.0)[0] * g).sum()
+    rng = np.random.default_rng(4)
+    # pre, dpre and dx are rounded to 8 bits of precision: each sum is off by 3 half steps of its terms (the slopes change by at
+    # most 1.2 of what their argument does), the differences themselves by h^2 and 1e-11 / h
+    for name, got, at in (("x", f64(dx), lambda d: loss(x + d, w, b)), ("w", f64(dw)[0], lambda d: loss(x, w + d, b)),
+                          ("bias", f64(dbias), lambda d: loss(x, w, b + d))):
+        size = {"x": np.abs(g).sum() * 0 + (np.abs(f64(dpre)) @ np.abs(w)), "w": np.abs(f64(dpre)).T @ np.abs(x),
+                "bias": np.abs(f64(dpre)).sum(0)}[name]
+        more = 1.2 * 4 * 2.0 ** -8  # (|pre| below 4 here: its half step, through the slopes)
+        terms = {"x": np.abs(np.tile(g, layer.wide // d_out)) @ np.abs(w), "w": np.abs(np.tile(g, layer.wide // d_out)).T @ np.abs(x),
+                 "bias": np.abs(np.tile(g, layer.wide // d_out)).sum(0)}[name] * (3 if act == "gated" else 1)
+        for _ in range(20):
+            i = tuple(rng.integers(0, s) for s in got.shape)
+            d = np.zeros_like(got)
+            d[i] = h
+            slope = (at(d) - at(-d)) / (2 * h)
+            kink = 0.0
+            if act == "relu":  # (a pre-activation at the kink)
+                kink = terms[i] * (np.abs(f64(pre)) < 1e-2).any()
+            assert abs(got[i] - slope) <= 3 * 2.0 ** -8 * size[i] + more * terms[i] + kink + 1e-5, (name, i, got[i], slope)
+
+
+@pytest.mark.parametrize("n,act", [(6, "gelu"), (600, "gated")])
+def test_captured_and_same_bits(n, act):
+    layer = Layer(n, 256, 320, act, BF16, residual=True)
+    count, dt = device_count(n), BF16
+    z = lambda *s, t=dt: torch.zeros(*s, dtype=t, device="cuda")
+    out, pre, dpre, dbias = z(n, 320), z(n, layer.wide), z(n, layer.wide), z(layer.wide, t=F32)
+    ws, dout = api.LayerWorkspace(layer.wide), normal((n, 320), dt, 5).cuda()
+
+    def step():
+        api.linear(layer.x, layer.w, layer.bias, act, layer.residual, count, out, pre)
+        api.linear_grad(dout, act, pre, count, dpre, dbias, False, ws)
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for turn, m in enumerate((n, 3, 0, n)):
+        layer.x.copy_(normal((n, 256), dt, 30 + turn))
+        count.fill_(m)
+        g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, pre, dpre, dbias)]
+        step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, (out, pre, dpre, dbias)):
+            assert torch.equal(a, b)
+
+
+def test_far_rows():
+    """Rows whose places pass 32 bits, in every operand that has rows."""
+    n, d, ld = 5, 64, 1 << 29
+    wide = lambda: torch.zeros((n - 1) * ld + d, dtype=BF16, device="cuda").as_strided((n, d), (ld, 1))
+    layer = Layer(n, d, d, "silu", BF16)
+    x, out = wide(), wide()
+    x.copy_(layer.x)
+    layer.x = x
+    api.linear(x, layer.w, layer.bias, "silu", None, None, out, None)
+    layer.check(out, None)
+    dpre, dbias = run_grad(out, "silu", x, None, dpre=out)
+    assert np.isfinite(f64(dpre)).all() and np.isfinite(f64(dbias)).all()

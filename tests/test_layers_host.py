@@ -25,6 +25,11 @@ NORM = dict(x=P, dtype=BF16, ldx=32, count=None, n_max=8, d=32, gamma=P, beta=P,
 NORM_GRAD = dict(dout=P, dtype=BF16, lddo=32, x=P, ldx=32, count=None, n_max=8, d=32, gamma=P, mean=P, rstd=P,
                  residual=None, ldr=0, dx=P, lddx=32, dgamma=P, dbeta=P, accumulate=0, ws=P, ws_bytes=BIG, stream=None)
 
+LINEAR = dict(x=P, dtype=BF16, ldx=32, count=None, n_max=8, d_in=32, d_out=24, w=P, bias=P, act=0, residual=None, ldr=0, out=P,
+              ldo=24, pre=None, ldpre=0, stream=None)
+LINEAR_GRAD = dict(dout=P, dtype=BF16, lddo=24, count=None, n_max=8, d_out=24, act=2, pre=P, ldpre=48, dpre=P, lddp=48,
+                   dbias=P, accumulate=0, ws=P, ws_bytes=BIG, stream=None)
+
 
 def cfg(**change):
     c = api.route_config("softmax", 4)
@@ -85,6 +90,19 @@ OF_TABLE = [(dict(table=None), WORKSPACE), (dict(table=P + 128), WORKSPACE), (di
             (dict(n_chunks=1 << 31), SHAPE)]
 
 REFUSED = [
+    ("aa_linear", LINEAR, [
+        (dict(x=None), NULL), (dict(w=None), NULL), (dict(out=None), NULL), (dict(dtype=F32), SHAPE), (dict(dtype=9), SHAPE),
+        (dict(n_max=-1), SHAPE), (dict(d_in=0), SHAPE), (dict(d_out=0), SHAPE), (dict(act=5), SHAPE), (dict(act=-1), SHAPE),
+        (dict(d_in=(1 << 24) + 1, ldx=BIG), SHAPE), (dict(d_out=(1 << 24) + 1, ldo=BIG), SHAPE), (dict(ldx=31), SHAPE),
+        (dict(ldo=23), SHAPE), (dict(residual=P, ldr=23), SHAPE), (dict(pre=P, ldpre=23), SHAPE),
+        (dict(act=2, pre=P, ldpre=47), SHAPE), (dict(x=P + 1), ALIGN), (dict(out=P + 1), ALIGN), (dict(w=P + 1), ALIGN),
+        (dict(residual=P + 1, ldr=24), ALIGN), (dict(pre=P + 1, ldpre=24), ALIGN), (dict(bias=P + 2), ALIGN),
+        (dict(count=P + 2), ALIGN), (dict(n_max=2 ** 31 - 1), SHAPE)]),
+    ("aa_linear_grad", LINEAR_GRAD, [
+        (dict(dout=None), NULL), (dict(pre=None), NULL), (dict(dpre=None, dbias=None), NULL), (dict(dtype=F32), SHAPE),
+        (dict(n_max=-1), SHAPE), (dict(d_out=0), SHAPE), (dict(act=5), SHAPE), (dict(lddo=23), SHAPE), (dict(ldpre=47), SHAPE),
+        (dict(lddp=47), SHAPE), (dict(dout=P + 1), ALIGN), (dict(pre=P + 1), ALIGN), (dict(dpre=P + 1), ALIGN),
+        (dict(dbias=P + 2), ALIGN), (dict(ws=None), WORKSPACE), (dict(ws=P + 8), WORKSPACE), (dict(ws_bytes=4096), WORKSPACE)]),
     ("aa_adamw_chunks", CHUNKS, OF_LIST),
     ("aa_adamw_table", TABLE, OF_LIST + [(dict(table=None), WORKSPACE), (dict(table=P + 64), WORKSPACE),
                                          (dict(table_bytes=8192), WORKSPACE)]),
