@@ -599,7 +599,7 @@ typedef struct aa_adamw_tensor {
 } aa_adamw_tensor;
 
 typedef struct aa_adamw_config {
-  float lr, beta1, beta2, eps, weight_decay; /* 0 <= beta < 1, eps > 0, lr and weight_decay >= 0 */
+  float lr, beta1, beta2, eps, weight_decay; /* 0 <= beta < 1, eps >= 2^-126, the others >= 0 */
   int32_t reserved;
   uint64_t seed; /* of the rounding of 8-bit states */
 } aa_adamw_config;

@@ -20,7 +20,6 @@ namespace aa {
 
 namespace {
 
-constexpr int kUnits = 256;  // compute units
 constexpr int kBatch = 32;   // entries that travel as arguments of one launch
 
 struct EntryBatch {
@@ -33,40 +32,97 @@ __global__ __launch_bounds__(256) void k_adamw_table(char *table, int64_t map, i
   const TensorEntry e = batch.e[blockIdx.x];
   const int32_t tensor = first + (int32_t)blockIdx.x;
   if (threadIdx.x == 0) reinterpret_cast<TensorEntry *>(table + kTableEntries)[tensor] = e;
-  if (tensor == 0 && threadIdx.x < 64) reinterpret_cast<int32_t *>(table)[threadIdx.x] = threadIdx.x == 2 ? (int32_t)n_chunks : 0;
+  if (tensor == 0)
+    for (int w = threadIdx.x; w < kControlWords; w += 256) reinterpret_cast<int32_t *>(table)[w] = w == 0 ? (int32_t)n_chunks : 0;
   int32_t *of = reinterpret_cast<int32_t *>(table + map) + e.first_chunk;
   const int64_t chunks = (e.n + kChunk - 1) / kChunk;
   for (int64_t c = threadIdx.x; c < chunks; c += 256) of[c] = tensor;
 }
 
+// Global memory, which a pointer that was itself read from memory does not say (memory of any kind is slower to ask for,
+// and what waits for LDS then waits for it).
+template <typename T>
+using Global = __attribute__((address_space(1))) T *;
+
+// Eight elements at p of which n (at least one) exist, the others 0.
+template <typename T>
+__device__ __forceinline__ Eight load_some(const T *p, int n) {
+  const Global<const T> g = (Global<const T>)p;
+  Eight o;
+  if (n >= 8) {
+    const Line<T> t = *(Global<const Line<T>>)p;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o.v[i] = (float)t[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o.v[i] = i < n ? (float)g[i] : 0.f;
+  }
+  return o;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_some(T *p, const Eight &o, int n) {
+  const Global<T> g = (Global<T>)p;
+  if (n >= 8) {
+    Line<T> t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = (T)o.v[i];
+    *(Global<Line<T>>)p = t;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) g[i] = (T)o.v[i];
+  }
+}
+
 // Gradients i .. i + 7 of a tensor, of which n (at least one) exist.
 __device__ __forceinline__ Eight load_grad(const TensorEntry &e, int64_t i, int n) {
-  if (e.grad_dtype == AA_BF16) return load8(static_cast<const __bf16 *>(e.grad) + i, n);
-  if (e.grad_dtype == AA_F16) return load8(static_cast<const _Float16 *>(e.grad) + i, n);
-  return load8(static_cast<const float *>(e.grad) + i, n);
+  if (e.grad_dtype == AA_BF16) return load_some(static_cast<const __bf16 *>(e.grad) + i, n);
+  if (e.grad_dtype == AA_F16) return load_some(static_cast<const _Float16 *>(e.grad) + i, n);
+  return load_some(static_cast<const float *>(e.grad) + i, n);
 }
 
-// The chunks of this block: a run of neighbouring ones.
-struct Run {
-  int64_t from, to;
-};
-__device__ __forceinline__ Run chunks_of_block(const AdamWArgs &a) {
-  const int64_t listed = reinterpret_cast<const int32_t *>(a.table)[2], all = a.n_chunks < listed ? a.n_chunks : listed;
-  return {all * blockIdx.x / gridDim.x, all * (blockIdx.x + 1) / gridDim.x};
+// Calls work(tensor's number, its entry, first and last element) for the parts of tensors in this block's chunks, a run of
+// neighbouring ones: what is known of a tensor is asked for once a part.
+template <typename Work>
+__device__ __forceinline__ void walk(const AdamWArgs &a, Work work) {
+  // (a number of chunks that is not the table's: nothing is walked; asked for with the first tensor, not before it)
+  const int listed = reinterpret_cast<const int32_t *>(a.table)[0];
+  const uint32_t all = (uint32_t)a.n_chunks, each = all / gridDim.x, more = all % gridDim.x;
+  const int64_t begin = (int64_t)each * blockIdx.x + min(blockIdx.x, more);
+  const int64_t end = begin + each + (blockIdx.x < more ? 1 : 0);
+  for (int64_t c = begin; c < end;) {
+    const int of_chunk = reinterpret_cast<const int32_t *>(a.table + a.map)[c];
+    if (listed != (int)a.n_chunks) return;
+    const int tensor = __builtin_amdgcn_readfirstlane(of_chunk);
+    const TensorEntry &e = reinterpret_cast<const TensorEntry *>(a.table + kTableEntries)[tensor];
+    const int64_t next = e.first_chunk + (e.n + kChunk - 1) / kChunk, to = next < end ? next : end;
+    const int64_t last = (to - e.first_chunk) * kChunk;
+    work(tensor, e, (c - e.first_chunk) * kChunk, last < e.n ? last : e.n);
+    c = to;
+  }
 }
 
-__device__ __forceinline__ int tensor_of(const AdamWArgs &a, int64_t chunk) {
-  return __builtin_amdgcn_readfirstlane(reinterpret_cast<const int32_t *>(a.table + a.map)[chunk]);
-}
-
-// Whether this block is the last of the grid to come here (its thread 0 only); the word is 0 again then.  ORDERED: what the
-// others' threads 0 wrote before is seen after.
-template <bool ORDERED>
-__device__ __forceinline__ bool last_block(int32_t *word) {
-  const int before = __hip_atomic_fetch_add(word, 1, ORDERED ? __ATOMIC_ACQ_REL : __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  if (before != (int)gridDim.x - 1) return false;
+// Whether this block is the last of the grid to come here (its thread 0 only); the words are 0 again then.  Additions to one word
+// run one after the other (13 ns each), so that 32 blocks count together, and their last for them.  What this thread
+// stored for the whole device before has arrived: those stores and the loads behind the last block's go past the caches that
+// are not shared, so that nothing has to be written back or thrown away.  (The norm of 25 M elements: a release and an acquire
+// a block 70 us, all blocks at one word 37.)
+__device__ __forceinline__ bool count_in(int32_t *word, int all) {
+  if (__hip_atomic_fetch_add(word, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != all - 1) return false;
   __hip_atomic_store(word, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
   return true;
+}
+__device__ __forceinline__ bool last_block(int32_t *words) {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  const int group = blockIdx.x / kGroupBlocks, groups = (gridDim.x + kGroupBlocks - 1) / kGroupBlocks;
+  const int here = min((int)gridDim.x - group * kGroupBlocks, kGroupBlocks);
+  return count_in(words + (1 + group) * kWordApart, here) && count_in(words, groups);
+}
+
+// The words of a call: 0 the norm, 1 the update.
+__device__ __forceinline__ int32_t *done_words(const AdamWArgs &a, int call) {
+  return reinterpret_cast<int32_t *>(a.table) + kWordApart + call * kDoneWords;
 }
 
 __device__ __forceinline__ double wave_sum(double v) {
@@ -75,24 +131,44 @@ __device__ __forceinline__ double wave_sum(double v) {
   return v;
 }
 
+// The squares of gradients [from, to) of a tensor, 128 bytes a thread at once.
+template <typename T>
+__device__ __forceinline__ double squares(const T *g, int64_t from, int64_t to) {
+  constexpr int kLines = 16 / sizeof(T), kTurn = 256 * 8;
+  double sum = 0.0;
+  for (int64_t i = from + threadIdx.x * 8; i < to; i += kLines * kTurn) {
+    Line<T> x[kLines];
+#pragma unroll
+    for (int l = 0; l < kLines; ++l) {
+      x[l] = Line<T>{};
+      if (i + l * kTurn + 8 <= to) x[l] = *(Global<const Line<T>>)(g + i + l * kTurn);
+    }
+#pragma unroll
+    for (int l = 0; l < kLines; ++l)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) sum = fma((double)(float)x[l][k], (double)(float)x[l][k], sum);
+  }
+  // the line that the tensor ends in
+  const int64_t rest = to - (to - from) % 8;
+  if (rest + threadIdx.x < to) {
+    const double x = (double)(float)((Global<const T>)g)[rest + threadIdx.x];
+    sum = fma(x, x, sum);
+  }
+  return sum;
+}
+
 // Sum of squares in 64 bits (32 would end at gradients of 1.8e19).  Each block's part, and the last block adds them
 // up in their order.
 __global__ __launch_bounds__(256) void k_grad_norm(const AdamWArgs a) {
   __shared__ double room[4];
   __shared__ int last;
-  const Run run = chunks_of_block(a);
-  const TensorEntry *entries = reinterpret_cast<const TensorEntry *>(a.table + kTableEntries);
   double *parts = reinterpret_cast<double *>(a.table + kTableParts);
   double sum = 0.0;
-  for (int64_t c = run.from; c < run.to; ++c) {
-    const TensorEntry &e = entries[tensor_of(a, c)];
-    const int64_t i = (c - e.first_chunk) * kChunk + threadIdx.x * 8;
-    if (i >= e.n) continue;
-    const int64_t left = e.n - i;
-    const Eight g = load_grad(e, i, left < 8 ? (int)left : 8);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) sum = fma((double)g.v[k], (double)g.v[k], sum);
-  }
+  walk(a, [&](int, const TensorEntry &e, int64_t from, int64_t to) {
+    if (e.grad_dtype == AA_BF16) sum += squares(static_cast<const __bf16 *>(e.grad), from, to);
+    else if (e.grad_dtype == AA_F16) sum += squares(static_cast<const _Float16 *>(e.grad), from, to);
+    else sum += squares(static_cast<const float *>(e.grad), from, to);
+  });
   sum = wave_sum(sum);
   const int wave = threadIdx.x / kWave;
   if ((threadIdx.x & 63) == 0) room[wave] = sum;
@@ -100,7 +176,7 @@ __global__ __launch_bounds__(256) void k_grad_norm(const AdamWArgs a) {
   if (threadIdx.x == 0) {
     __hip_atomic_store(parts + blockIdx.x, room[0] + room[1] + room[2] + room[3], __ATOMIC_RELAXED,
                        __HIP_MEMORY_SCOPE_AGENT);
-    last = last_block<true>(reinterpret_cast<int32_t *>(a.table));
+    last = last_block(done_words(a, 0));
   }
   __syncthreads();
   if (!last) return;
@@ -126,6 +202,12 @@ struct Step {
   uint32_t k0, k1, t;
 };
 
+// Root of v >= 0 by the unit's instruction (one unit of the last place), which takes numbers below the normal ones for 0.
+__device__ __forceinline__ float root_of(float v) {
+  const bool low = v < 0x1p-96f;
+  return __builtin_amdgcn_sqrtf(low ? v * 0x1p64f : v) * (low ? 0x1p-32f : 1.f);
+}
+
 // The new m and v (its root in r) of eight elements, and their parameters.
 __device__ __forceinline__ void update8(const Step &s, const Eight &g, Eight &m, Eight &v, Eight &r, Eight &p, float shrink) {
 #pragma unroll
@@ -133,16 +215,16 @@ __device__ __forceinline__ void update8(const Step &s, const Eight &g, Eight &m,
     const float d = g.v[k] * s.factor;
     m.v[k] = s.beta1 * m.v[k] + (1.f - s.beta1) * d;
     v.v[k] = s.beta2 * v.v[k] + (1.f - s.beta2) * (d * d);
-    r.v[k] = sqrtf(v.v[k]);
-    p.v[k] = p.v[k] * shrink - s.rate * m.v[k] / (r.v[k] * s.root + s.eps);
+    r.v[k] = root_of(v.v[k]);
+    p.v[k] = p.v[k] * shrink - s.rate * m.v[k] * __builtin_amdgcn_rcpf(r.v[k] * s.root + s.eps);
   }
 }
 
 __device__ __forceinline__ void store_param(const TensorEntry &e, int64_t i, int n, const Eight &p) {
-  store8(e.param + i, p, n);
+  store_some(e.param + i, p, n);
   if (!e.copy) return;
-  if (e.copy_dtype == AA_BF16) store8(static_cast<__bf16 *>(e.copy) + i, p, n);
-  else store8(static_cast<_Float16 *>(e.copy) + i, p, n);
+  if (e.copy_dtype == AA_BF16) store_some(static_cast<__bf16 *>(e.copy) + i, p, n);
+  else store_some(static_cast<_Float16 *>(e.copy) + i, p, n);
 }
 
 struct Codes {
@@ -153,13 +235,13 @@ typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(1)));
 __device__ __forceinline__ Codes load_codes(const uint8_t *p, int n) {
   Codes c = {{0u, 0u}};
   if (n >= 8) {
-    const u32x2_any v = *reinterpret_cast<const u32x2_any *>(p);
+    const u32x2_any v = *(Global<const u32x2_any>)p;
     c.w[0] = v[0];
     c.w[1] = v[1];
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (k < n) c.w[k / 4] |= (uint32_t)p[k] << (k % 4 * 8);
+      if (k < n) c.w[k / 4] |= (uint32_t)((Global<const uint8_t>)p)[k] << (k % 4 * 8);
   }
   return c;
 }
@@ -169,11 +251,11 @@ __device__ __forceinline__ void store_codes(uint8_t *p, int n, const Codes &c) {
     u32x2_any v;
     v[0] = c.w[0];
     v[1] = c.w[1];
-    *reinterpret_cast<u32x2_any *>(p) = v;
+    *(Global<u32x2_any>)p = v;
   } else {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-      if (k < n) p[k] = (uint8_t)(c.w[k / 4] >> (k % 4 * 8));
+      if (k < n) ((Global<uint8_t>)p)[k] = (uint8_t)(c.w[k / 4] >> (k % 4 * 8));
   }
 }
 
@@ -204,36 +286,41 @@ __device__ __forceinline__ float block_max(float v) {
   return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-__device__ __forceinline__ float power_of_two(int e) { return __int_as_float((e + 127) << 23); }
-
-// Codes and scale of the block's states.  A step of the format at a is 2^max(exponent - 3, -9); a in steps plus the draw's
-// part of one, cut, is the rounding.  What is not finite is held as NaN and takes no part in the scale.
-template <bool AT_LEAST_ONE>
+// Codes and scale of the block's states, by the unit's own conversion with a rounding by draw: it adds the upper bits of
+// the word to what it cuts off, at numbers below the format's normal ones, too.  What is not finite becomes NaN and takes no part
+// in the scale.  POSITIVE: no value is below 0, and what is above it is at least a step.
+template <bool POSITIVE>
 __device__ __forceinline__ Codes encode(const Eight &x, const uint4 &draws, float *scale) {
-  float most = 0.f;
+  const auto larger = [](float a, float b, float c) { return fmaxf(fmaxf(a, b), c); };
+  float most = larger(fabsf(x.v[0]), fabsf(x.v[1]), fabsf(x.v[2]));
+  most = larger(most, fabsf(x.v[3]), fabsf(x.v[4]));
+  most = larger(most, fabsf(x.v[5]), fabsf(x.v[6]));
+  most = block_max(fmaxf(most, fabsf(x.v[7])));
+  if (__builtin_expect(__ballot(!(most < __builtin_inff())) != 0ull, 0)) {  // (a wave that holds an infinity)
+    most = 0.f;
 #pragma unroll
-  for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x.v[k]) < __builtin_inff() ? fabsf(x.v[k]) : 0.f);
-  most = block_max(most);
+    for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x.v[k]) < __builtin_inff() ? fabsf(x.v[k]) : 0.f);
+    most = block_max(most);
+  }
   const int e = max((int)(__float_as_uint(most) >> 23) - 126 - 8, -126);
-  *scale = most > 0.f ? power_of_two(e) : 0.f;
-  const float inv = power_of_two(-e);
+  *scale = most > 0.f ? __int_as_float((e + 127) << 23) : 0.f;
+  const float inv = __int_as_float((127 - e) << 23);
   const uint32_t words[4] = {draws.x, draws.y, draws.z, draws.w};
   float y[8];
 #pragma unroll
   for (int k = 0; k < 8; ++k) {
-    const uint32_t draw = k & 1 ? words[k >> 1] >> 16 : words[k >> 1] & 0xFFFFu;
-    const float a = fabsf(x.v[k]) * inv;
-    const int s = max((int)(__float_as_uint(a) >> 23) - 130, -9);
-    float q = floorf(a * power_of_two(-s) + (float)draw * 0x1p-16f);
-    if (AT_LEAST_ONE && a > 0.f) q = fmaxf(q, 1.f);
-    y[k] = copysignf(q * power_of_two(s), x.v[k]);
-    if (!(fabsf(x.v[k]) < __builtin_inff())) y[k] = __builtin_nanf("");
+    y[k] = x.v[k] * inv;
+    if (POSITIVE && x.v[k] > 0.f) y[k] = fmaxf(y[k], 0x1p-9f);
   }
   Codes c;
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[h * 4], y[h * 4 + 1], 0, false);
-    c.w[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[h * 4 + 2], y[h * 4 + 3], w, true);
+    int w = 0;
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(y[h * 4 + 0], (int)(words[h * 2] << 16), w, 0);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(y[h * 4 + 1], (int)(words[h * 2] & 0xFFFF0000u), w, 1);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(y[h * 4 + 2], (int)(words[h * 2 + 1] << 16), w, 2);
+    w = __builtin_amdgcn_cvt_sr_fp8_f32(y[h * 4 + 3], (int)(words[h * 2 + 1] & 0xFFFF0000u), w, 3);
+    c.w[h] = (uint32_t)w;
   }
   return c;
 }
@@ -257,42 +344,44 @@ __global__ __launch_bounds__(256) void k_adamw_step(const AdamWArgs a) {
     s.k0 = (uint32_t)a.cfg.seed;
     s.k1 = (uint32_t)(a.cfg.seed >> 32);
     s.t = (uint32_t)before + 1u;
-    const Run run = chunks_of_block(a);
-    const TensorEntry *entries = reinterpret_cast<const TensorEntry *>(a.table + kTableEntries);
-    for (int64_t c = run.from; c < run.to; ++c) {
-      const int tensor = tensor_of(a, c);
-      const TensorEntry &e = entries[tensor];
-      const int64_t i = (c - e.first_chunk) * kChunk + threadIdx.x * 8, left = e.n - i;
-      const int n = left < 8 ? (int)left : 8;
+    walk(a, [&](int tensor, const TensorEntry &e, int64_t from, int64_t to) {
       const float shrink = 1.f - s.shrink * e.decay;
-      Eight r;
       if (e.bits == 32) {
-        if (n <= 0) continue;
-        float *pm = static_cast<float *>(e.m) + i, *pv = static_cast<float *>(e.v) + i;
-        const Eight g = load_grad(e, i, n);
-        Eight p = load8(e.param + i, n), m = load8(pm, n), v = load8(pv, n);
-        update8(s, g, m, v, r, p, shrink);
-        store_param(e, i, n, p);
-        store8(pm, m, n);
-        store8(pv, v, n);
-      } else {
-        Eight m, v, p;
+        for (int64_t i = from + threadIdx.x * 8; i < to; i += 256 * 8) {
+          const int n = to - i < 8 ? (int)(to - i) : 8;
+          float *pm = static_cast<float *>(e.m) + i, *pv = static_cast<float *>(e.v) + i;
+          const Eight g = load_grad(e, i, n);
+          Eight p = load_some(e.param + i, n), m = load_some(pm, n), v = load_some(pv, n), r;
+          update8(s, g, m, v, r, p, shrink);
+          store_param(e, i, n, p);
+          store_some(pm, m, n);
+          store_some(pv, v, n);
+        }
+        return;
+      }
+      // (whole waves take part where one lane does: they share the scales)
+      for (int64_t base = from; base < to; base += 256 * 8) {
+        const int64_t i = base + threadIdx.x * 8;
+        const int n = to - i < 8 ? (int)(to - i) : 8;
         uint8_t *pm = static_cast<uint8_t *>(e.m) + i, *pv = static_cast<uint8_t *>(e.v) + i;
-        float *ms = e.m_scale + i / kStateBlock, *vs = e.v_scale + i / kStateBlock;
+        const Global<float> ms = (Global<float>)(e.m_scale + i / kStateBlock), vs = (Global<float>)(e.v_scale + i / kStateBlock);
+        Eight m, v, r, p;
 #pragma unroll
         for (int k = 0; k < 8; ++k) m.v[k] = r.v[k] = 0.f;
         if (n > 0) {
           const Eight g = load_grad(e, i, n);
-          p = load8(e.param + i, n);
+          p = load_some(e.param + i, n);
           m = decode(load_codes(pm, n), *ms);
           v = decode(load_codes(pv, n), *vs);
 #pragma unroll
           for (int k = 0; k < 8; ++k) v.v[k] *= v.v[k];
           update8(s, g, m, v, r, p, shrink);
           store_param(e, i, n, p);
+          if (n < 8) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k)
-            if (k >= n) m.v[k] = r.v[k] = 0.f;
+            for (int k = 0; k < 8; ++k)
+              if (k >= n) m.v[k] = r.v[k] = 0.f;
+          }
         }
         const uint4 draws = philox_words((uint32_t)(i / 8), 0x80000000u | (uint32_t)tensor, s.t, 0u, s.k0, s.k1);
         float m_scale, v_scale;
@@ -306,11 +395,11 @@ __global__ __launch_bounds__(256) void k_adamw_step(const AdamWArgs a) {
           }
         }
       }
-    }
+    });
   }
   // every block has read the counter before it is counted here
   __syncthreads();
-  if (threadIdx.x == 0 && last_block<false>(reinterpret_cast<int32_t *>(a.table) + 1) && !skip) *a.t = before + 1;
+  if (threadIdx.x == 0 && last_block(done_words(a, 1)) && !skip) *a.t = before + 1;
 }
 
 }  // namespace
@@ -343,7 +432,7 @@ hipError_t launch_grad_norm(const AdamWArgs &a, hipStream_t st) {
 }
 
 hipError_t launch_adamw_step(const AdamWArgs &a, hipStream_t st) {
-  const int64_t most = kUnits * 8, blocks = a.n_chunks < 1 ? 1 : a.n_chunks < most ? a.n_chunks : most;
+  const int64_t most = kMostBlocks, blocks = a.n_chunks < 1 ? 1 : a.n_chunks < most ? a.n_chunks : most;
   hipLaunchKernelGGL(k_adamw_step, dim3((uint32_t)blocks), dim3(256), 0, st, a);
   return hipGetLastError();
 }

@@ -20,9 +20,13 @@ struct TensorEntry {
   float decay;
 };
 
-// The table: control words (word 0, 1: blocks that are done with a call; 2: chunks), the norm's parts, the entries, and the tensor
-// of each chunk.
-constexpr size_t kTableParts = 256;
+// The table: control words (the number of chunks, then for the norm and for the update the blocks that are done with the call),
+// the norm's parts, the entries, and the tensor of each chunk.
+constexpr int kMostBlocks = 2048, kGroupBlocks = 32;  // of a launch; that count themselves together
+constexpr int kWordApart = 16;                        // int32 words between two that are counted in
+constexpr int kDoneWords = (1 + kMostBlocks / kGroupBlocks) * kWordApart;
+constexpr int kControlWords = kWordApart + 2 * kDoneWords;
+constexpr size_t kTableParts = (kControlWords * sizeof(int32_t) + 255) / 256 * 256;
 constexpr size_t kTableEntries = kTableParts + kNormBlocks * sizeof(double);
 inline size_t table_map(int64_t n_tensors) { return align_up(kTableEntries + n_tensors * sizeof(TensorEntry), 256); }
 inline size_t table_bytes(int64_t n_tensors, int64_t n_chunks) {

@@ -295,7 +295,7 @@ int32_t aa_adamw_step(void *table, size_t table_bytes_, int32_t n_tensors, int64
   const auto beta = [](float b) { return b >= 0.0f && b < 1.0f; };
   const auto size = [](float v) { return v >= 0.0f && isfinite(v); };
   if (!beta(cfg->beta1) || !beta(cfg->beta2) || !size(cfg->lr) || !size(cfg->weight_decay)) return AA_ERR_SHAPE;
-  if (!size(cfg->eps) || cfg->eps == 0.0f) return AA_ERR_SHAPE;
+  if (!size(cfg->eps) || cfg->eps < 0x1p-126f) return AA_ERR_SHAPE;  // (a normal number: it is divided by)
   AA_TRY(check_words(lr_factor, false));
   AA_TRY(check_words(grad_factor, false));
   AA_TRY(check_words(count, false));

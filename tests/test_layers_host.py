@@ -111,7 +111,7 @@ REFUSED = [
         (dict(out=P + 2), ALIGN), (dict(scale=P + 1), ALIGN)]),
     ("aa_adamw_step", STEP, OF_TABLE + [
         (dict(cfg=None), NULL), (dict(cfg=opt(beta1=1.0)), SHAPE), (dict(cfg=opt(beta1=-0.1)), SHAPE),
-        (dict(cfg=opt(beta2=NAN)), SHAPE), (dict(cfg=opt(eps=0.0)), SHAPE), (dict(cfg=opt(eps=INF)), SHAPE),
+        (dict(cfg=opt(beta2=NAN)), SHAPE), (dict(cfg=opt(eps=0.0)), SHAPE), (dict(cfg=opt(eps=1e-39)), SHAPE), (dict(cfg=opt(eps=INF)), SHAPE),
         (dict(cfg=opt(lr=-1.0)), SHAPE), (dict(cfg=opt(lr=INF)), SHAPE), (dict(cfg=opt(weight_decay=-1.0)), SHAPE),
         (dict(t=None), NULL), (dict(t=P + 2), ALIGN), (dict(lr_factor=P + 2), ALIGN), (dict(grad_factor=P + 2), ALIGN),
         (dict(count=P + 2), ALIGN)]),
