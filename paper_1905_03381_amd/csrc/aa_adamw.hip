@@ -103,18 +103,11 @@ __device__ __forceinline__ void walk(const AdamWArgs &a, Work work) {
   }
 }
 
-// Whether this block is the last of the grid to come here (its thread 0 only); the words are 0 again then.  Additions to one word
-// run one after the other (13 ns each), so that 32 blocks count together, and their last for them.  What this thread
-// stored for the whole device before has arrived: those stores and the loads behind the last block's go past the caches that
-// are not shared, so that nothing has to be written back or thrown away.  (The norm of 25 M elements: a release and an acquire
-// a block 70 us, all blocks at one word 37.)
-__device__ __forceinline__ bool count_in(int32_t *word, int all) {
-  if (__hip_atomic_fetch_add(word, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != all - 1) return false;
-  __hip_atomic_store(word, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  return true;
-}
+// Whether this block is the last of the grid to come here (its thread 0 only).  Additions to one word run one after the
+// other (13 ns each), so that 32 blocks count together, and their last for them.  (The norm of 25 M elements: a release and an
+// acquire a block 70 us, all blocks at one word 37.)
 __device__ __forceinline__ bool last_block(int32_t *words) {
-  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  stores_arrived();
   const int group = blockIdx.x / kGroupBlocks, groups = (gridDim.x + kGroupBlocks - 1) / kGroupBlocks;
   const int here = min((int)gridDim.x - group * kGroupBlocks, kGroupBlocks);
   return count_in(words + (1 + group) * kWordApart, here) && count_in(words, groups);

@@ -214,7 +214,10 @@ int32_t aa_balance(const void *logits, int32_t dtype, int64_t ld, const int32_t 
   a.counts = counts;
   a.share = share;
   a.loss = loss;
-  a.z_part = reinterpret_cast<float *>(static_cast<char *>(ws) + 256);
+  static_assert(256 + kBalanceTerms * sizeof(double) + kBalanceBlocks * sizeof(float) <= kLayerHead, "");
+  a.done = static_cast<int32_t *>(ws);
+  a.terms = reinterpret_cast<double *>(static_cast<char *>(ws) + 256);
+  a.z_part = reinterpret_cast<float *>(a.terms + kBalanceTerms);
   a.part = body(ws);
   return hip_status(launch_balance(a, as_stream(stream)));
 }

@@ -98,4 +98,15 @@ __device__ __forceinline__ float lanes_sum(float v, int lane) {
   }
 }
 
+// What this thread has stored for the whole device has arrived there.  Such stores, and the loads behind count_in, go past
+// the caches that are not shared, so that nothing has to be written back or thrown away.
+__device__ __forceinline__ void stores_arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Counts one of `all` that come to `word`; true for the last of them, and the word is 0 again then.
+__device__ __forceinline__ bool count_in(int32_t *word, int all) {
+  if (__hip_atomic_fetch_add(word, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != all - 1) return false;
+  __hip_atomic_store(word, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  return true;
+}
+
 }  // namespace aa

@@ -5,137 +5,13 @@
 // takes 36 now, 9 of it the plan: 16,384 rows, 256 experts in 8 groups, 8 choices).  Bound by instructions: a turn of
 // the choice is a maximum over a lane's experts and over the lanes, scores are exponentials in 64 bits; reading the logits is
 // a small part (of 65,536 rows of 128 experts 15 us, 2.3 TB/s, without a bias, 33 with one).
-#include "aa_route.hpp"
+#include "aa_route_lanes.hpp"
 
 #include <type_traits>
 
 namespace aa {
 
 namespace {
-
-constexpr float kNegInf = -__builtin_inff();
-
-// What the lanes of a wave wrote to LDS before is read by its other lanes after.
-__device__ __forceinline__ void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
-// Largest value and sum over aligned groups of LPR (16 or 64) lanes, every lane gets it: inside a row of 16 lanes
-// quad swaps, half mirror, mirror; across rows exchanges with the lanes 16 and 32 away.  No LDS.
-template <int CTRL>
-__device__ __forceinline__ float lane_move(float v) {
-  return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xF, 0xF, true));
-}
-template <int CTRL>
-__device__ __forceinline__ double lane_move(double v) {
-  const int lo = __builtin_amdgcn_update_dpp(0, __double2loint(v), CTRL, 0xF, 0xF, true);
-  const int hi = __builtin_amdgcn_update_dpp(0, __double2hiint(v), CTRL, 0xF, 0xF, true);
-  return __hiloint2double(hi, lo);
-}
-
-template <bool FAR>  // the lane 16 or (FAR) 32 away and this one, in some order
-__device__ __forceinline__ void exchange(uint32_t v, uint32_t *x, uint32_t *y) {
-  const auto r = FAR ? __builtin_amdgcn_permlane32_swap(v, v, false, false)
-                     : __builtin_amdgcn_permlane16_swap(v, v, false, false);
-  *x = r[0];
-  *y = r[1];
-}
-template <bool FAR>
-__device__ __forceinline__ void exchange(float v, float *x, float *y) {
-  uint32_t a, b;
-  exchange<FAR>(__float_as_uint(v), &a, &b);
-  *x = __uint_as_float(a);
-  *y = __uint_as_float(b);
-}
-template <bool FAR>
-__device__ __forceinline__ void exchange(double v, double *x, double *y) {
-  uint32_t al, bl, ah, bh;
-  exchange<FAR>((uint32_t)__double2loint(v), &al, &bl);
-  exchange<FAR>((uint32_t)__double2hiint(v), &ah, &bh);
-  *x = __hiloint2double((int)ah, (int)al);
-  *y = __hiloint2double((int)bh, (int)bl);
-}
-
-__device__ __forceinline__ float larger(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ double larger(double a, double b) { return fmax(a, b); }
-
-template <int LPR, typename V>
-__device__ __forceinline__ V lanes_max(V v) {
-  static_assert(LPR == 16 || LPR == 64, "");
-  v = larger(v, lane_move<0xB1>(v));
-  v = larger(v, lane_move<0x4E>(v));
-  v = larger(v, lane_move<0x141>(v));
-  v = larger(v, lane_move<0x140>(v));
-  if (LPR == 64) {
-    V x, y;
-    exchange<false>(v, &x, &y);
-    exchange<true>(larger(x, y), &x, &y);
-    v = larger(x, y);
-  }
-  return v;
-}
-
-template <int LPR, typename V>
-__device__ __forceinline__ V lanes_sum(V v) {
-  static_assert(LPR == 16 || LPR == 64, "");
-  v += lane_move<0xB1>(v);
-  v += lane_move<0x4E>(v);
-  v += lane_move<0x141>(v);
-  v += lane_move<0x140>(v);
-  if (LPR == 64) {
-    V x, y;
-    exchange<false>(v, &x, &y);
-    exchange<true>(x + y, &x, &y);
-    v = x + y;
-  }
-  return v;
-}
-
-// N neighbouring logits of a row, -inf for those at or past E and for NaN.  vec: they exist whole or not at all, and can
-// be moved at once.
-template <typename T, int N>
-__device__ __forceinline__ void load_logits(const T *row, int e0, int E, bool vec, float *x) {
-  constexpr int kOn = N * sizeof(T) < 16 ? N * sizeof(T) : 16;
-  typedef T Line __attribute__((ext_vector_type(N), aligned(kOn)));
-  if (vec) {
-    if (e0 < E) {
-      const Line v = *reinterpret_cast<const Line *>(row + e0);
-#pragma unroll
-      for (int i = 0; i < N; ++i) x[i] = (float)v[i];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = (float)row[min(e0 + i, E - 1)];
-  }
-#pragma unroll
-  for (int i = 0; i < N; ++i)
-    if (e0 + i >= E || !(x[i] > kNegInf)) x[i] = kNegInf;
-}
-
-template <int N>
-__device__ __forceinline__ void load_logits(const void *logits, int dtype, int64_t at, int e0, int E, bool vec, float *x) {
-  if (dtype == AA_BF16) load_logits<__bf16, N>(static_cast<const __bf16 *>(logits) + at, e0, E, vec, x);
-  else if (dtype == AA_F16) load_logits<_Float16, N>(static_cast<const _Float16 *>(logits) + at, e0, E, vec, x);
-  else load_logits<float, N>(static_cast<const float *>(logits) + at, e0, E, vec, x);
-}
-
-template <typename T, int N>
-__device__ __forceinline__ void store_logits(T *row, int e0, int E, bool vec, const float *x) {
-  constexpr int kOn = N * sizeof(T) < 16 ? N * sizeof(T) : 16;
-  typedef T Line __attribute__((ext_vector_type(N), aligned(kOn)));
-  if (vec) {
-    if (e0 >= E) return;
-    Line v;
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = (T)x[i];
-    *reinterpret_cast<Line *>(row + e0) = v;
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (e0 + i < E) row[e0 + i] = (T)x[i];
-  }
-}
 
 // exp(v) of v <= 0 in 64 bits, 0 far below: v = n ln 2 + r, |r| <= ln 2 / 2, and the power series of e^r to r^13 (the
 // next term is below 2^-57).  Half the instructions of the library's, which serves all of the range.
@@ -151,8 +27,6 @@ __device__ __forceinline__ double exp_below(double v) {
   p = fma(p, r, 1.0);
   return ldexp(p, (int)n);
 }
-
-constexpr float kNoScore = -745.1332f;  // ln 2^-1075: from there down exp_below is 0
 
 // 1 / v for 1 <= v <= 2, by Newton's steps.
 __device__ __forceinline__ double reciprocal(double v) {
@@ -421,245 +295,26 @@ __global__ __launch_bounds__(256) void k_route(const RouteArgs a) {
   }
 }
 
-// ---- balance loss ---------------------------------------------------------------------------------------
-// With c_e the choices of expert e among the m K of the rows in use, p_te = s_te / sum_e s_te and q_t the softmax of a row:
-//   loss = coef E / (m K) sum_e c_e P_e + z / m sum_t lse_t^2,   P_e = sum_t p_te / m,  lse_t = log sum_e exp x_te
-//   d/dx_te = coef E / (m^2 K) p_te w_te (c_e - sum_e p_te c_e) + 2 z / m lse_t q_te,   w = 1 (softmax) or 1 - s_te (sigmoid).
-// c_e may be counted from the mean of all: both c_e - sum p c then lose fewer digits.
-
-// What a row's EPL logits a lane come to: the shares of the sum of scores (sigmoid: with the scores' complements), the
-// softmax and log sum exp (0 where there is none that is finite).
-template <int LPR, int EPL>
-__device__ __forceinline__ void row_shares(const float (&x)[EPL], bool softmax, float (&p)[EPL], float (&rest)[EPL],
-                                           float (&q)[EPL], float *lse) {
-  float top = kNegInf, sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) top = fmaxf(top, x[i]);
-  top = lanes_max<LPR>(top);
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    q[i] = !(x[i] > kNegInf) ? 0.f : x[i] == top ? 1.f : __expf(x[i] - top);
-    sum += q[i];
-  }
-  sum = lanes_sum<LPR>(sum);
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) q[i] *= inv;
-  *lse = fabsf(top) < -kNegInf ? top + __logf(sum) : 0.f;
-  if (softmax) {
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      p[i] = q[i];
-      rest[i] = 1.f;
-    }
-    return;
-  }
-  // scores relative to the highest: in 32 bits those of low logits would all be 0
-  const float low = fminf(top, 0.f);
-  float all = 0.f;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    const float t = __expf(-fabsf(x[i])), r = 1.f / (1.f + t);
-    p[i] = x[i] > kNegInf ? __expf(fminf(x[i], 0.f) - low) * r : 0.f;
-    rest[i] = x[i] > 0.f ? t * r : r;
-    all += p[i];
-  }
-  all = lanes_sum<LPR>(all);
-  const float part = all > 0.f ? 1.f / all : 0.f;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) p[i] *= part;
-}
-
-// The experts' choices, counted from their mean, and the factors of the two terms.
-template <int LPR, int EPL>
-__device__ __forceinline__ void balance_scales(const RouteGradArgs &a, int rows, int e0, float (&counts)[EPL],
-                                               float *scale, float *z_scale) {
-  int sum = 0, c[EPL];
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) {
-    c[i] = e0 + i < a.n_experts ? a.counts[e0 + i] : 0;
-    sum += c[i];
-  }
-  const double mean = lanes_sum<LPR>((double)sum) / a.n_experts;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) counts[i] = (float)((double)c[i] - mean);
-  const double m = rows, up = a.dloss ? *a.dloss : 1.f;
-  *scale = (float)(up * a.coef * a.n_experts / (m * m * a.cfg.top_k));
-  *z_scale = (float)(up * 2.0 * a.z_coef / m);
-}
-
-template <int LPR, int EPL>
-__device__ __forceinline__ void balance_terms(const float (&x)[EPL], bool softmax, const float (&counts)[EPL],
-                                              float scale, float z_scale, float (&out)[EPL]) {
-  float p[EPL], rest[EPL], q[EPL], lse, dot = 0.f;
-  row_shares<LPR, EPL>(x, softmax, p, rest, q, &lse);
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) dot += p[i] * counts[i];
-  dot = lanes_sum<LPR>(dot);
-  lse *= z_scale;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) out[i] = scale * p[i] * rest[i] * (counts[i] - dot) + lse * q[i];
-}
-
-constexpr int kBalanceThreads = 1024;
-
-// (sixteen experts a lane take more registers than sixteen waves leave)
-template <int EPL>
-constexpr int kRowsThreads = EPL > 8 ? 512 : kBalanceThreads;
-
-// Shares and choices of the rows that a block takes, a lane's experts in registers; what the block's waves have is added
-// up in LDS, half of them at a time.
-template <int LPR, int EPL>
-__global__ __launch_bounds__(kRowsThreads<EPL>) void k_balance_rows(const BalanceArgs a) {
-  constexpr int kRows = kWave / LPR, kThreads = kRowsThreads<EPL>, kWaves = kThreads / kWave;
-  __shared__ float room[kWaves / 2][EPL][kWave];
-  __shared__ int hist[LPR * EPL];
-  __shared__ float z_room[kWaves];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % LPR, e0 = sub * EPL;
-  const int rows = rows_in_use(a.count, a.n_max), E = a.n_experts, K = a.cfg.top_k;
-  const bool softmax = a.cfg.score == AA_SCORE_SOFTMAX;
-  for (int e = threadIdx.x; e < LPR * EPL; e += kThreads) hist[e] = 0;
-  __syncthreads();
-  float sums[EPL], z = 0.f;
-#pragma unroll
-  for (int i = 0; i < EPL; ++i) sums[i] = 0.f;
-  for (int64_t base = ((int64_t)blockIdx.x * kWaves + wave) * kRows; base < rows; base += (int64_t)gridDim.x * kWaves * kRows) {
-    const int64_t row = base + lane / LPR;
-    const bool live = row < rows;
-    float x[EPL];
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) x[i] = kNegInf;
-    if (live) load_logits<EPL>(a.logits, a.dtype, row * a.ld, e0, E, a.vec, x);
-    if (live && sub < K) {
-      const int id = a.ids[row * K + sub];
-      if (id >= 0 && id < E) atomicAdd(&hist[id], 1);
-    }
-    float p[EPL], rest[EPL], q[EPL], lse;
-    row_shares<LPR, EPL>(x, softmax, p, rest, q, &lse);
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) sums[i] += p[i];
-    z += sub == 0 ? lse * lse : 0.f;
-  }
-  if constexpr (LPR == 16) {  // the wave's rows
-#pragma unroll
-    for (int i = 0; i < EPL; ++i) {
-      float u, v;
-      exchange<false>(sums[i], &u, &v);
-      exchange<true>(u + v, &u, &v);
-      sums[i] = u + v;
-    }
-  }
-  z = lanes_sum<64>(z);
-  if (lane == 0) z_room[wave] = z;
-#pragma unroll
-  for (int half = kWaves / 2; half >= 1; half /= 2) {
-    if (wave >= half && wave < 2 * half) {
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) room[wave - half][i][lane] = sums[i];
-    }
-    __syncthreads();
-    if (wave < half) {
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) sums[i] += room[wave][i][lane];
-    }
-    __syncthreads();
-  }
-  const int wide = (E + 3) & ~3;
-  float *part = a.part + (size_t)blockIdx.x * 2 * wide;
-  int *choices = reinterpret_cast<int *>(part + wide);
-  if (wave == 0 && lane < LPR) {
-#pragma unroll
-    for (int i = 0; i < EPL; ++i)
-      if (e0 + i < wide) part[e0 + i] = e0 + i < E ? sums[i] : 0.f;
-  }
-  for (int e = threadIdx.x; e < wide; e += kThreads) choices[e] = e < LPR * EPL ? hist[e] : 0;
-  if (threadIdx.x == 0) {
-    float all = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) all += z_room[w];
-    a.z_part[blockIdx.x] = all;
-  }
-}
-
-// The blocks' parts, added up in their order by one block, four experts a thread.
-__global__ __launch_bounds__(kBalanceThreads) void k_balance_join(const BalanceArgs a, int blocks) {
-  typedef int i4 __attribute__((ext_vector_type(4)));
-  __shared__ f4 room_p[kBalanceThreads];
-  __shared__ i4 room_c[kBalanceThreads];
-  __shared__ double terms[kBalanceThreads / kWave], squares[kBalanceThreads / kWave];
-  const int rows = rows_in_use(a.count, a.n_max), E = a.n_experts, wide = (E + 3) & ~3, quads = wide / 4;
-  const int shares = kBalanceThreads / quads, quad = threadIdx.x % quads, share = threadIdx.x / quads;
-  f4 p = {0.f, 0.f, 0.f, 0.f};
-  i4 c = {0, 0, 0, 0};
-  if (share < shares) {
-    const int each = (blocks + shares - 1) / shares, from = min(share * each, blocks), to = min(from + each, blocks);
-    const float *at = a.part + quad * 4;
-#pragma unroll 8
-    for (int b = from; b < to; ++b) {
-      p += *reinterpret_cast<const f4 *>(at + (size_t)b * 2 * wide);
-      c += *reinterpret_cast<const i4 *>(at + (size_t)b * 2 * wide + wide);
-    }
-  }
-  room_p[threadIdx.x] = p;
-  room_c[threadIdx.x] = c;
-  __syncthreads();
-  double term = 0.0, square = (int)threadIdx.x < blocks ? (double)a.z_part[threadIdx.x] : 0.0;
-  if ((int)threadIdx.x < quads) {
-    for (int s = 1; s < shares; ++s) {
-      p += room_p[s * quads + threadIdx.x];
-      c += room_c[s * quads + threadIdx.x];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = threadIdx.x * 4 + i;
-      if (e >= E) continue;
-      const double mean = rows > 0 ? (double)p[i] / rows : 0.0;
-      term += (double)c[i] * mean;
-      a.counts[e] = c[i];
-      if (a.share) a.share[e] = (float)mean;
-    }
-  }
-  term = lanes_sum<64>(term);
-  square = lanes_sum<64>(square);
-  if ((threadIdx.x & 63) == 0) {
-    terms[threadIdx.x / kWave] = term;
-    squares[threadIdx.x / kWave] = square;
-  }
-  __syncthreads();
-  if (threadIdx.x != 0 || !a.loss) return;
-  term = square = 0.0;
-  for (int w = 0; w < kBalanceThreads / kWave; ++w) {
-    term += terms[w];
-    square += squares[w];
-  }
-  a.loss[0] = rows > 0 ? (float)(term * a.coef * E / ((double)rows * a.cfg.top_k)) : 0.f;
-  a.loss[1] = rows > 0 ? (float)(square * a.z_coef / rows) : 0.f;
-}
-
-// ---- gradient of the routing ----------------------------------------------------------------------------
 // LPR lanes a row, EPL neighbouring experts each; lane k keeps choice k.  With v the score of the choices and
 // a = scale dweights:
 //   renormalised   ds_k = (a_k - sum a v / S) / S,  S = sum v
 //   sigmoid        dlogit_k = ds_k v_k (1 - v_k), 0 elsewhere
 //   softmax        dlogit_e = s_e (ds_e - sum ds v); renormalised: the softmax over the choices alone.
-// BALANCE: the gradient of the balance loss (below) is added to it.
-template <int LPR, int EPL, bool BALANCE>
+template <int LPR, int EPL>
 __global__ __launch_bounds__(256) void k_route_grad(const RouteGradArgs a) {
   constexpr int kRows = kWave / LPR;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, sub = lane % LPR, e0 = sub * EPL;
   const int rows = rows_in_use(a.count, a.n_max);
   const int E = a.n_experts, K = a.cfg.top_k;
   const bool softmax = a.cfg.score == AA_SCORE_SOFTMAX, renorm = a.cfg.renormalise != 0;
-  float counts[EPL], scale = 0.f, z_scale = 0.f;
-  if constexpr (BALANCE) balance_scales<LPR, EPL>(a, rows, e0, counts, &scale, &z_scale);
   for (int64_t base = ((int64_t)blockIdx.x * 4 + wave) * kRows; base < rows; base += (int64_t)gridDim.x * 4 * kRows) {
     const int64_t row = base + lane / LPR;
     const bool live = row < rows;
     float x[EPL];
-    if (live && (softmax || BALANCE)) load_logits<EPL>(a.logits, a.dtype, row * a.ld, e0, E, a.vec, x);
+    if (live && softmax) load_logits<EPL>(a.logits, a.dtype, row * a.ld, e0, E, a.vec, x);
     int id = -1;
     float d = 0.f, xk = kNegInf;
-    if (live && sub < K && !(BALANCE && !a.dweights)) {
+    if (live && sub < K) {
       id = a.ids[row * K + sub];
       d = a.dweights[row * K + sub] * a.cfg.scale;
       if (id < 0 || id >= E) id = -1;
@@ -671,13 +326,11 @@ __global__ __launch_bounds__(256) void k_route_grad(const RouteGradArgs a) {
 #pragma unroll
     for (int i = 0; i < EPL; ++i) base_[i] = 0.f;
     float top = kNegInf;  // of the row
-    if ((softmax || BALANCE) && !live) {
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) x[i] = kNegInf;
-    }
-    float balance[EPL];
-    if constexpr (BALANCE) balance_terms<LPR, EPL>(x, softmax, counts, scale, z_scale, balance);
     if (softmax) {
+      if (!live) {
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) x[i] = kNegInf;
+      }
 #pragma unroll
       for (int i = 0; i < EPL; ++i) top = fmaxf(top, x[i]);
       top = lanes_max<LPR>(top);
@@ -726,10 +379,6 @@ __global__ __launch_bounds__(256) void k_route_grad(const RouteGradArgs a) {
 #pragma unroll
       for (int i = 0; i < EPL; ++i)
         if (at == i) base_[i] = vk;
-    }
-    if constexpr (BALANCE) {
-#pragma unroll
-      for (int i = 0; i < EPL; ++i) base_[i] += balance[i];
     }
     if (live) {
       const int64_t to = row * a.ld_out;
@@ -912,42 +561,10 @@ __global__ __launch_bounds__(kPlanThreads) void k_route_few(const RouteArgs a, c
   place_tile<LPR * EPL, false>(p, 0, 1);
 }
 
-// Whether every lane's EPL logits exist whole or not at all and can be moved at once.
-bool whole_lanes(const void *p, int64_t ld, int32_t E, int epl, int32_t dtype) {
-  const int bytes = dtype == AA_F32 ? 4 : 2, on = epl * bytes < 16 ? epl * bytes : 16;
-  return E % epl == 0 && ld * bytes % on == 0 && reinterpret_cast<uintptr_t>(p) % on == 0;
-}
-
 // No groups, or each of whole lanes, as many as a power of two.
 bool groups_of_lanes(const RouteArgs &a, int epl) {
   const int size = a.n_experts / a.cfg.n_groups, lanes = size / epl;
   return a.cfg.n_groups == 1 || (size % epl == 0 && (lanes & (lanes - 1)) == 0);
-}
-
-dim3 blocks_for(int32_t n_max, int rows_a_block) {
-  const int64_t want = ((int64_t)n_max + rows_a_block - 1) / rows_a_block;
-  return dim3((uint32_t)(want < (1 << 22) ? want : 1 << 22));  // (blocks take turns)
-}
-
-// The lanes of a row: 16 for up to most16 experts where they hold the choices too, else the wave (65,536 rows, 4 choices,
-// sigmoid, without and with a bias: 32 experts 10.4 / 16.2 us, a wave a row 31.3 / 41.3).
-template <typename Launch>
-hipError_t by_width(int32_t E, int32_t K, int32_t most16, Launch launch) {
-  using std::integral_constant;
-  if (K <= 16 && E <= most16) {
-    const integral_constant<int, 16> lpr;
-    if (E <= 16) return launch(lpr, integral_constant<int, 1>());
-    if (E <= 32) return launch(lpr, integral_constant<int, 2>());
-    if (E <= 64) return launch(lpr, integral_constant<int, 4>());
-    if (E <= 128) return launch(lpr, integral_constant<int, 8>());
-    return launch(lpr, integral_constant<int, 16>());
-  }
-  const integral_constant<int, 64> lpr;
-  if (E <= 64) return launch(lpr, integral_constant<int, 1>());
-  if (E <= 128) return launch(lpr, integral_constant<int, 2>());
-  if (E <= 256) return launch(lpr, integral_constant<int, 4>());
-  if (E <= 512) return launch(lpr, integral_constant<int, 8>());
-  return launch(lpr, integral_constant<int, 16>());
 }
 
 }  // namespace
@@ -997,38 +614,9 @@ hipError_t launch_route_grad(const RouteGradArgs &args, hipStream_t st) {
     constexpr int LPR = decltype(lpr)::value, EPL = decltype(epl)::value;
     a.vec = whole_lanes(a.logits, a.ld, a.n_experts, EPL, a.dtype) &&
             whole_lanes(a.dlogits, a.ld_out, a.n_experts, EPL, a.dtype);
-    hipLaunchKernelGGL((k_route_grad<LPR, EPL, false>), blocks_for(a.n_max, 4 * (kWave / LPR)), dim3(256), 0, st, a);
+    hipLaunchKernelGGL((k_route_grad<LPR, EPL>), blocks_for(a.n_max, 4 * (kWave / LPR)), dim3(256), 0, st, a);
     return hipGetLastError();
   });
-}
-
-hipError_t launch_balance_grad(const RouteGradArgs &args, hipStream_t st) {
-  RouteGradArgs a = args;
-  if (a.n_max == 0) return hipSuccess;
-  return by_width(a.n_experts, a.cfg.top_k, 128, [&](auto lpr, auto epl) {
-    constexpr int LPR = decltype(lpr)::value, EPL = decltype(epl)::value;
-    a.vec = whole_lanes(a.logits, a.ld, a.n_experts, EPL, a.dtype) &&
-            whole_lanes(a.dlogits, a.ld_out, a.n_experts, EPL, a.dtype);
-    const dim3 want = blocks_for(a.n_max, 4 * (kWave / LPR));
-    hipLaunchKernelGGL((k_route_grad<LPR, EPL, true>), want, dim3(256), 0, st, a);
-    return hipGetLastError();
-  });
-}
-
-hipError_t launch_balance(const BalanceArgs &args, hipStream_t st) {
-  BalanceArgs a = args;
-  int blocks = 0;
-  const hipError_t e = by_width(a.n_experts, a.cfg.top_k, 128, [&](auto lpr, auto epl) {
-    constexpr int LPR = decltype(lpr)::value, EPL = decltype(epl)::value, kThreads = kRowsThreads<EPL>, kRows = kThreads / LPR;
-    const int64_t want = ((int64_t)a.n_max + kRows - 1) / kRows;
-    blocks = (int)(want < 1 ? 1 : want < kBalanceBlocks ? want : kBalanceBlocks);
-    a.vec = whole_lanes(a.logits, a.ld, a.n_experts, EPL, a.dtype);
-    hipLaunchKernelGGL((k_balance_rows<LPR, EPL>), dim3(blocks), dim3(kThreads), 0, st, a);
-    return hipGetLastError();
-  });
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(k_balance_join, dim3(1), dim3(kBalanceThreads), 0, st, a, blocks);
-  return hipGetLastError();
 }
 
 hipError_t launch_expert_plan(const PlanArgs &a, hipStream_t st) {

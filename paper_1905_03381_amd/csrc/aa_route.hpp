@@ -40,7 +40,7 @@ struct RouteGradArgs {
 
 struct BalanceArgs {
   const void *logits;
-  int32_t dtype, vec;
+  int32_t dtype;
   int64_t ld;
   const int32_t *count;
   int32_t n_max, n_experts;
@@ -49,11 +49,14 @@ struct BalanceArgs {
   float coef, z_coef;
   int32_t *counts;
   float *share, *loss;
-  float *z_part;  // [blocks]
+  int32_t *done;  // a control word, 0 between calls
+  float *z_part;  // [kBalanceBlocks]
+  double *terms;  // [kBalanceTerms]
   float *part;    // [blocks][2][E up to a multiple of 4]: shares, then (int32) choices
 };
 
-constexpr int kBalanceBlocks = 256;
+constexpr int kBalanceBlocks = 512;
+constexpr int kBalanceTerms = AA_MAX_EXPERTS / 16 + 1;
 
 struct PlanArgs {
   const int32_t *ids;
