@@ -372,6 +372,10 @@ __device__ __forceinline__ Run<8> eight_columns(const f4 a, const f4 b) {
 
 __device__ __forceinline__ Run<4> four_columns(const f4 a) { return {{a[0], a[1], a[2], a[3]}}; }
 
+// The same by the unit's reciprocal (one unit of the last place; a division takes ten instructions, and 16,384 x 2048 ->
+// 8192 with gelu 560 us).
+__device__ __forceinline__ float sigmoid_near(float v) { return __builtin_amdgcn_rcpf(1.0f + __expf(-v)); }
+
 // 2 sqrt(2 / pi) (x + 0.044715 x^3): gelu(x) = x sigmoid of it.
 __device__ __forceinline__ float gelu_argument(float x) {
   constexpr float k = 1.5957691216057308f;
@@ -391,12 +395,12 @@ __device__ __forceinline__ void finish(const ProductArgs &a, int64_t q, int j, c
     }
     if (ACT == AA_ACT_SILU || ACT == AA_ACT_GELU) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) r.v[i] = v.v[i] * sigmoid_fast(ACT == AA_ACT_GELU ? gelu_argument(v.v[i]) : v.v[i]);
+      for (int i = 0; i < N; ++i) r.v[i] = v.v[i] * sigmoid_near(ACT == AA_ACT_GELU ? gelu_argument(v.v[i]) : v.v[i]);
     }
     if (DENSE && ACT != AA_ACT_GATED && a.pre) store_run(static_cast<T *>(a.pre) + q * a.ldpre + j, v, n);
     if (ACT == AA_ACT_GATED) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) r.v[i] = v.v[i] * sigmoid_fast(v.v[i]) * up.v[i];
+      for (int i = 0; i < N; ++i) r.v[i] = v.v[i] * (DENSE ? sigmoid_near(v.v[i]) : sigmoid_fast(v.v[i])) * up.v[i];
       if (a.pre) {
         T *h = static_cast<T *>(a.pre) + q * a.ldpre + j;
         store_run(h, v, n);
@@ -787,33 +791,28 @@ __global__ __launch_bounds__(WI *WJ *kWave, 2) void k_product(const ProductArgs 
 // result columns of one group (with AA_ACT_GATED half of them the gate's, half the same of up); its waves share the
 // summed dimension out in chunks of 64, straight from memory into the matrix instructions' registers with kAhead
 // chunks on their way and no meeting, and join their sums in LDS.  Rows go 16 MF at a time.
-template <typename T, int ACT, int NF, int MF, bool GATHER, bool DENSE>
+template <typename T, int ACT, int NF, int MF, bool GATHER>
 __global__ __launch_bounds__(256) void k_product_few(const ProductArgs a) {
   constexpr bool GATED = ACT == AA_ACT_GATED;
   constexpr int kWaves = 4, kOut = GATED ? NF / 2 : NF, kAhead = 4;
   __shared__ f4 sums[kWaves - 1][NF][MF][kWave];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  // the blockIdx.y-th group that has rows
   int e = -1, lo = 0, hi = 0;
-  if constexpr (DENSE) {
-    e = 0;
-    hi = rows_in_use(a.count, a.rows_max);
-  } else {
-    // the blockIdx.y-th group that has rows
-    for (int e0 = 0, seen = 0; e0 < a.n_experts && e < 0; e0 += kWave) {
-      const int at = min(e0 + lane, a.n_experts - 1);
-      const int from = a.offsets[at], to = a.offsets[at + 1];
-      const bool some = e0 + lane < a.n_experts && to > from;
-      const unsigned long long with = __ballot(some);
-      const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(with >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)with, 0u));
-      const unsigned long long mine = __ballot(some && seen + before == (int)blockIdx.y);
-      if (mine != 0ull) {
-        const int who = __ffsll((long long)mine) - 1;
-        e = e0 + who;
-        lo = __builtin_amdgcn_readlane(from, who);
-        hi = __builtin_amdgcn_readlane(to, who);
-      }
-      seen += __popcll(with);
+  for (int e0 = 0, seen = 0; e0 < a.n_experts && e < 0; e0 += kWave) {
+    const int at = min(e0 + lane, a.n_experts - 1);
+    const int from = a.offsets[at], to = a.offsets[at + 1];
+    const bool some = e0 + lane < a.n_experts && to > from;
+    const unsigned long long with = __ballot(some);
+    const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(with >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)with, 0u));
+    const unsigned long long mine = __ballot(some && seen + before == (int)blockIdx.y);
+    if (mine != 0ull) {
+      const int who = __ffsll((long long)mine) - 1;
+      e = e0 + who;
+      lo = __builtin_amdgcn_readlane(from, who);
+      hi = __builtin_amdgcn_readlane(to, who);
     }
+    seen += __popcll(with);
   }
   if (e < 0) return;
   e = __builtin_amdgcn_readfirstlane(e);
@@ -919,14 +918,8 @@ __global__ __launch_bounds__(256) void k_product_few(const ProductArgs a) {
 #pragma unroll
         for (int f = 0; f < kOut; ++f) {
           const int q = q0 + m * 16 + (lane & 15), c = j0 + f * 16 + (lane >> 4) * 4;
-          if (q >= hi || c >= a.d_out) continue;
-          if constexpr (DENSE) {
-            if (a.bias) {
-              acc[f][m] += bias_of(a, c, 0);
-              if (GATED) acc[GATED ? f + kOut : f][m] += bias_of(a, c, a.d_out);
-            }
-          }
-          finish<T, kForward, ACT, DENSE>(a, q, c, four_columns(acc[f][m]), four_columns(acc[GATED ? f + kOut : f][m]));
+          if (q < hi && c < a.d_out)
+            finish<T, kForward, ACT, false>(a, q, c, four_columns(acc[f][m]), four_columns(acc[GATED ? f + kOut : f][m]));
         }
     }
     __syncthreads();  // (the sums are read)
@@ -993,12 +986,12 @@ hipError_t launch_tiles(ProductArgs a, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <typename T, int ACT, bool DENSE, int NF, int MF>
+template <typename T, int ACT, int NF, int MF>
 hipError_t launch_few(const ProductArgs &a, hipStream_t st) {
   const int out_n = 16 * (ACT == AA_ACT_GATED ? NF / 2 : NF);
   const dim3 grid((a.d_out + out_n - 1) / out_n, a.rows_max < a.n_experts ? a.rows_max : a.n_experts), block(256);
-  if (!DENSE && a.order) hipLaunchKernelGGL((k_product_few<T, ACT, NF, MF, !DENSE, DENSE>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((k_product_few<T, ACT, NF, MF, false, DENSE>), grid, block, 0, st, a);
+  if (a.order) hipLaunchKernelGGL((k_product_few<T, ACT, NF, MF, true>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((k_product_few<T, ACT, NF, MF, false>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
@@ -1029,9 +1022,9 @@ hipError_t launch_product(const ProductArgs &a, hipStream_t st) {
     const double t256 = turns(n256, kUnits) * (steps * 1.75 + 5.0);
     const double t128 = turns(n128, 2 * kUnits) * (steps * (n128 <= kUnits ? 0.6 : 1.05) + 3.0);
     const double t32 = turns(n32, 2 * kUnits) * (steps * 0.42 + 3.5);
-    if constexpr (MODE == kForward) {
+    if constexpr (MODE == kForward && !DENSE) {
       if (rows <= 32 && n128 <= 320)
-        return rows <= 16 ? launch_few<T, ACT, DENSE, 2, 1>(a, st) : launch_few<T, ACT, DENSE, 2, 2>(a, st);
+        return rows <= 16 ? launch_few<T, ACT, 2, 1>(a, st) : launch_few<T, ACT, 2, 2>(a, st);
     }
     // (what goes through registers: the one tile that has them)
     if (!a.aligned) return launch_tiles<T, MODE, ACT, DENSE, 2, 2, 4, 4, 2, false>(a, st);
