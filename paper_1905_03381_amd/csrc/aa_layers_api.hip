@@ -23,6 +23,9 @@ int32_t check_norm(int32_t dtype, int32_t n_max, int32_t d, const int32_t *count
 
 bool is_dense_act(int32_t act) { return act >= AA_ACT_NONE && act <= AA_ACT_GELU; }
 
+// Results of so many bytes, half of the cache that all of the chip shares, are not there any more when they are read.
+constexpr int64_t kPassingBytes = 128ll << 20;
+
 // Rows of a dense layer.
 int32_t check_linear(int32_t dtype, const int32_t *count, int32_t n_max, int32_t d_out, int32_t act) {
   if (dtype != AA_BF16 && dtype != AA_F16) return AA_ERR_SHAPE;
@@ -160,6 +163,7 @@ int32_t aa_linear(const void *x, int32_t dtype, int64_t ldx, const int32_t *coun
   a.bias = bias;
   a.residual = residual;
   a.ldres = ldr;
+  a.passing = (int64_t)n_max * d_out * 2 >= kPassingBytes;
   return hip_status(launch_linear(a, dtype == AA_F16, as_stream(stream)));
 }
 

@@ -36,16 +36,15 @@ __device__ __forceinline__ void row_sums(float &a, float &b, int lane, float (*r
   a = lanes_sum<W>(a, lane);
   b = lanes_sum<W>(b, lane);
   if constexpr (TPR > kWave) {
-    static_assert(kThreads<TPR> == TPR, "one row a block");
-    const int wave = threadIdx.x / kWave;
+    const int wave = threadIdx.x / kWave, first = wave / (TPR / kWave) * (TPR / kWave);  // (of the row's waves)
     if (lane == 0) {
       room[wave][0] = a;
       room[wave][1] = b;
     }
     __syncthreads();
     const int w = lane & 15;  // (each 16 lanes add up the waves', at most 16)
-    a = lanes_sum<16>(w < TPR / kWave ? room[w][0] : 0.f, lane);
-    b = lanes_sum<16>(w < TPR / kWave ? room[w][1] : 0.f, lane);
+    a = lanes_sum<16>(w < TPR / kWave ? room[first + w][0] : 0.f, lane);
+    b = lanes_sum<16>(w < TPR / kWave ? room[first + w][1] : 0.f, lane);
   }
 }
 
@@ -104,18 +103,31 @@ __device__ __forceinline__ void row_moments(const Eight (&x)[NV], int d, int c0,
 }
 
 // NV lines of a row, `step` columns apart, from column c0 on; 0 past its end.  NARROW: the row may hold fewer than eight
-// columns.
-template <bool NARROW, typename T, int NV>
+// columns.  PASSING: past the caches.
+template <bool NARROW, bool PASSING = false, typename T, int NV>
 __device__ __forceinline__ void load_row(const T *row, int c0, int step, int d, Eight (&x)[NV]) {
 #pragma unroll
   for (int v = 0; v < NV; ++v) {
     const int c = c0 + v * step;
     Line<T> t = {};
     if (c < d) {
-      if (d % 8 == 0) t = *reinterpret_cast<const Line<T> *>(row + c);
-      else t = NARROW ? load_line(row + c, d - c) : load_line_early(row + c, d - c);
+      if (d % 8 != 0) t = NARROW ? load_line(row + c, d - c) : load_line_early(row + c, d - c);
+      else if (PASSING) t = __builtin_nontemporal_load(reinterpret_cast<const Line<T> *>(row + c));
+      else t = *reinterpret_cast<const Line<T> *>(row + c);
     }
     x[v] = to_eight<T>(t);
+  }
+}
+
+template <bool PASSING, typename T>
+__device__ __forceinline__ void store_line(T *p, const Eight &o, int n) {
+  if (PASSING && n >= 8) {
+    Line<T> t;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = (T)o.v[i];
+    __builtin_nontemporal_store(t, reinterpret_cast<Line<T> *>(p));
+  } else {
+    store8(p, o, n);
   }
 }
 
@@ -135,7 +147,7 @@ __device__ __forceinline__ void load_vector(const float *p, float none, int c0, 
 template <int TPR>
 constexpr bool kKeep = TPR < 1024;
 
-template <typename T, int TPR, int NV>
+template <typename T, int TPR, int NV, bool PASSING>
 __global__ __launch_bounds__(kThreads<TPR>) void k_layer_norm(const NormArgs a) {
   constexpr int kRows = kThreads<TPR> / TPR, kStepC = TPR * 8;
   __shared__ float room[2][kThreads<TPR> / kWave][2];
@@ -171,7 +183,7 @@ __global__ __launch_bounds__(kThreads<TPR>) void k_layer_norm(const NormArgs a) 
       }
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[v].v[i] = (x[v].v[i] - mean) * rstd * g[0].v[i] + b[0].v[i];
-      store8(out + c, x[v], d - c);
+      store_line<PASSING>(out + c, x[v], d - c);
     }
   }
 }
@@ -231,16 +243,22 @@ __global__ __launch_bounds__(kLongThreads) void k_layer_norm_long(const NormArgs
   }
 }
 
-template <typename T, int TPR, int NV>
-__global__ __launch_bounds__(kThreads<TPR>) void k_layer_norm_grad(const NormArgs a) {
-  constexpr int NT = kThreads<TPR>, kRows = NT / TPR, kStepC = TPR * 8;
+// Threads of a block of the gradient: there are as many blocks as the sums have parts, two a compute unit, and 16 waves there
+// are needed (19,960 x 1688 bf16: 82 us with 8).
+template <int TPR>
+constexpr int kGradThreads = TPR > 512 ? TPR : 512;
+
+template <typename T, int TPR, int NV, bool PASSING>
+__global__ __launch_bounds__(kGradThreads<TPR>) void k_layer_norm_grad(const NormArgs a) {
+  constexpr int NT = kGradThreads<TPR>, kRows = NT / TPR, kStepC = TPR * 8;
+  constexpr bool kNarrow = TPR == 16;
   __shared__ float room[2][NT / kWave][2];
   __shared__ float joined[kRows > 1 ? kRows : 1][kRows > 1 ? NV * kStepC : 1];
   const int rows = rows_in_use(a.count, a.n_max), d = a.d;
   const int lane = threadIdx.x & 63, c0 = (int)threadIdx.x % TPR * 8;
   const bool sums = a.dgamma || a.dbeta;
   Eight gamma[NV], dg[NV], db[NV];
-  if (kKeep<TPR>) load_vector<TPR == 16>(a.gamma, 1.f, c0, kStepC, d, gamma);
+  if (kKeep<TPR>) load_vector<kNarrow>(a.gamma, 1.f, c0, kStepC, d, gamma);
 #pragma unroll
   for (int v = 0; v < NV; ++v)
 #pragma unroll
@@ -248,12 +266,22 @@ __global__ __launch_bounds__(kThreads<TPR>) void k_layer_norm_grad(const NormArg
   int turn = 0;
   for (int64_t base = (int64_t)blockIdx.x * kRows; base < rows; base += (int64_t)gridDim.x * kRows, turn ^= 1) {
     const uint32_t row = row_of<TPR>(base);
-    if (row >= (uint32_t)rows) break;
+    // (threads whose row is past the last go along: with a dy of 0 they add nothing)
+    const bool live = row < (uint32_t)rows;
     Eight x[NV], dy[NV];
-    load_row<TPR == 16>(static_cast<const T *>(a.x) + (int64_t)row * a.ldx, c0, kStepC, d, x);
-    load_row<TPR == 16>(static_cast<const T *>(a.dout) + (int64_t)row * a.lddo, c0, kStepC, d, dy);
-    const float mean = a.mean[row], rstd = a.rstd[row];
-    if (!kKeep<TPR>) load_vector<TPR == 16>(a.gamma, 1.f, c0, kStepC, d, gamma);
+    float mean = 0.f, rstd = 0.f;
+    if (live) {
+      load_row<kNarrow, PASSING>(static_cast<const T *>(a.x) + (int64_t)row * a.ldx, c0, kStepC, d, x);
+      load_row<kNarrow, PASSING>(static_cast<const T *>(a.dout) + (int64_t)row * a.lddo, c0, kStepC, d, dy);
+      mean = a.mean[row];
+      rstd = a.rstd[row];
+    } else {
+#pragma unroll
+      for (int v = 0; v < NV; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[v].v[i] = dy[v].v[i] = 0.f;
+    }
+    if (!kKeep<TPR>) load_vector<kNarrow>(a.gamma, 1.f, c0, kStepC, d, gamma);
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int v = 0; v < NV; ++v)
@@ -268,6 +296,7 @@ __global__ __launch_bounds__(kThreads<TPR>) void k_layer_norm_grad(const NormArg
         s2 += g * xh;
       }
     row_sums<TPR>(s1, s2, lane, room[turn]);
+    if (!live) continue;
     s1 /= (float)d;
     s2 /= (float)d;
     T *out = static_cast<T *>(a.out) + (int64_t)row * a.ldo;
@@ -281,11 +310,11 @@ __global__ __launch_bounds__(kThreads<TPR>) void k_layer_norm_grad(const NormArg
       for (int i = 0; i < 8; ++i) r.v[i] = rstd * (dy[v].v[i] - s1 - x[v].v[i] * s2);
       if (a.residual) {
         Eight add[1];
-        load_row<TPR == 16>(res, c, 0, d, add);
+        load_row<kNarrow, PASSING>(res, c, 0, d, add);
 #pragma unroll
         for (int i = 0; i < 8; ++i) r.v[i] += add[0].v[i];
       }
-      store8(out + c, r, d - c);
+      store_line<PASSING>(out + c, r, d - c);
     }
   }
   if (!sums) return;
@@ -437,6 +466,14 @@ hipError_t by_row_width(int32_t d, Launch launch, Long long_rows) {
   return long_rows();
 }
 
+// Results of so many bytes, half of the cache that all of the chip shares, are not there any more when they are read: they pass
+// it by, and in the gradient so do the rows (16,384 x 8192 bf16 with a residual 203 -> 186 us; 30,000 x 4096 96 -> 94, its rows
+// too 97; 8191 x 1021 f32, 33 MB, 25.1 and 26.6).
+template <typename T>
+bool passing(const NormArgs &a) {
+  return (int64_t)a.n_max * a.d * (int64_t)sizeof(T) >= 128ll << 20;
+}
+
 template <typename T>
 hipError_t layer_norm(const NormArgs &a, hipStream_t st) {
   return by_row_width(
@@ -444,8 +481,9 @@ hipError_t layer_norm(const NormArgs &a, hipStream_t st) {
       [&](auto tpr, auto nv) {
         constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, kRows = kThreads<TPR> / TPR;
         const int64_t want = ((int64_t)a.n_max + kRows - 1) / kRows, most = (int64_t)kUnits * 2048 / kThreads<TPR>;
-        hipLaunchKernelGGL((k_layer_norm<T, TPR, NV>), dim3((uint32_t)(want < most ? want : most)),
-                           dim3(kThreads<TPR>), 0, st, a);
+        const dim3 grid((uint32_t)(want < most ? want : most)), block(kThreads<TPR>);
+        if (passing<T>(a)) hipLaunchKernelGGL((k_layer_norm<T, TPR, NV, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((k_layer_norm<T, TPR, NV, false>), grid, block, 0, st, a);
         return hipGetLastError();
       },
       [&] {
@@ -460,10 +498,12 @@ hipError_t layer_norm_grad(const NormArgs &a, hipStream_t st) {
   return by_row_width(
       a.d,
       [&](auto tpr, auto nv) {
-        constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, kRows = kThreads<TPR> / TPR;
+        constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, kRows = kGradThreads<TPR> / TPR;
         const int64_t want = ((int64_t)a.n_max + kRows - 1) / kRows;
         const int parts = (int)(want < most ? want : most);
-        hipLaunchKernelGGL((k_layer_norm_grad<T, TPR, NV>), dim3(parts), dim3(kThreads<TPR>), 0, st, a);
+        const dim3 grid(parts), block(kGradThreads<TPR>);
+        if (passing<T>(a)) hipLaunchKernelGGL((k_layer_norm_grad<T, TPR, NV, true>), grid, block, 0, st, a);
+        else hipLaunchKernelGGL((k_layer_norm_grad<T, TPR, NV, false>), grid, block, 0, st, a);
         const hipError_t e = hipGetLastError();
         return e != hipSuccess ? e : join_columns(a, parts, st);
       },
