@@ -8,6 +8,7 @@
     python -m paper_1905_03381_amd.workloads rho           # dense fused step at fixed keep rates
     python -m paper_1905_03381_amd.workloads score         # dense scoring pass at growing pool sizes
     python -m paper_1905_03381_amd.workloads experts       # a Boss with a block of experts on the kept rows
+    python -m paper_1905_03381_amd.workloads boss          # a Boss of normed blocks trained with AdamW on the kept rows
 
 Each prints one JSON line: the stages of the workload with their time per call (HIP events
 on the launch stream, median of the repeats), the bytes each stage has to move and the
@@ -451,7 +452,81 @@ def experts(a, torch, api, synth):
             "kept_per_pool": m, "loss_first": curve[0], "loss_last": curve[-1]}
 
 
-WORKLOADS = {"experts": experts, "rho": rho, "sparse": sparse, "images": images, "translation": translation, "sk": sk,
+def boss(a, torch, api, synth):
+    """A Boss of an input layer, two normed blocks of 16 gated experts (two a row, balance loss) and a read-out, trained by
+    AdamW with clipping and states in 8 bits on the rows the Assistant keeps.
+
+    n rows of 512 in pools of 16,384 (fewer if n is smaller).  The host never waits inside a step."""
+    from .boss import AdamW, Boss
+    n, d, width, f, E, K = a.n or 262_144, 512, 1024, 512, 16, 2
+    P = min(16_384, n // 4)
+    X, y, _ = synth.dense_svm(n=n, d=d, threads=a.threads)
+    X *= d ** 0.5
+    Xd, yd = torch.from_numpy(X).cuda(), torch.from_numpy(y).cuda()
+    Xb, F = Xd.to(torch.bfloat16), api.Features.dense(Xd)
+    perm = torch.from_numpy(synth.epoch_permutation(n, seed=7, epoch=0)).cuda()
+    model = Boss(P, d, width, f, 1, E, K, p=0.1, balance=0.01, z_loss=1e-4)
+    optimizer = AdamW(model, 1e-3, weight_decay=0.01, max_norm=1.0, state_bits=8)
+    z = lambda *s, t=torch.float32: torch.zeros(*s, dtype=t, device="cuda")
+    ws, phi, b, T = api.Workspace(P, d), z(d), z(1), z(1)
+    seen, cnt = z(1, t=torch.int32), z(1, t=torch.int32)
+    prob, keep, pos, ids = z(P), z(P, t=torch.uint8), z(P, t=torch.int32), z(P, t=torch.int32)
+    x, out, dout = (z(P, w, t=torch.bfloat16) for w in (d, 1, 1))
+    row, loss = torch.arange(P, device="cuda"), z(P)
+
+    def generate(step):
+        t = step % steps
+        idx = perm[t * P:(t + 1) * P]
+        api.score_shrink(F, idx, P, phi, b, 0.1, 42, step, None, prob, keep, pos, cnt, ws)
+        api.gather(Xb, 2 * d, idx, pos, cnt, P, x, ids)
+
+    def forward(step):
+        model.forward(x, cnt, step, out)
+        yk, live = yd[ids.long()], row < cnt
+        margin = yk * out[:, 0].float()
+        loss.copy_(torch.where(live, (1 - margin).clamp(min=0), 0.0))
+        dout[:, 0] = torch.where(live & (margin < 1), -yk / cnt.clamp(min=1), 0.0)
+
+    def backward(step):
+        model.backward(x, cnt, step, dout)
+
+    def update(step):
+        optimizer.step(cnt)
+
+    def assistant(step):
+        api.threshold_update(loss, cnt, P, 0.9, T, seen)
+        api.assistant_update(F, ids, cnt, P, loss, T, phi, b, 0.1, 0.0, ws)
+
+    steps, kept, losses, times = max(1, n // P), [], [], {}
+    parts = (generate, forward, backward, update, assistant)
+    for step in range(3 * steps):                   # three epochs; keep draws and masks go by the step
+        marks = [torch.cuda.Event(enable_timing=True) for _ in range(len(parts) + 1)]
+        marks[0].record()
+        for part, after in zip(parts, marks[1:]):
+            part(step)
+            after.record()
+        if step:                                    # the first step loads the kernels
+            for part, lo, hi in zip(parts, marks, marks[1:]):
+                times.setdefault(part.__name__, []).append((lo, hi))
+        kept.append(cnt.clone())
+        losses.append(loss.sum() / cnt.clamp(min=1))
+    torch.cuda.synchronize()
+    us = {k: float(np.median([lo.elapsed_time(hi) * 1e3 for lo, hi in v])) for k, v in times.items()}
+    m = float(torch.stack(kept).float().mean())
+    weights = sum(w.numel() for w in model.weights())
+    flops = 2 * m * (d * width + 2 * (E * width + K * 3 * f * width))
+    curve = torch.stack(losses).view(-1).tolist()
+    stages = [_stage("score + keep + gather of the kept rows (bf16)", us["generate"], P * (4 * d + 9) + m * 4 * d),
+              _stage("Boss and loss", us["forward"], note=f"{flops / us['forward'] / 1e6:.0f} TFLOP/s"),
+              _stage("gradients", us["backward"], note=f"{2 * flops / us['backward'] / 1e6:.0f} TFLOP/s"),
+              _stage(f"AdamW on {weights} weights, clipped", us["update"], weights * (8 + 4 + 4 + 2 + 4 + 16 / 256)),
+              _stage("threshold and Assistant update", us["assistant"])]
+    return {"workload": f"Boss of two blocks of {E} experts ({K} a row), n={n} d={d} width={width} f={f} pool={P}",
+            "stages": stages, "kept_per_pool": m, "loss_first": curve[0], "loss_last": curve[-1],
+            "balance_loss": [block.balance_loss.tolist() for block in model.blocks]}
+
+
+WORKLOADS = {"boss": boss, "experts": experts, "rho": rho, "sparse": sparse, "images": images, "translation": translation, "sk": sk,
              "stale": stale, "score": score}
 
 

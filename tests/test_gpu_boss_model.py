@@ -1,0 +1,184 @@
+"""The operators around a block of experts together, as boss.Boss and boss.AdamW use them: gradients of the whole model
+against a plain one in 64 bits, updates against torch's, a step in a graph.
+
+Tolerance of the model's gradients: every buffer between two operators is rounded to 2^-8 of its values at most (bf16) and passes
+at most about 14 buffers on its way (input layer, two blocks of norm, logits or hidden rows and sum, last norm, read-out, and back);
+the operators between them are near isometries here (norms, residuals of unit size), so that in the 2-norm they add up to at
+most 14 2^-8 = 5.5 %; f16 has an eighth of that."""
+import numpy as np
+import pytest
+import torch
+
+from layers_ref import BF16, F16, F32, U32, check, device_count, f64, normal
+from paper_1905_03381_amd import api
+from paper_1905_03381_amd.boss import AdamW, Boss, ExpertBlock
+
+pytestmark = pytest.mark.gpu
+
+D64 = torch.float64
+
+
+def plain_block(block, x, i, weights, m):
+    """The block of experts with the choices that it made (no dropout)."""
+    router, gate_up, down, gamma, beta = weights
+    h = torch.nn.functional.layer_norm(x, x.shape[1:], gamma, beta, 1e-5)
+    logits = h @ router[0].t()
+    ids = block.ids[:m].cpu().long()
+    s = torch.softmax(logits, 1).gather(1, ids)
+    s = s / s.sum(1, keepdim=True)
+    out = x
+    f = down.shape[2]
+    for k in range(ids.shape[1]):
+        g = torch.bmm(gate_up[ids[:, k]], h.unsqueeze(2)).squeeze(2)
+        y = torch.bmm(down[ids[:, k]], (torch.nn.functional.silu(g[:, :f]) * g[:, f:]).unsqueeze(2)).squeeze(2)
+        out = out + s[:, k:k + 1] * y
+    coef, z = block.balance
+    E = router.shape[1]
+    counts = torch.bincount(ids.view(-1), minlength=E).double()
+    loss = coef * E / (m * ids.shape[1]) * (counts * torch.softmax(logits, 1).mean(0)).sum()
+    return out, loss + z * (torch.logsumexp(logits, 1) ** 2).mean()
+
+
+def plain(model, x, m):
+    """out and the balance losses, and the weights that their gradients are asked of."""
+    w = [v.detach().cpu().to(D64).requires_grad_(True) for v in model.weights()]
+    h = torch.nn.functional.gelu(x @ w[0].t() + w[1], approximate="tanh")
+    total, at = 0.0, 2
+    for i, block in enumerate(model.blocks):
+        h, loss = plain_block(block, h, i, w[at:at + 5], m)
+        total, at = total + loss, at + 5
+    h = torch.nn.functional.layer_norm(h, h.shape[1:], w[at], w[at + 1], 1e-5)
+    return h @ w[at + 2].t() + w[at + 3], total, w
+
+
+@pytest.mark.parametrize("dtype,off", [(BF16, 14 * 2.0 ** -8), (F16, 14 * 2.0 ** -11)])
+@pytest.mark.parametrize("n_max,count", [(300, 300), (300, 190), (24, 24)])
+def test_gradients_of_the_model(dtype, off, n_max, count):
+    d_in, d, f, d_out, E, K = 40, 64, 48, 3, 8, 2
+    model = Boss(n_max, d_in, d, f, d_out, E, K, dtype=dtype, balance=0.3, z_loss=0.01)
+    for i, (w, g) in enumerate(zip(model.weights(), model.grads)):
+        if w.dim() == 1:  # (weights of norms and biases that are not 1 and 0)
+            w.add_(normal(tuple(w.shape), F32, i, 0.1).cuda())
+    x, dout = normal((n_max, d_in), dtype, 3).cuda(), normal((n_max, d_out), dtype, 4, 1 / count).cuda()
+    out = torch.full((n_max, d_out), 7.0, dtype=dtype, device="cuda")
+    cnt = device_count(count)
+    model.forward(x, cnt, 0, out)
+    model.backward(x, cnt, 0, dout)
+    want, balance, weights = plain(model, x[:count].cpu().to(D64), count)
+    ((want * dout[:count].cpu().to(D64)).sum() + balance).backward()
+    norm = np.linalg.norm
+    got = f64(out)[:count]
+    assert norm(got - want.detach().numpy()) <= off * norm(want.detach().numpy())
+    assert (f64(out)[count:] == 7).all()
+    for i, (g, w) in enumerate(zip(model.grads, weights)):
+        g, w = f64(g), w.grad.numpy()
+        assert norm(g - w) <= off * norm(w), (i, tuple(w.shape), norm(g - w) / norm(w))
+    losses = sum(float(b.balance_loss.sum()) for b in model.blocks)
+    assert abs(losses - float(balance.detach())) <= off * float(balance.detach())
+
+
+def test_a_block_without_norm_and_balance_is_as_it_was():
+    """The options off: the calls and results of before."""
+    n, d = 50, 64
+    x, dout = normal((n, d), BF16, 3).cuda(), normal((n, d), BF16, 4).cuda()
+    a, b = ExpertBlock(n, d, 48, 8, 2, p=0.2), ExpertBlock(n, d, 48, 8, 2, p=0.2, balance=0.0, norm=False)
+    assert len(a.weights()) == len(a.grads) == 3
+    for block in (a, b):
+        block.o, block.d = torch.zeros_like(x), torch.zeros_like(x)
+        block.forward(x, device_count(n), 5, block.o)
+        block.backward(x, device_count(n), 5, dout, block.d)
+    assert torch.equal(a.o, b.o) and torch.equal(a.d, b.d)
+
+
+def test_fewer_rows_than_the_model_are_refused():
+    model, x = Boss(40, 16, 32, 16, 2, 4, 2), torch.zeros(39, 16, dtype=BF16, device="cuda")
+    with pytest.raises(api.AAError):
+        model.forward(x, device_count(39), 0, torch.zeros(40, 2, dtype=BF16, device="cuda"))
+
+
+def small_model(n_max=64):
+    return Boss(n_max, 24, 32, 16, 2, 4, 2, layers=1, balance=0.1)
+
+
+def test_updates_are_torchs():
+    """Three updates against torch.optim.AdamW in 64 bits on the same gradients: each is off by 40 U of the step's size and 4 U
+    of the parameter, and hands that on."""
+    model = small_model()
+    opt = AdamW(model, 1e-2, weight_decay=0.1, max_norm=0.5)
+    params = [torch.nn.Parameter(m.detach().cpu().to(D64)) for m in opt.masters]
+    f = lambda v: float(np.float32(v))
+    groups = [dict(params=[p], weight_decay=0.0 if p.dim() == 1 else f(0.1)) for p in params]
+    theirs = torch.optim.AdamW(groups, lr=f(1e-2), betas=(f(0.9), f(0.999)), eps=f(1e-8))
+    for step in range(3):
+        for i, (g, p) in enumerate(zip(model.grads, params)):
+            g.copy_(normal(tuple(g.shape), F32, 100 * step + i))
+            p.grad = g.detach().cpu().to(D64)
+        opt.step(device_count(5))
+        torch.nn.utils.clip_grad_norm_(params, 0.5)
+        theirs.step()
+    assert int(opt.t.item()) == 3
+    for m, p, w in zip(opt.masters, params, model.weights()):
+        # (clip_grad_norm_ divides by the norm + 1e-6: 2e-8 of these norms, above 50; a step is at most about lr)
+        check(m, p.detach().numpy(), 3 * (1e-2 * (60 * U32 + 1e-6) + 4 * U32 * np.abs(p.detach().numpy())), "master")
+        assert torch.equal(w, m.to(w.dtype))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_an_empty_batch_changes_nothing(bits):
+    model = small_model()
+    opt = AdamW(model, 1e-2, max_norm=1.0, state_bits=bits)
+    x, dout = normal((64, 24), BF16, 3).cuda(), normal((64, 2), BF16, 4).cuda()
+    out, cnt = torch.zeros(64, 2, dtype=BF16, device="cuda"), device_count(0)
+    kept = [w.clone() for w in model.weights()]
+    model.forward(x, cnt, 0, out)
+    model.backward(x, cnt, 0, dout)
+    assert all((g == 0).all() for g in model.grads)
+    opt.step(cnt)
+    assert all(torch.equal(a, b) for a, b in zip(kept, model.weights())) and int(opt.t.item()) == 0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_step_in_a_graph(bits):
+    """Forward, backward and update captured once and replayed on other batches, next to an eager model's."""
+    n = 200
+    make = lambda: Boss(n, 24, 64, 32, 2, 8, 2, layers=2, balance=0.1, p=0.1)
+    a, b = make(), make()
+    oa, ob = (AdamW(m, 1e-2, weight_decay=0.1, max_norm=0.5, state_bits=bits) for m in (a, b))
+    x, dout = torch.zeros(n, 24, dtype=BF16, device="cuda"), torch.zeros(n, 2, dtype=BF16, device="cuda")
+    out_a, out_b, cnt = torch.zeros_like(dout), torch.zeros_like(dout), device_count(0)
+
+    def step(model, opt, out):
+        model.forward(x, cnt, 3, out)
+        model.backward(x, cnt, 3, dout)
+        opt.step(cnt)
+
+    step(a, oa, out_a)   # (loads the kernels; an empty batch)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step(a, oa, out_a)
+    for turn, m in enumerate((n, 120, 0, 1, n)):
+        x.copy_(normal((n, 24), BF16, 10 + turn)), dout.copy_(normal((n, 2), BF16, 30 + turn)), cnt.fill_(m)
+        g.replay()
+        torch.cuda.synchronize()
+        step(b, ob, out_b)
+        torch.cuda.synchronize()
+        assert torch.equal(out_a[:m], out_b[:m]) and torch.equal(oa.norm, ob.norm)
+        for s, t in zip(a.weights() + oa.masters + a.grads, b.weights() + ob.masters + b.grads):
+            assert torch.equal(s, t)
+        assert int(oa.t.item()) == int(ob.t.item())
+    assert int(oa.t.item()) == 4
+
+
+def test_state_bits_are_checked():
+    with pytest.raises(api.AAError):
+        AdamW(small_model(), 1e-3, state_bits=16)
+
+
+def test_the_workload_runs(capsys):
+    import json
+    from paper_1905_03381_amd import workloads
+    workloads.main(["boss", "--n", "16384", "--threads", "4"])
+    got = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
+    assert len(got["stages"]) == 5 and got["kept_per_pool"] > 0
+    assert all(np.isfinite(v) for v in [got["loss_first"], got["loss_last"]] + sum(got["balance_loss"], []))
