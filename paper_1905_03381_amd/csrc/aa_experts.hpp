@@ -31,7 +31,7 @@ struct ProductArgs {
   const float *bias;
   const void *residual;
   int64_t ldres;
-  int32_t passing;  // results are stored past the caches
+  int32_t passing, passing_pre;  // results, pre are stored past the caches
 };
 
 hipError_t launch_expert_forward(const ProductArgs &a, bool f16, hipStream_t st);

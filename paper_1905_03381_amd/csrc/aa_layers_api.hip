@@ -23,7 +23,8 @@ int32_t check_norm(int32_t dtype, int32_t n_max, int32_t d, const int32_t *count
 
 bool is_dense_act(int32_t act) { return act >= AA_ACT_NONE && act <= AA_ACT_GELU; }
 
-// Results of so many bytes, half of the cache that all of the chip shares, are not there any more when they are read.
+// Results of so many bytes, half of the cache that all of the chip shares, are not there any more when they are read.  (Rows
+// off 16-byte boundaries fill lines in parts, which the caches put together: 4422 x 1024 -> 8018 with pre 89 us, past them 124.)
 constexpr int64_t kPassingBytes = 128ll << 20;
 
 // Rows of a dense layer.
@@ -163,7 +164,8 @@ int32_t aa_linear(const void *x, int32_t dtype, int64_t ldx, const int32_t *coun
   a.bias = bias;
   a.residual = residual;
   a.ldres = ldr;
-  a.passing = (int64_t)n_max * d_out * 2 >= kPassingBytes;
+  a.passing = rows_on_16(out, ldo, 2) && (int64_t)n_max * d_out * 2 >= kPassingBytes;
+  a.passing_pre = pre && rows_on_16(pre, ldpre, 2) && (int64_t)n_max * wide * 2 >= kPassingBytes;
   return hip_status(launch_linear(a, dtype == AA_F16, as_stream(stream)));
 }
 

@@ -343,6 +343,12 @@ __device__ __forceinline__ void store_run(T *p, const Run<N> &x, int n) {
 }
 
 template <typename T, int N>
+__device__ __forceinline__ void store_dense(bool passing, T *p, const Run<N> &x, int n) {
+  if (passing) store_run<T, N, true>(p, x, n);
+  else store_run(p, x, n);
+}
+
+template <typename T, int N>
 __device__ __forceinline__ Run<N> load_run(const T *p, int n) {
   constexpr int kPer = N * sizeof(T) < 16 ? N : 16 / sizeof(T);
   typedef T Line __attribute__((ext_vector_type(kPer), aligned(sizeof(T))));
@@ -401,14 +407,14 @@ __device__ __forceinline__ void finish(const ProductArgs &a, int64_t q, int j, c
 #pragma unroll
       for (int i = 0; i < N; ++i) r.v[i] = v.v[i] * sigmoid_near(ACT == AA_ACT_GELU ? gelu_argument(v.v[i]) : v.v[i]);
     }
-    if (DENSE && ACT != AA_ACT_GATED && a.pre) store_run<T, N, true>(static_cast<T *>(a.pre) + q * a.ldpre + j, v, n);
+    if (DENSE && ACT != AA_ACT_GATED && a.pre) store_dense(a.passing_pre, static_cast<T *>(a.pre) + q * a.ldpre + j, v, n);
     if (ACT == AA_ACT_GATED) {
 #pragma unroll
       for (int i = 0; i < N; ++i) r.v[i] = v.v[i] * (DENSE ? sigmoid_near(v.v[i]) : sigmoid_fast(v.v[i])) * up.v[i];
       if (a.pre) {
         T *h = static_cast<T *>(a.pre) + q * a.ldpre + j;
-        store_run<T, N, DENSE>(h, v, n);
-        store_run<T, N, DENSE>(h + a.d_out, up, n);
+        store_dense(DENSE && a.passing_pre, h, v, n);
+        store_dense(DENSE && a.passing_pre, h + a.d_out, up, n);
       }
     }
     if (DENSE && a.residual) {
@@ -432,8 +438,7 @@ __device__ __forceinline__ void finish(const ProductArgs &a, int64_t q, int j, c
     }
     store_run(o + a.d_in, du, n);
   }
-  if (DENSE && a.passing) store_run<T, N, true>(o, r, n);
-  else store_run(o, r, n);
+  store_dense(DENSE && a.passing, o, r, n);
 }
 
 template <typename T, int N>
