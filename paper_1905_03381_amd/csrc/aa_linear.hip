@@ -49,12 +49,26 @@ __global__ __launch_bounds__(256) void k_act_grad(const ActGradArgs a) {
   Eight sum, sum_up;
 #pragma unroll
   for (int i = 0; i < 8; ++i) sum.v[i] = sum_up.v[i] = 0.f;
+  const bool words = d % 8 != 0;
+  const auto load = [&](const T *p, int n) __attribute__((always_inline)) {
+    return words && n >= 8 ? to_eight<T>(load_words(p)) : load8(p, n);
+  };
+  const auto store = [&](T *p, const Eight &v, int n) __attribute__((always_inline)) {
+    if (words && n >= 8) {
+      Line<T> t;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[i] = (T)v.v[i];
+      store_words(p, t);
+    } else {
+      store8(p, v, n);
+    }
+  };
   if (c < d) {
     const int n = d - (int)c;
     for (int64_t row = (int64_t)blockIdx.y * kRows + r0; row < rows; row += (int64_t)a.parts * kRows) {
-      Eight g = load8(static_cast<const T *>(a.dout) + row * a.lddo + c, n), h, up;
-      if (ACT != AA_ACT_NONE) h = load8(static_cast<const T *>(a.pre) + row * a.ldpre + c, n);
-      if (ACT == AA_ACT_GATED) up = load8(static_cast<const T *>(a.pre) + row * a.ldpre + d + c, n);
+      Eight g = load(static_cast<const T *>(a.dout) + row * a.lddo + c, n), h, up;
+      if (ACT != AA_ACT_NONE) h = load(static_cast<const T *>(a.pre) + row * a.ldpre + c, n);
+      if (ACT == AA_ACT_GATED) up = load(static_cast<const T *>(a.pre) + row * a.ldpre + d + c, n);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         float du = 0.f;
@@ -67,8 +81,8 @@ __global__ __launch_bounds__(256) void k_act_grad(const ActGradArgs a) {
       }
       if (a.dpre) {
         T *out = static_cast<T *>(a.dpre) + row * a.lddp + c;
-        store8(out, g, n);
-        if (ACT == AA_ACT_GATED) store8(out + d, up, n);
+        store(out, g, n);
+        if (ACT == AA_ACT_GATED) store(out + d, up, n);
       }
     }
   }

@@ -25,6 +25,7 @@
 #pragma once
 
 #include "aa_experts.hpp"
+#include "aa_lines.hpp"
 #include "aa_route.hpp"
 
 #include <type_traits>
@@ -344,8 +345,20 @@ __device__ __forceinline__ void store_run(T *p, const Run<N> &x, int n) {
 
 template <typename T, int N>
 __device__ __forceinline__ void store_dense(bool passing, T *p, const Run<N> &x, int n) {
-  if (passing) store_run<T, N, true>(p, x, n);
-  else store_run(p, x, n);
+  if (passing) {
+    store_run<T, N, true>(p, x, n);
+    return;
+  }
+  if constexpr (N == 8) {  // (rows of odd widths: half of them begin inside a word of four bytes)
+    if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 2)) {
+      Line<T> t;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[i] = (T)x.v[i];
+      store_words(p, t);
+      return;
+    }
+  }
+  store_run(p, x, n);
 }
 
 template <typename T, int N>
@@ -418,7 +431,15 @@ __device__ __forceinline__ void finish(const ProductArgs &a, int64_t q, int j, c
       }
     }
     if (DENSE && a.residual) {
-      const Run<N> add = load_run<T, N>(static_cast<const T *>(a.residual) + q * a.ldres + j, n);
+      const T *p = static_cast<const T *>(a.residual) + q * a.ldres + j;
+      Run<N> add;
+      if (N == 8 && n >= 8) {
+        const Line<T> t = load_words(p);
+#pragma unroll
+        for (int i = 0; i < N; ++i) add.v[i] = (float)t[i];
+      } else {
+        add = load_run<T, N>(p, n);
+      }
 #pragma unroll
       for (int i = 0; i < N; ++i) r.v[i] += add.v[i];
     }
