@@ -615,89 +615,119 @@ class LayerWorkspace:
         _take(self, int(lib().aa_layer_workspace_bytes(d_max)), device)
 
 
+# (Calls of a row or a few take as long as the host: each of these asks a tensor for six things where _matrix and _array ask for
+# ten.  What is unusual goes to those, for their messages.)
+_F32, _I32, _Tensor = torch.float32, torch.int32, torch.Tensor
+
+
 def _count(count):
-    return _array(count, "count", torch.int32, least=1)
+    if count is None:
+        return None
+    if type(count) is _Tensor and count.dtype is _I32 and count.is_cuda and count.dim() == 1 and count.numel() == 1:
+        return count.data_ptr()
+    return _array(count, "count", _I32, least=1)
+
+
+def _vector(t, name, n):
+    """Pointer of n neighbouring float32 values; None stays None."""
+    if t is None:
+        return None
+    if type(t) is _Tensor and t.dtype is _F32 and t.is_cuda and t.shape == (n,) and t.is_contiguous():
+        return t.data_ptr()
+    return _array(t, name, _F32, (n,))
+
+
+def _rows_like(t, name, dtype, n, d):
+    """(pointer, row stride) of n rows of d neighbouring columns of the given type (or more rows)."""
+    if type(t) is _Tensor and t.dtype is dtype and t.is_cuda and t.shape == (n, d):
+        ld, step = t.stride()
+        if step == 1:
+            return t.data_ptr(), ld if n > 1 else d
+    return _matrix(t, name, dtype, d, n)
+
+
+def _first_rows(t, name, types):
+    """(type code, pointer, row stride, rows, columns) of the matrix that a call's sizes and type come from."""
+    if type(t) is _Tensor and t.is_cuda and t.dim() == 2:
+        code = types.get(t.dtype)
+        n, d = t.shape
+        ld, step = t.stride()
+        if code is not None and step == 1:
+            return code, t.data_ptr(), ld if n > 1 else d, n, d
+    code = _type(t, name, types is _HALVES)
+    p, ld = _matrix(t, name)
+    return code, p, ld, t.shape[0], t.shape[1]
+
+
+_HALVES = {t: c for t, c in DTYPES.items() if t is not _F32}
 
 
 def layer_norm(x, gamma, beta, eps, count, out, mean=None, rstd=None):
     """gamma, beta: float32 [d] or None (1 and 0); mean, rstd: float32 [n], for the backward pass."""
-    dt = _type(x, "x")
-    xp, ldx = _matrix(x, "x")
-    n, d = x.shape
-    op, ldo = _matrix(out, "out", x.dtype, d, n)
-    _check(lib().aa_layer_norm(xp, dt, ldx, _count(count), n, d, _array(gamma, "gamma", torch.float32, (d,)),
-                               _array(beta, "beta", torch.float32, (d,)), eps, op, ldo,
-                               _array(mean, "mean", torch.float32, (n,)), _array(rstd, "rstd", torch.float32, (n,)),
-                               _stream()), "aa_layer_norm")
+    dt, xp, ldx, n, d = _first_rows(x, "x", DTYPES)
+    op, ldo = _rows_like(out, "out", x.dtype, n, d)
+    _check(lib().aa_layer_norm(xp, dt, ldx, _count(count), n, d, _vector(gamma, "gamma", d), _vector(beta, "beta", d), eps,
+                               op, ldo, _vector(mean, "mean", n), _vector(rstd, "rstd", n), _stream()), "aa_layer_norm")
 
 
 def layer_norm_grad(dout, x, gamma, mean, rstd, residual, count, dx, dgamma, dbeta, accumulate, ws):
     """residual: what is added to dx, or None; dgamma, dbeta: either may be None, and ws where both are."""
-    dt = _type(dout, "dout")
-    gp, ldg = _matrix(dout, "dout")
-    n, d = dout.shape
-    xp, ldx = _matrix(x, "x", dout.dtype, d, n)
-    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", dout.dtype, d, n)
-    op, ldo = _matrix(dx, "dx", dout.dtype, d, n)
+    dt, gp, ldg, n, d = _first_rows(dout, "dout", DTYPES)
+    xp, ldx = _rows_like(x, "x", dout.dtype, n, d)
+    rp, ldr = (None, 0) if residual is None else _rows_like(residual, "residual", dout.dtype, n, d)
+    op, ldo = _rows_like(dx, "dx", dout.dtype, n, d)
     scratch = (None, 0) if dgamma is None and dbeta is None else _scratch(ws, "a LayerWorkspace")
     _check(lib().aa_layer_norm_grad(gp, dt, ldg, xp, ldx, _count(count), n, d,
-                                    _array(gamma, "gamma", torch.float32, (d,)), _array(mean, "mean", torch.float32, (n,)),
-                                    _array(rstd, "rstd", torch.float32, (n,)), rp, ldr, op, ldo,
-                                    _array(dgamma, "dgamma", torch.float32, (d,)),
-                                    _array(dbeta, "dbeta", torch.float32, (d,)), int(bool(accumulate)), *scratch,
-                                    _stream()), "aa_layer_norm_grad")
+                                    _vector(gamma, "gamma", d), _vector(mean, "mean", n), _vector(rstd, "rstd", n), rp, ldr,
+                                    op, ldo, _vector(dgamma, "dgamma", d), _vector(dbeta, "dbeta", d),
+                                    int(bool(accumulate)), *scratch, _stream()), "aa_layer_norm_grad")
 
 
 def linear(x, w, bias, act, residual, count, out, pre=None):
     """w [d_out, d_in] (gated: [2 d_out, d_in]) and bias (float32, or None) for all rows; pre: what the activation is taken
     of, for the backward pass."""
-    dt, a = _type(x, "x", True), _name_of(DENSE_ACTIVATIONS, act, "act")
-    xp, ldx = _matrix(x, "x")
-    n, d_in = x.shape
+    a = _name_of(DENSE_ACTIVATIONS, act, "act")
+    dt, xp, ldx, n, d_in = _first_rows(x, "x", _HALVES)
     _require(isinstance(w, torch.Tensor) and w.dim() == 2 and w.shape[1] == d_in, "w: [rows, d_in]")
     wide, dtype = w.shape[0], x.dtype
     _require(a != 2 or wide % 2 == 0, "w: [rows, d_in]")
     d_out = wide // 2 if a == 2 else wide
-    op, ldo = _matrix(out, "out", dtype, d_out, n)
-    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", dtype, d_out, n)
-    pp, ldp = (None, 0) if pre is None else _matrix(pre, "pre", dtype, wide, n)
+    op, ldo = _rows_like(out, "out", dtype, n, d_out)
+    rp, ldr = (None, 0) if residual is None else _rows_like(residual, "residual", dtype, n, d_out)
+    pp, ldp = (None, 0) if pre is None else _rows_like(pre, "pre", dtype, n, wide)
     _check(lib().aa_linear(xp, dt, ldx, _count(count), n, d_in, d_out, _array(w, "w", dtype),
-                           _array(bias, "bias", torch.float32, (wide,)), a, rp, ldr, op, ldo, pp, ldp, _stream()),
+                           _vector(bias, "bias", wide), a, rp, ldr, op, ldo, pp, ldp, _stream()),
            "aa_linear")
 
 
 def linear_grad(dout, act, pre, count, dpre, dbias, accumulate, ws):
     """pre: not needed without an activation; dpre or dbias may be None, and ws where dbias is."""
-    dt, a = _type(dout, "dout", True), _name_of(DENSE_ACTIVATIONS, act, "act")
-    gp, ldg = _matrix(dout, "dout")
-    (n, d), dtype = dout.shape, dout.dtype
+    a = _name_of(DENSE_ACTIVATIONS, act, "act")
+    dt, gp, ldg, n, d = _first_rows(dout, "dout", _HALVES)
+    dtype = dout.dtype
     wide = 2 * d if a == 2 else d
-    pp, ldp = (None, 0) if a == 0 else _matrix(pre, "pre", dtype, wide, n)
-    op, ldo = (None, 0) if dpre is None else _matrix(dpre, "dpre", dtype, wide, n)
+    pp, ldp = (None, 0) if a == 0 else _rows_like(pre, "pre", dtype, n, wide)
+    op, ldo = (None, 0) if dpre is None else _rows_like(dpre, "dpre", dtype, n, wide)
     scratch = (None, 0) if dbias is None else _scratch(ws, "a LayerWorkspace")
     _check(lib().aa_linear_grad(gp, dt, ldg, _count(count), n, d, a, pp, ldp, op, ldo,
-                                _array(dbias, "dbias", torch.float32, (wide,)), int(bool(accumulate)), *scratch,
+                                _vector(dbias, "dbias", wide), int(bool(accumulate)), *scratch,
                                 _stream()), "aa_linear_grad")
 
 
 def balance(logits, count, cfg, ids, coef, z_coef, counts, share, loss, ws):
     """counts: int32 [E]; share: float32 [E] or None; loss: float32 [2] or None; ws: a LayerWorkspace of E columns."""
-    dt = _type(logits, "logits")
-    x, ld = _matrix(logits, "logits")
-    n, E = logits.shape
+    dt, x, ld, n, E = _first_rows(logits, "logits", DTYPES)
     _require(counts is not None, "counts: needed")
     _check(lib().aa_balance(x, dt, ld, _count(count), n, E, C.byref(cfg), _array(ids, "ids", torch.int32, (n, cfg.top_k)),
                             coef, z_coef, _array(counts, "counts", torch.int32, (E,)),
-                            _array(share, "share", torch.float32, (E,)), _array(loss, "loss", torch.float32, (2,)),
+                            _vector(share, "share", E), _vector(loss, "loss", 2),
                             *_scratch(ws, "a LayerWorkspace"), _stream()), "aa_balance")
 
 
 def balance_grad(logits, count, cfg, ids, dweights, counts, coef, z_coef, dloss, dlogits):
     """dweights None: the balance loss alone (ids is then not read and may be None); dloss: a float32 tensor of one, or None."""
-    dt = _type(logits, "logits")
-    x, ld = _matrix(logits, "logits")
-    n, E = logits.shape
-    out, ld_out = _matrix(dlogits, "dlogits", logits.dtype, E, n)
+    dt, x, ld, n, E = _first_rows(logits, "logits", DTYPES)
+    out, ld_out = _rows_like(dlogits, "dlogits", logits.dtype, n, E)
     _check(lib().aa_balance_grad(x, dt, ld, _count(count), n, E, C.byref(cfg),
                                  _array(ids, "ids", torch.int32, (n, cfg.top_k)),
                                  _array(dweights, "dweights", torch.float32, (n, cfg.top_k)),

@@ -115,7 +115,7 @@ __device__ __forceinline__ bool last_block(int32_t *words) {
   stores_arrived();
   const int group = blockIdx.x / kGroupBlocks, groups = (gridDim.x + kGroupBlocks - 1) / kGroupBlocks;
   const int here = min((int)gridDim.x - group * kGroupBlocks, kGroupBlocks);
-  return count_in(words + (1 + group) * kWordApart, here) && count_in(words, groups);
+  return count_in(words + (1 + group) * kWordApart, here) && (groups == 1 || count_in(words, groups));
 }
 
 // The words of a call: 0 the norm, 1 the update.
@@ -330,76 +330,76 @@ __global__ __launch_bounds__(256) void k_adamw_step(const AdamWArgs a) {
   const float factor = a.grad_factor ? *a.grad_factor : 1.f;
   // an empty batch, or gradients that are not finite: nothing changes
   const bool skip = (a.count && *a.count <= 0) || !(fabsf(factor) < __builtin_inff());
-  if (!skip) {
-    const float lr = a.cfg.lr * (a.lr_factor ? *a.lr_factor : 1.f);
-    const float t = (float)before + 1.f;
-    Step s;
-    s.beta1 = a.cfg.beta1;
-    s.beta2 = a.cfg.beta2;
-    s.eps = a.cfg.eps;
-    s.factor = factor;
-    s.rate = lr / -expm1f(t * a.log_beta1);
-    s.root = 1.f / sqrtf(-expm1f(t * a.log_beta2));
-    s.shrink = lr * a.cfg.weight_decay;
-    s.k0 = (uint32_t)a.cfg.seed;
-    s.k1 = (uint32_t)(a.cfg.seed >> 32);
-    s.t = (uint32_t)before + 1u;
-    walk(a, [&](int tensor, const TensorEntry &e, int64_t from, int64_t to) {
-      const float shrink = 1.f - s.shrink * e.decay;
-      if (e.bits == 32) {
-        for (int64_t i = from + threadIdx.x * 8; i < to; i += 256 * 8) {
-          const int n = to - i < 8 ? (int)(to - i) : 8;
-          float *pm = static_cast<float *>(e.m) + i, *pv = static_cast<float *>(e.v) + i;
-          const Eight g = load_grad<PASSING>(e, i, n);
-          Eight p = load_some<PASSING>(e.param + i, n), m = load_some<PASSING>(pm, n), v = load_some<PASSING>(pv, n), r;
-          update8(s, g, m, v, r, p, shrink);
-          store_param<PASSING>(e, i, n, p);
-          store_some<PASSING>(pm, m, n);
-          store_some<PASSING>(pv, v, n);
-        }
-        return;
-      }
-      // (whole waves take part where one lane does: they share the scales)
-      for (int64_t base = from; base < to; base += 256 * 8) {
-        const int64_t i = base + threadIdx.x * 8;
-        const int n = to - i < 8 ? (int)(to - i) : 8;
-        uint8_t *pm = static_cast<uint8_t *>(e.m) + i, *pv = static_cast<uint8_t *>(e.v) + i;
-        const Global<float> ms = (Global<float>)(e.m_scale + i / kStateBlock), vs = (Global<float>)(e.v_scale + i / kStateBlock);
-        Eight m, v, r, p;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) m.v[k] = r.v[k] = 0.f;
-        if (n > 0) {
-          const Eight g = load_grad<PASSING>(e, i, n);
-          p = load_some<PASSING>(e.param + i, n);
-          m = decode(load_codes(pm, n), *ms);
-          v = decode(load_codes(pv, n), *vs);
-#pragma unroll
-          for (int k = 0; k < 8; ++k) v.v[k] *= v.v[k];
-          update8(s, g, m, v, r, p, shrink);
-          store_param<PASSING>(e, i, n, p);
-          if (n < 8) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-              if (k >= n) m.v[k] = r.v[k] = 0.f;
-          }
-        }
-        const uint4 draws = philox_words((uint32_t)(i / 8), 0x80000000u | (uint32_t)tensor, s.t, 0u, s.k0, s.k1);
-        float m_scale, v_scale;
-        const Codes cm = encode<false>(m, draws, &m_scale), cv = encode<true>(r, draws, &v_scale);
-        if (n > 0) {
-          store_codes(pm, n, cm);
-          store_codes(pv, n, cv);
-          if (threadIdx.x % (kStateBlock / 8) == 0) {
-            *ms = m_scale;
-            *vs = v_scale;
-          }
-        }
-      }
-    });
-  }
-  // every block has read the counter before it is counted here
+  // The counter's new value is stored by the last block to come here: all waves of all have read the old one then.
+  asm volatile("" ::"s"(before));
   __syncthreads();
   if (threadIdx.x == 0 && last_block(done_words(a, 1)) && !skip) *a.t = before + 1;
+  if (skip) return;
+  const float lr = a.cfg.lr * (a.lr_factor ? *a.lr_factor : 1.f);
+  const float t = (float)before + 1.f;
+  Step s;
+  s.beta1 = a.cfg.beta1;
+  s.beta2 = a.cfg.beta2;
+  s.eps = a.cfg.eps;
+  s.factor = factor;
+  s.rate = lr / -expm1f(t * a.log_beta1);
+  s.root = 1.f / sqrtf(-expm1f(t * a.log_beta2));
+  s.shrink = lr * a.cfg.weight_decay;
+  s.k0 = (uint32_t)a.cfg.seed;
+  s.k1 = (uint32_t)(a.cfg.seed >> 32);
+  s.t = (uint32_t)before + 1u;
+  walk(a, [&](int tensor, const TensorEntry &e, int64_t from, int64_t to) {
+    const float shrink = 1.f - s.shrink * e.decay;
+    if (e.bits == 32) {
+      for (int64_t i = from + threadIdx.x * 8; i < to; i += 256 * 8) {
+        const int n = to - i < 8 ? (int)(to - i) : 8;
+        float *pm = static_cast<float *>(e.m) + i, *pv = static_cast<float *>(e.v) + i;
+        const Eight g = load_grad<PASSING>(e, i, n);
+        Eight p = load_some<PASSING>(e.param + i, n), m = load_some<PASSING>(pm, n), v = load_some<PASSING>(pv, n), r;
+        update8(s, g, m, v, r, p, shrink);
+        store_param<PASSING>(e, i, n, p);
+        store_some<PASSING>(pm, m, n);
+        store_some<PASSING>(pv, v, n);
+      }
+      return;
+    }
+    // (whole waves take part where one lane does: they share the scales)
+    for (int64_t base = from; base < to; base += 256 * 8) {
+      const int64_t i = base + threadIdx.x * 8;
+      const int n = to - i < 8 ? (int)(to - i) : 8;
+      uint8_t *pm = static_cast<uint8_t *>(e.m) + i, *pv = static_cast<uint8_t *>(e.v) + i;
+      const Global<float> ms = (Global<float>)(e.m_scale + i / kStateBlock), vs = (Global<float>)(e.v_scale + i / kStateBlock);
+      Eight m, v, r, p;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) m.v[k] = r.v[k] = 0.f;
+      if (n > 0) {
+        const Eight g = load_grad<PASSING>(e, i, n);
+        p = load_some<PASSING>(e.param + i, n);
+        m = decode(load_codes(pm, n), *ms);
+        v = decode(load_codes(pv, n), *vs);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v.v[k] *= v.v[k];
+        update8(s, g, m, v, r, p, shrink);
+        store_param<PASSING>(e, i, n, p);
+        if (n < 8) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k)
+            if (k >= n) m.v[k] = r.v[k] = 0.f;
+        }
+      }
+      const uint4 draws = philox_words((uint32_t)(i / 8), 0x80000000u | (uint32_t)tensor, s.t, 0u, s.k0, s.k1);
+      float m_scale, v_scale;
+      const Codes cm = encode<false>(m, draws, &m_scale), cv = encode<true>(r, draws, &v_scale);
+      if (n > 0) {
+        store_codes(pm, n, cm);
+        store_codes(pv, n, cv);
+        if (threadIdx.x % (kStateBlock / 8) == 0) {
+          *ms = m_scale;
+          *vs = v_scale;
+        }
+      }
+    }
+  });
 }
 
 }  // namespace

@@ -101,7 +101,12 @@ __global__ __launch_bounds__(256) void k_act_grad(const ActGradArgs a) {
       float all = 0.f;
 #pragma unroll
       for (int r = 0; r < kRows; ++r) all += room[half][r][k];
-      a.part[((int64_t)blockIdx.y * kHalves + half) * d + at] = all;
+      if (gridDim.y > 1) {
+        a.part[((int64_t)blockIdx.y * kHalves + half) * d + at] = all;
+      } else {  // (a part that is alone)
+        float *to = a.dbias + (int64_t)half * d + at;
+        *to = a.accumulate ? *to + all : all;
+      }
     }
 }
 
@@ -116,7 +121,7 @@ hipError_t act_grad(ActGradArgs a, hipStream_t st) {
   a.parts = (int32_t)(parts > 1 ? parts : 1);
   hipLaunchKernelGGL((k_act_grad<T, ACT, CL>), dim3((uint32_t)stripes, (uint32_t)a.parts), dim3(256), 0, st, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !a.dbias) return e;
+  if (e != hipSuccess || !a.dbias || a.parts == 1) return e;
   return launch_join_columns(a.part, a.parts, (int64_t)a.d * kHalves, a.d, a.dbias, kHalves == 2 ? a.dbias + a.d : nullptr,
                              a.accumulate, st);
 }

@@ -318,15 +318,26 @@ __global__ __launch_bounds__(kGradThreads<TPR>) void k_layer_norm_grad(const Nor
     }
   }
   if (!sums) return;
+  // a block that is alone has the sums, the others a part of them each
+  const bool alone = gridDim.x == 1, add = alone && a.accumulate;
   float *part = a.part + (int64_t)blockIdx.x * 2 * d;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     const Eight(&s)[NV] = which == 0 ? dg : db;
+    float *to = alone ? (which == 0 ? a.dgamma : a.dbeta) : part + (int64_t)which * d;
+    if (!to) continue;
     if constexpr (kRows == 1) {
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int c = c0 + v * kStepC;
-        if (c < d) store8(part + (int64_t)which * d + c, s[v], d - c);
+        if (c >= d) continue;
+        Eight all = s[v];
+        if (add) {
+          const Eight old = load8(to + c, d - c);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) all.v[i] += old.v[i];
+        }
+        store8(to + c, all, d - c);
       }
     } else {  // the rows that the block took at once
       __syncthreads();
@@ -339,7 +350,7 @@ __global__ __launch_bounds__(kGradThreads<TPR>) void k_layer_norm_grad(const Nor
         float sum = 0.f;
 #pragma unroll
         for (int r = 0; r < kRows; ++r) sum += joined[r][c];
-        part[(int64_t)which * d + c] = sum;
+        to[c] = add ? to[c] + sum : sum;
       }
     }
   }
@@ -505,7 +516,7 @@ hipError_t layer_norm_grad(const NormArgs &a, hipStream_t st) {
         if (passing<T>(a)) hipLaunchKernelGGL((k_layer_norm_grad<T, TPR, NV, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((k_layer_norm_grad<T, TPR, NV, false>), grid, block, 0, st, a);
         const hipError_t e = hipGetLastError();
-        return e != hipSuccess ? e : join_columns(a, parts, st);
+        return e != hipSuccess || parts == 1 ? e : join_columns(a, parts, st);
       },
       [&] {
         if (a.dgamma || a.dbeta) {  // (first: dx may be dout or x)
