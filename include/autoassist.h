@@ -516,7 +516,8 @@ size_t aa_layer_workspace_bytes(int32_t d_max);
 
 /* Layer norm: out[t] = (x[t] - mean_t) rstd_t gamma + beta over the d columns of a row, mean_t = sum x / d,
  * rstd_t = 1 / sqrt(sum (x - mean_t)^2 / d + eps).  gamma, beta: [d] (NULL: 1 and 0).  mean, rstd: [n_max], what
- * the backward pass needs (NULL: not written).  eps >= 0, finite.  out may be x. */
+ * the backward pass needs (NULL: not written).  eps >= 0, finite (a row of equal values has no norm with eps == 0: what comes
+ * out is not finite, or rounding's).  out may be x. */
 int32_t aa_layer_norm(const void *x, int32_t dtype, int64_t ldx, const int32_t *count, int32_t n_max, int32_t d,
                       const float *gamma, const float *beta, float eps, void *out, int64_t ldo, float *mean,
                       float *rstd, void *stream);
@@ -531,7 +532,7 @@ int32_t aa_layer_norm_grad(const void *dout, int32_t dtype, int64_t lddo, const 
                            const float *rstd, const void *residual, int64_t ldr, void *dx, int64_t lddx,
                            float *dgamma, float *dbeta, int32_t accumulate, void *ws, size_t ws_bytes, void *stream);
 
-/* Dense layer (dtype AA_BF16 or AA_F16, sums in fp32): for the rows in use
+/* Dense layer (dtype AA_BF16 or AA_F16, sums in fp32): for the rows in use (those of x that are not may be read, too)
  *   h = w x[t] + bias,   out[t] = residual[t] + act(h)
  * with w [d_out][d_in] and bias [d_out], with AA_ACT_GATED [2 d_out][d_in] and [2 d_out] (gate rows, then up rows),
  * contiguous.  bias, residual: NULL for none.  pre (NULL: not written) receives h, [n_max][d_out] or

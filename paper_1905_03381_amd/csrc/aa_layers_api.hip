@@ -110,7 +110,7 @@ int32_t aa_layer_norm_grad(const void *dout, int32_t dtype, int64_t lddo, const 
   AA_TRY(check_words(rstd, n_max > 0));
   AA_TRY(check_words(dgamma, false));
   AA_TRY(check_words(dbeta, false));
-  if (dgamma || dbeta) AA_TRY(check_ws(ws, ws_bytes, layer_bytes(d)));
+  if (dgamma || dbeta) AA_TRY(check_ws(ws, ws_bytes, layer_need(d)));
   NormArgs a{};
   a.x = x;
   a.ldx = ldx;
@@ -179,7 +179,7 @@ int32_t aa_linear_grad(const void *dout, int32_t dtype, int64_t lddo, const int3
   if (act != AA_ACT_NONE) AA_TRY(check_rows(pre, n_max, ldpre, wide, 2));
   if (dpre) AA_TRY(check_rows(dpre, n_max, lddp, wide, 2));
   AA_TRY(check_words(dbias, false));
-  if (dbias) AA_TRY(check_ws(ws, ws_bytes, layer_bytes(wide)));
+  if (dbias) AA_TRY(check_ws(ws, ws_bytes, layer_need(wide)));
   ActGradArgs a{};
   a.dout = dout;
   a.lddo = lddo;
@@ -205,7 +205,7 @@ int32_t aa_balance(const void *logits, int32_t dtype, int64_t ld, const int32_t 
   AA_TRY(check_words(counts, true));
   AA_TRY(check_words(share, false));
   AA_TRY(check_words(loss, false));
-  AA_TRY(check_ws(ws, ws_bytes, layer_bytes(n_experts)));
+  AA_TRY(check_ws(ws, ws_bytes, layer_need(n_experts)));
   BalanceArgs a{};
   a.logits = logits;
   a.dtype = dtype;

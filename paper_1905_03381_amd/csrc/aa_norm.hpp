@@ -30,11 +30,18 @@ __host__ __device__ inline int column_parts(int64_t d) {
   const int64_t p = (4ll << 20) / (d > 0 ? d : 1);
   return (int)(p < 1 ? 1 : p > kColumnPartsMost ? kColumnPartsMost : p);
 }
-// The workspace: control words, kLayerHead bytes of what blocks have one of, then the columns' parts.
+// The workspace: control words, kLayerHead bytes of what blocks have one of, then the columns' parts.  What rows of d columns
+// need of it, and what rows of up to d_max do (a number of columns may need more than a larger one: parts are whole).
 constexpr size_t kLayerHead = 4096;
-inline size_t layer_bytes(int64_t d) {
-  const size_t parts = align_up((size_t)column_parts(d) * 2 * d * sizeof(float), 256);
+inline size_t layer_need(int64_t d) {
+  const size_t parts = (size_t)column_parts(d) * 2 * d * sizeof(float);
   return kLayerHead + (parts > 16384 ? parts : 16384);
+}
+inline size_t layer_bytes(int64_t d_max) {
+  const int64_t most = (4ll << 20) * 2 * (int64_t)sizeof(float);  // of columns that the parts are limited for
+  const int64_t parts = (int64_t)kColumnPartsMost * 2 * d_max * (int64_t)sizeof(float);
+  const int64_t one = 2 * d_max * (int64_t)sizeof(float), need = parts < most ? parts : one > most ? one : most;
+  return kLayerHead + align_up(need > 16384 ? (size_t)need : 16384, 256);
 }
 
 // first[c], second[c] (+)= the sum over the parts, `stride` floats apart, of their columns c and d + c (either may be NULL);

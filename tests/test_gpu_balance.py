@@ -83,6 +83,19 @@ def test_rows(n, count, E, K, kind):
     check_balance(x, ids, kind, count, run(x, ids, kind, count))
 
 
+@pytest.mark.parametrize("n", [60, 3000])
+def test_counts_alone_and_rows_that_are_not_in_use(n):
+    x, ids = case(n, 64, 4, BF16, 7)
+    x, ids, m = x.cuda(), ids.cuda(), n // 2
+    want = run(x, ids, "sigmoid", m)
+    x[m:], ids[m:] = float("nan"), 5
+    counts = torch.zeros(64, dtype=torch.int32, device="cuda")
+    api.balance(x, device_count(m), api.route_config("sigmoid", 4), ids, 0.02, 0.003, counts, None, None, api.LayerWorkspace(64))
+    assert torch.equal(counts, want[0])
+    for a, b in zip(run(x, ids, "sigmoid", m), want):
+        assert torch.equal(a, b)
+
+
 def test_ids_outside_are_no_choices():
     x, ids = case(50, 16, 4, F32, 7)
     ids[3, 1], ids[4, 0], ids[5, 2] = 16, -9, 2 ** 31 - 1

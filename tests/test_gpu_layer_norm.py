@@ -72,6 +72,28 @@ def test_without_vectors_and_statistics(d):
     check_norm(x, np.ones(d), b64, None, run_norm(x, None, beta, None))
 
 
+@pytest.mark.parametrize("d", [12, 300, 700, 5000, 20_000])
+def test_rows_that_are_not_in_use_may_hold_anything(d):
+    n, m = 40, 17
+    x, dout, res = (rows(n, d, BF16, 3 + i).cuda() for i in range(3))
+    mean, rstd = statistics(x)
+    for t in (x, dout, res, mean, rstd):
+        t[m:] = float("nan")
+    gamma, beta, g64, b64 = vectors(d, 3)
+    check_norm(x, g64, b64, m, run_norm(x, gamma, beta, m))
+    check_grad(dout, x, g64, mean, rstd, res, m, run_grad(dout, x, gamma, mean, rstd, res, m))
+
+
+def test_one_workspace_for_all_widths():
+    ws = api.LayerWorkspace(12_000)
+    for d in (3, 500, 8192, 8193, 12_000):
+        x, dout = rows(600, d, BF16, 3).cuda(), normal((600, d), BF16, 4).cuda()
+        mean, rstd = statistics(x)
+        dx, dgamma, dbeta = torch.zeros_like(x), torch.zeros(d, device="cuda"), torch.zeros(d, device="cuda")
+        api.layer_norm_grad(dout, x, None, mean, rstd, None, None, dx, dgamma, dbeta, False, ws)
+        check_grad(dout, x, np.ones(d), mean, rstd, None, None, (dx, dgamma, dbeta))
+
+
 @pytest.mark.parametrize("d", [12, 700, 3000, 20_000])
 def test_equal_columns_far_means_and_in_place(d):
     """Rows of one value have only eps; rows far from 0 keep the digits that their differences have."""

@@ -82,6 +82,14 @@ def test_rows_in_use(n, count, act):
     layer.check(*layer.run())
 
 
+@pytest.mark.parametrize("n,count", [(20, 3), (40, 17), (300, 100), (1100, 700)])
+@pytest.mark.parametrize("d_in", [128, 129])
+def test_rows_that_are_not_in_use_may_hold_anything(n, count, d_in):
+    layer = Layer(n, d_in, 192, "gelu", BF16, residual=True, count=count)
+    layer.x[count:], layer.residual[count:] = float("nan"), float("inf")
+    layer.check(*layer.run())
+
+
 @pytest.mark.parametrize("n", [8, 400])
 def test_residual_in_place(n):
     layer = Layer(n, 128, 192, "silu", BF16, residual=True)

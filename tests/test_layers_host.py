@@ -1,6 +1,7 @@
 """Refusals of the operators around a Boss block of experts: every one is decided on the host before anything is
 launched, so these run without a GPU.  The pointers handed over are never read."""
 import pytest
+import torch
 
 from paper_1905_03381_amd import api
 
@@ -149,18 +150,51 @@ def test_refused(L, name, args, change, want):
 
 
 def test_workspace_grows_with_the_columns(L):
-    sizes = [L.aa_layer_workspace_bytes(d) for d in (0, 1, 64, 8192, 1 << 16, 1 << 24)]
-    assert sizes[0] == sizes[1] and all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[-1] < 1 << 28
-    assert all(s % 256 == 0 for s in sizes)
+    """One made for d_max columns serves every call of fewer: its size grows, and a call of d asks for no more than that of d."""
+    widths = sorted({1, 2, 3, 64, 1000, 1024, 8191, 8192, 8193, 12_000, 16_383, 16_384, 70_001, 1 << 20, (1 << 22) - 1, 1 << 22,
+                     (1 << 22) + 1, 1 << 24} | {(7919 * k) % 30_000 + 1 for k in range(200)})
+    sizes = [L.aa_layer_workspace_bytes(d) for d in widths]
+    assert L.aa_layer_workspace_bytes(0) == sizes[0]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:])) and sizes[-1] < 1 << 28 and all(s % 256 == 0 for s in sizes)
 
 
-def test_python_refusals():
-    import torch
-    t = torch.zeros(4, 8)  # (not a CUDA tensor)
+def test_a_workspace_serves_fewer_columns(L):
+    """A call of no rows and no sums' room: refused for the workspace, or launched (which fails without a GPU)."""
+    for d_max in (1, 5, 8192, 8193, 12_000, 16_383, 16_385, 70_001, (1 << 22) + 5):
+        for d in {1, 4, 8192, 8193, 11_999, 16_384, d_max} - {w for w in (1, 4, 8192, 8193, 11_999, 16_384) if w > d_max}:
+            call = dict(NORM_GRAD, n_max=0, d=d, lddo=d, ldx=d, lddx=d, ws_bytes=L.aa_layer_workspace_bytes(d_max), accumulate=1)
+            assert L.aa_layer_norm_grad(*call.values()) == OK, (d_max, d)
+
+
+T = torch.zeros(4, 8)  # (not a CUDA tensor)
+HALF = torch.zeros(4, 8, dtype=torch.bfloat16)
+
+
+@pytest.mark.parametrize("call", [
+    lambda: api.layer_norm(T, None, None, 1e-5, None, T),
+    lambda: api.layer_norm(None, None, None, 1e-5, None, T),
+    lambda: api.layer_norm(torch.zeros(4), None, None, 1e-5, None, T),
+    lambda: api.layer_norm(torch.zeros(4, 8, dtype=torch.float64), None, None, 1e-5, None, T),
+    lambda: api.layer_norm_grad(T, T, None, None, None, None, None, T, None, None, False, None),
+    lambda: api.linear(HALF, HALF, None, "gelu", None, None, HALF),
+    lambda: api.linear(T, T, None, "gelu", None, None, T),
+    lambda: api.linear(HALF, HALF, None, "tanh", None, None, HALF),
+    lambda: api.linear(HALF, None, None, "none", None, None, HALF),
+    lambda: api.linear_grad(HALF, "silu", None, None, HALF, None, False, None),
+    lambda: api.linear_grad(None, "silu", None, None, HALF, None, False, None),
+    lambda: api.balance(T, None, cfg(), None, 0.1, 0.1, None, None, None, None),
+    lambda: api.balance(None, None, cfg(), None, 0.1, 0.1, None, None, None, None),
+    lambda: api.balance_grad(T, None, cfg(), None, None, None, 0.1, 0.1, None, T),
+    lambda: api.adamw_tensor(T, T, T, T),
+    lambda: api.adamw_tensor(None, T, T, T),
+    lambda: api.adamw_tensor(T, torch.zeros(4, dtype=torch.float64), T, T),
+    lambda: api.AdamWTable([]),
+    lambda: api.grad_norm(None, 1.0, None, None),
+    lambda: api.adamw_step(None, None, None, None, None, None),
+])
+def test_python_refusals(call):
     with pytest.raises(api.AAError):
-        api.layer_norm(t, None, None, 1e-5, None, t)
-    with pytest.raises(api.AAError):
-        api.layer_norm_grad(t, t, None, None, None, None, None, t, None, None, False, None)
+        call()
 
 
 def test_chunks_of_tensors(L):
