@@ -55,7 +55,7 @@ struct BalanceArgs {
   float *part;    // [blocks][2][E up to a multiple of 4]: shares, then (int32) choices
 };
 
-constexpr int kBalanceBlocks = 512;
+constexpr int kBalanceBlocks = 256;
 constexpr int kBalanceTerms = AA_MAX_EXPERTS / 16 + 1;
 
 struct PlanArgs {
