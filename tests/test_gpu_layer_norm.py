@@ -9,9 +9,9 @@ from paper_1905_03381_amd import api
 
 pytestmark = pytest.mark.gpu
 
-# Either side of what a thread, 16 and 64 lanes, 4, 8 and 16 waves hold, and rows that no block holds.
-WIDTHS = [1, 2, 7, 8, 9, 65, 127, 128, 129, 511, 512, 513, 1000, 1024, 1025, 2047, 2048, 2049, 4093, 4096, 4097, 8191,
-          8192, 8193, 16_384, 16_385, 70_001]
+# Either side of what a thread, 16 and 64 lanes, 4 and 8 waves hold, and rows that no block holds.
+WIDTHS = [1, 2, 7, 8, 9, 65, 127, 128, 129, 255, 256, 257, 511, 512, 513, 1000, 1024, 1025, 2047, 2048, 2049, 4093, 4096, 4097, 8191,
+          8192, 8193, 12_287, 12_288, 12_289, 16_384, 16_385, 70_001]
 
 
 def vectors(d, seed, affine=True):
@@ -55,7 +55,7 @@ def test_widths(d, dtype):
 
 
 @pytest.mark.parametrize("n,count", [(1, None), (1, 0), (3, -5), (3, 7), (17, 16), (300, 299), (9000, None)])
-@pytest.mark.parametrize("d", [24, 640, 1500])
+@pytest.mark.parametrize("d", [24, 200, 400, 640, 1500, 9000])
 def test_rows(n, count, d):
     x = rows(n, d, BF16, n + d).cuda()
     gamma, beta, g64, b64 = vectors(d, 3)
@@ -158,7 +158,7 @@ def test_grad_widths(d, dtype):
 
 
 @pytest.mark.parametrize("n,count", [(1, None), (2, 0), (3, -5), (3, 7), (17, 16), (300, 299), (9000, None)])
-@pytest.mark.parametrize("d", [24, 640, 1500])
+@pytest.mark.parametrize("d", [24, 200, 400, 640, 1500, 9000])
 @pytest.mark.parametrize("accumulate", [False, True])
 def test_grad_rows(n, count, d, accumulate):
     x, dout = rows(n, d, F16, n + d).cuda(), normal((n, d), F16, 4).cuda()
