@@ -2,7 +2,8 @@
 //
 // The tensors are cut into chunks of 2048 elements, listed once in a table on the device; a launch walks all of them, each block a
 // run of neighbouring chunks, eight neighbouring elements a thread.  Bound by memory: 28 to 30 bytes an element with
-// states in 32 bits, 16 to 18 with states in 8.
+// states in 32 bits, 16 to 18 with states in 8 (25.2 M elements, 32-bit states and gradients, 16-bit copies: 155 us, 4.9 TB/s; 46 M,
+// 8-bit states, 16-bit gradients: 165 to 171, where the draws and the conversions also count: 38 M vector instructions).
 //
 // States in 8 bits: 256 neighbours share a power of two that brings their largest into [128, 256), and each is held
 // as an e4m3 number (steps of an eighth to a sixteenth of it, down to 2^-17 of the largest).  v is held as its root, so
@@ -156,7 +157,7 @@ __device__ __forceinline__ double squares(const T *g, int64_t from, int64_t to) 
 }
 
 // Sum of squares in 64 bits (32 would end at gradients of 1.8e19).  Each block's part, and the last block adds them
-// up in their order.
+// up in their order.  25.2 M elements in 32 bits 22 us, 4.6 TB/s.
 __global__ __launch_bounds__(256) void k_grad_norm(const AdamWArgs a) {
   __shared__ double room[4];
   __shared__ int last;

@@ -38,7 +38,7 @@ __device__ __forceinline__ float through(float d, float h, float up, float *du) 
   return d;
 }
 
-// CL lanes along the columns, 256 / CL rows at a time; blockIdx.y: the part.
+// CL lanes along the columns, 256 / CL rows at a time; blockIdx.y: the part.  6001 x 1544 f16, silu: 15.6 us, 3.6 TB/s.
 template <typename T, int ACT, int CL>
 __global__ __launch_bounds__(256) void k_act_grad(const ActGradArgs a) {
   constexpr int kRows = 256 / CL, kHalves = ACT == AA_ACT_GATED ? 2 : 1;
@@ -113,8 +113,11 @@ __global__ __launch_bounds__(256) void k_act_grad(const ActGradArgs a) {
 template <typename T, int ACT, int CL>
 hipError_t act_grad(ActGradArgs a, hipStream_t st) {
   constexpr int kRows = 256 / CL, kHalves = ACT == AA_ACT_GATED ? 2 : 1;
-  // parts: eight blocks a compute unit, no more than there are rows or the workspace has room for
-  const int64_t stripes = ((int64_t)a.d + CL * 8 - 1) / (CL * 8), fill = 2048 / stripes, turns = ((int64_t)a.n_max + kRows - 1) / kRows;
+  // Parts: eight blocks a compute unit, four where each still has much to do (bf16: 16,384 x 8192 gelu 166 us by eight, 155 by
+  // four, 30,000 x 5000 139 and 129; 6001 x 1536 13.6 and 14.9; of lines off 16 bytes 50,000 x 1100 82 and 104), no more than
+  // there are rows or the workspace has room for.
+  const bool much = a.d % 8 == 0 && (int64_t)a.n_max * a.d >= 16ll << 20;
+  const int64_t stripes = ((int64_t)a.d + CL * 8 - 1) / (CL * 8), fill = (much ? 1024 : 2048) / stripes, turns = ((int64_t)a.n_max + kRows - 1) / kRows;
   const int64_t room = column_parts((int64_t)a.d * kHalves);
   int64_t parts = fill < turns ? fill : turns;
   parts = parts < room ? parts : room;
@@ -126,9 +129,10 @@ hipError_t act_grad(ActGradArgs a, hipStream_t st) {
                              a.accumulate, st);
 }
 
+// 64 lanes cover 512 columns (60,000 x 333 silu: 61 us, by 16 lanes 34; 50,000 x 1100: 82, 92).
 template <typename T, int ACT>
 hipError_t by_columns(const ActGradArgs &a, hipStream_t st) {
-  return a.d <= 128 ? act_grad<T, ACT, 16>(a, st) : act_grad<T, ACT, 64>(a, st);
+  return a.d <= 384 ? act_grad<T, ACT, 16>(a, st) : act_grad<T, ACT, 64>(a, st);
 }
 
 template <typename T>
@@ -146,7 +150,7 @@ hipError_t by_act(const ActGradArgs &a, hipStream_t st) {
 // up's) of 16 MF rows; its waves share the summed dimension out in chunks of 64, straight from memory into the matrix
 // instructions' registers, kAhead of them on their way, and join their sums in LDS.  Rows are asked for whether they are in use
 // or not: the count would be waited for first.  ODD: rows that may begin inside a word of four bytes.
-// Four waves; eight or sixteen were slower (one row 4096 -> 136: 6.6, 7.2, 8.2 us).
+// Four waves; eight or sixteen were slower (one row 4096 -> 136: 6.6, 7.2, 8.2 us).  One row 2048 -> 4096, 17 MB: 6 to 7.6 us.
 constexpr int kFewWaves = 4;
 
 // Sixteen bytes of a row at any address.  A load that begins inside a word of four bytes takes as long as four (9 rows 4781 ->

@@ -422,7 +422,7 @@ __global__ __launch_bounds__(256) void k_layer_norm_columns(const NormArgs a, in
 }
 
 // first[c], second[c] (+)= the sum over the parts (`stride` apart) of their columns c and d + c: 64 columns a block, 16
-// shares of the parts, joined in their order.
+// shares of the parts, joined in their order.  512 parts of 8192 columns 6.6 us, of 1021 3.9.
 constexpr int kJoinShares = 16;
 
 __global__ __launch_bounds__(kJoinShares *kWave) void k_join_columns(const float *part, int parts, int64_t stride, int d,
