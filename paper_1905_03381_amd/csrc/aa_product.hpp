@@ -1008,11 +1008,13 @@ hipError_t launch_tiles(ProductArgs a, hipStream_t st) {
                        0, st, a);
   else
     hipLaunchKernelGGL((k_product<T, MODE, ACT, WI, WJ, FI, FJ, NB, false, ALIGNED, DENSE>), grid, block, 0, st, a);
-  if (a.parts > 1) {
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const dim3 join((uint32_t)(ni * nj * (BM * BN / 1024)));
-    hipLaunchKernelGGL((k_join_parts<T, BM, BN>), join, dim3(256), 0, st, a);
+  if constexpr (MODE == kGradWeight) {
+    if (a.parts > 1) {
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+      const dim3 join((uint32_t)(ni * nj * (BM * BN / 1024)));
+      hipLaunchKernelGGL((k_join_parts<T, BM, BN>), join, dim3(256), 0, st, a);
+    }
   }
   return hipGetLastError();
 }
