@@ -606,7 +606,8 @@ typedef struct aa_adamw_config {
 } aa_adamw_config;
 
 /* The list of the tensors on the device: made once, used by every step as long as the tensors stay where they are.
- * `tensors` is a HOST array of n_tensors (1 to 65536); no element belongs to two of them.  aa_adamw_chunks: how many chunks they are cut
+ * `tensors` is a HOST array of n_tensors (1 to 65536); memory that an update writes (param, copy, states, scales) is listed
+ * once and is no gradient: AA_ERR_SHAPE.  aa_adamw_chunks: how many chunks they are cut
  * into, or a negative AA_ERR_* if the list is refused.  `table`: device memory of aa_adamw_table_bytes(n_tensors, n_chunks)
  * bytes, 256-byte aligned; it must not be used by two calls that may overlap in time. */
 int64_t aa_adamw_chunks(const aa_adamw_tensor *tensors, int32_t n_tensors);

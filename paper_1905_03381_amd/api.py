@@ -615,6 +615,28 @@ class LayerWorkspace:
         _take(self, int(lib().aa_layer_workspace_bytes(d_max)), device)
 
 
+def _current():
+    return torch.cuda.current_device() if _device is None else _device()
+
+
+def _here(t, name):
+    """A GPU tensor is on the device that the call's stream is of."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != _current():
+        raise AAError(f"{name}: on device {t.get_device()}, the current one is {_current()}")
+
+
+def _flat(t, name, dtype, shape=None, least=0):
+    """_array of a tensor on the current device."""
+    _here(t, name)
+    return _array(t, name, dtype, shape, least)
+
+
+def _layer_scratch(ws):
+    scratch = _scratch(ws, "a LayerWorkspace")
+    _here(ws.buf, "ws")
+    return scratch
+
+
 # (Calls of a row or a few take as long as the host: each of these asks a tensor for six things where _matrix and _array ask for
 # ten.  What is unusual goes to those, for their messages.)
 _F32, _I32, _Tensor = torch.float32, torch.int32, torch.Tensor
@@ -623,37 +645,39 @@ _F32, _I32, _Tensor = torch.float32, torch.int32, torch.Tensor
 def _count(count):
     if count is None:
         return None
-    if type(count) is _Tensor and count.dtype is _I32 and count.is_cuda and count.dim() == 1 and count.numel() == 1:
+    if type(count) is _Tensor and count.dtype is _I32 and count.is_cuda and count.get_device() == _current() and count.dim() == 1 and count.numel() == 1:
         return count.data_ptr()
-    return _array(count, "count", _I32, least=1)
+    return _flat(count, "count", _I32, least=1)
 
 
 def _vector(t, name, n):
     """Pointer of n neighbouring float32 values; None stays None."""
     if t is None:
         return None
-    if type(t) is _Tensor and t.dtype is _F32 and t.is_cuda and t.shape == (n,) and t.is_contiguous():
+    if type(t) is _Tensor and t.dtype is _F32 and t.is_cuda and t.get_device() == _current() and t.shape == (n,) and t.is_contiguous():
         return t.data_ptr()
-    return _array(t, name, _F32, (n,))
+    return _flat(t, name, _F32, (n,))
 
 
 def _rows_like(t, name, dtype, n, d):
     """(pointer, row stride) of n rows of d neighbouring columns of the given type (or more rows)."""
-    if type(t) is _Tensor and t.dtype is dtype and t.is_cuda and t.shape == (n, d):
+    if type(t) is _Tensor and t.dtype is dtype and t.is_cuda and t.get_device() == _current() and t.shape == (n, d):
         ld, step = t.stride()
         if step == 1:
             return t.data_ptr(), ld if n > 1 else d
+    _here(t, name)
     return _matrix(t, name, dtype, d, n)
 
 
 def _first_rows(t, name, types):
     """(type code, pointer, row stride, rows, columns) of the matrix that a call's sizes and type come from."""
-    if type(t) is _Tensor and t.is_cuda and t.dim() == 2:
+    if type(t) is _Tensor and t.is_cuda and t.get_device() == _current() and t.dim() == 2:
         code = types.get(t.dtype)
         n, d = t.shape
         ld, step = t.stride()
         if code is not None and step == 1:
             return code, t.data_ptr(), ld if n > 1 else d, n, d
+    _here(t, name)
     code = _type(t, name, types is _HALVES)
     p, ld = _matrix(t, name)
     return code, p, ld, t.shape[0], t.shape[1]
@@ -676,7 +700,7 @@ def layer_norm_grad(dout, x, gamma, mean, rstd, residual, count, dx, dgamma, dbe
     xp, ldx = _rows_like(x, "x", dout.dtype, n, d)
     rp, ldr = (None, 0) if residual is None else _rows_like(residual, "residual", dout.dtype, n, d)
     op, ldo = _rows_like(dx, "dx", dout.dtype, n, d)
-    scratch = (None, 0) if dgamma is None and dbeta is None else _scratch(ws, "a LayerWorkspace")
+    scratch = (None, 0) if dgamma is None and dbeta is None else _layer_scratch(ws)
     _check(lib().aa_layer_norm_grad(gp, dt, ldg, xp, ldx, _count(count), n, d,
                                     _vector(gamma, "gamma", d), _vector(mean, "mean", n), _vector(rstd, "rstd", n), rp, ldr,
                                     op, ldo, _vector(dgamma, "dgamma", d), _vector(dbeta, "dbeta", d),
@@ -695,7 +719,7 @@ def linear(x, w, bias, act, residual, count, out, pre=None):
     op, ldo = _rows_like(out, "out", dtype, n, d_out)
     rp, ldr = (None, 0) if residual is None else _rows_like(residual, "residual", dtype, n, d_out)
     pp, ldp = (None, 0) if pre is None else _rows_like(pre, "pre", dtype, n, wide)
-    _check(lib().aa_linear(xp, dt, ldx, _count(count), n, d_in, d_out, _array(w, "w", dtype),
+    _check(lib().aa_linear(xp, dt, ldx, _count(count), n, d_in, d_out, _flat(w, "w", dtype),
                            _vector(bias, "bias", wide), a, rp, ldr, op, ldo, pp, ldp, _stream()),
            "aa_linear")
 
@@ -708,7 +732,7 @@ def linear_grad(dout, act, pre, count, dpre, dbias, accumulate, ws):
     wide = 2 * d if a == 2 else d
     pp, ldp = (None, 0) if a == 0 else _rows_like(pre, "pre", dtype, n, wide)
     op, ldo = (None, 0) if dpre is None else _rows_like(dpre, "dpre", dtype, n, wide)
-    scratch = (None, 0) if dbias is None else _scratch(ws, "a LayerWorkspace")
+    scratch = (None, 0) if dbias is None else _layer_scratch(ws)
     _check(lib().aa_linear_grad(gp, dt, ldg, _count(count), n, d, a, pp, ldp, op, ldo,
                                 _vector(dbias, "dbias", wide), int(bool(accumulate)), *scratch,
                                 _stream()), "aa_linear_grad")
@@ -718,10 +742,10 @@ def balance(logits, count, cfg, ids, coef, z_coef, counts, share, loss, ws):
     """counts: int32 [E]; share: float32 [E] or None; loss: float32 [2] or None; ws: a LayerWorkspace of E columns."""
     dt, x, ld, n, E = _first_rows(logits, "logits", DTYPES)
     _require(counts is not None, "counts: needed")
-    _check(lib().aa_balance(x, dt, ld, _count(count), n, E, C.byref(cfg), _array(ids, "ids", torch.int32, (n, cfg.top_k)),
-                            coef, z_coef, _array(counts, "counts", torch.int32, (E,)),
+    _check(lib().aa_balance(x, dt, ld, _count(count), n, E, C.byref(cfg), _flat(ids, "ids", torch.int32, (n, cfg.top_k)),
+                            coef, z_coef, _flat(counts, "counts", torch.int32, (E,)),
                             _vector(share, "share", E), _vector(loss, "loss", 2),
-                            *_scratch(ws, "a LayerWorkspace"), _stream()), "aa_balance")
+                            *_layer_scratch(ws), _stream()), "aa_balance")
 
 
 def balance_grad(logits, count, cfg, ids, dweights, counts, coef, z_coef, dloss, dlogits):
@@ -729,10 +753,10 @@ def balance_grad(logits, count, cfg, ids, dweights, counts, coef, z_coef, dloss,
     dt, x, ld, n, E = _first_rows(logits, "logits", DTYPES)
     out, ld_out = _rows_like(dlogits, "dlogits", logits.dtype, n, E)
     _check(lib().aa_balance_grad(x, dt, ld, _count(count), n, E, C.byref(cfg),
-                                 _array(ids, "ids", torch.int32, (n, cfg.top_k)),
-                                 _array(dweights, "dweights", torch.float32, (n, cfg.top_k)),
-                                 _array(counts, "counts", torch.int32, (E,)), coef, z_coef,
-                                 _array(dloss, "dloss", torch.float32, least=1), out, ld_out, _stream()),
+                                 _flat(ids, "ids", torch.int32, (n, cfg.top_k)),
+                                 _flat(dweights, "dweights", torch.float32, (n, cfg.top_k)),
+                                 _flat(counts, "counts", torch.int32, (E,)), coef, z_coef,
+                                 _flat(dloss, "dloss", torch.float32, least=1), out, ld_out, _stream()),
            "aa_balance_grad")
 
 
@@ -748,7 +772,7 @@ def adamw_tensor(param, grad, m, v, copy=None, m_scale=None, v_scale=None, decay
     state = torch.float8_e4m3fn if bits8 else torch.float32
 
     def flat(t, name, dtype, size=n):
-        p = _array(t, name, dtype)
+        p = _flat(t, name, dtype)
         _require(p is not None and t.numel() == size, f"{name}: {size} elements are needed")
         return p
 
@@ -785,20 +809,22 @@ def adamw_config(lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0)
 
 
 def _scalar(t, name, dtype=torch.float32):
-    return _array(t, name, dtype, least=1)
+    return _flat(t, name, dtype, least=1)
 
 
 def grad_norm(table, max_norm, scale, out):
     """out: float32 [2], the norm of all gradients and the factor for adamw_step; scale: a float32 tensor of one, or None."""
     _require(out is not None, "out: needed")
+    _here(table.buf, "table")
     _check(lib().aa_grad_norm(table.ptr, table.bytes, table.n, table.chunks, max_norm, _scalar(scale, "scale"),
-                              _array(out, "out", torch.float32, least=2), _stream()), "aa_grad_norm")
+                              _flat(out, "out", torch.float32, least=2), _stream()), "aa_grad_norm")
 
 
 def adamw_step(table, cfg, lr_factor, grad_factor, count, t):
     """lr_factor, grad_factor: float32 tensors of one, or None (1); count: an int32 tensor of one, or None; t: the int32 tensor of
     one that counts the updates."""
     _require(t is not None, "t: needed")
+    _here(table.buf, "table")
     _check(lib().aa_adamw_step(table.ptr, table.bytes, table.n, table.chunks, C.byref(cfg),
                                _scalar(lr_factor, "lr_factor"), _scalar(grad_factor, "grad_factor"), _count(count),
                                _scalar(t, "t", torch.int32), _stream()), "aa_adamw_step")

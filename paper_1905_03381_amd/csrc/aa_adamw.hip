@@ -28,13 +28,13 @@ struct EntryBatch {
 };
 
 // Entries [first, first + gridDim.x) of the table and the chunks that belong to them.
-__global__ __launch_bounds__(256) void k_adamw_table(char *table, int64_t map, int64_t n_chunks, int32_t first,
+__global__ __launch_bounds__(256) void k_adamw_table(char *table, int64_t map, int64_t n_chunks, int32_t n, int32_t first,
                                                      const EntryBatch batch) {
   const TensorEntry e = batch.e[blockIdx.x];
   const int32_t tensor = first + (int32_t)blockIdx.x;
   if (threadIdx.x == 0) reinterpret_cast<TensorEntry *>(table + kTableEntries)[tensor] = e;
   if (tensor == 0)
-    for (int w = threadIdx.x; w < kControlWords; w += 256) reinterpret_cast<int32_t *>(table)[w] = w == 0 ? (int32_t)n_chunks : 0;
+    for (int w = threadIdx.x; w < kControlWords; w += 256) reinterpret_cast<int32_t *>(table)[w] = w == 0 ? (int32_t)n_chunks : w == 1 ? n : 0;
   int32_t *of = reinterpret_cast<int32_t *>(table + map) + e.first_chunk;
   const int64_t chunks = (e.n + kChunk - 1) / kChunk;
   for (int64_t c = threadIdx.x; c < chunks; c += 256) of[c] = tensor;
@@ -92,14 +92,14 @@ __device__ __forceinline__ Eight load_grad(const TensorEntry &e, int64_t i, int 
 // neighbouring ones: what is known of a tensor is asked for once a part.
 template <typename Work>
 __device__ __forceinline__ void walk(const AdamWArgs &a, Work work) {
-  // (a number of chunks that is not the table's: nothing is walked; asked for with the first tensor, not before it)
-  const int listed = reinterpret_cast<const int32_t *>(a.table)[0];
+  // (numbers that are not the table's: nothing is walked; asked for with the first tensor, not before it)
+  const int chunks = reinterpret_cast<const int32_t *>(a.table)[0], tensors = reinterpret_cast<const int32_t *>(a.table)[1];
   const uint32_t all = (uint32_t)a.n_chunks, each = all / gridDim.x, more = all % gridDim.x;
   const int64_t begin = (int64_t)each * blockIdx.x + min(blockIdx.x, more);
   const int64_t end = begin + each + (blockIdx.x < more ? 1 : 0);
   for (int64_t c = begin; c < end;) {
     const int of_chunk = reinterpret_cast<const int32_t *>(a.table + a.map)[c];
-    if (listed != (int)a.n_chunks) return;
+    if (chunks != (int)a.n_chunks || tensors != a.n_tensors) return;
     const int tensor = __builtin_amdgcn_readfirstlane(of_chunk);
     const TensorEntry &e = reinterpret_cast<const TensorEntry *>(a.table + kTableEntries)[tensor];
     const int64_t next = e.first_chunk + (e.n + kChunk - 1) / kChunk, to = next < end ? next : end;
@@ -419,7 +419,7 @@ hipError_t launch_adamw_table(const aa_adamw_tensor *tensors, int32_t n, char *t
                     t.n,     chunk,        t.grad_dtype, t.copy_dtype, t.state_bits, t.decay};
       chunk += (t.n + kChunk - 1) / kChunk;
     }
-    hipLaunchKernelGGL(k_adamw_table, dim3(here), dim3(256), 0, st, table, map, n_chunks, first, batch);
+    hipLaunchKernelGGL(k_adamw_table, dim3(here), dim3(256), 0, st, table, map, n_chunks, n, first, batch);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

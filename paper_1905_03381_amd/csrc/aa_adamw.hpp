@@ -20,7 +20,7 @@ struct TensorEntry {
   float decay;
 };
 
-// The table: control words (the number of chunks, then for the norm and for the update the blocks that are done with the call),
+// The table: control words (the numbers of chunks and of tensors, then for the norm and for the update the blocks that are done with the call),
 // the norm's parts, the entries, and the tensor of each chunk.
 constexpr int kMostBlocks = 2048, kGroupBlocks = 32;  // of a launch; that count themselves together
 constexpr int kWordApart = 16;                        // int32 words between two that are counted in
@@ -36,6 +36,7 @@ inline size_t table_bytes(int64_t n_tensors, int64_t n_chunks) {
 struct AdamWArgs {
   char *table;
   int64_t map;  // byte offset of the chunks' tensors
+  int32_t n_tensors;
   int64_t n_chunks;
   aa_adamw_config cfg;
   float log_beta1, log_beta2;

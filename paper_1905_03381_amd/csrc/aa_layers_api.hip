@@ -9,6 +9,9 @@
 
 #include <math.h>
 
+#include <algorithm>
+#include <new>
+
 using namespace aa;
 
 namespace {
@@ -54,6 +57,44 @@ int32_t check_tensor(const aa_adamw_tensor &t) {
   const bool fits = on(t.param, 4) && on(t.grad, type_bytes(t.grad_dtype)) && on(t.copy, 2) && on(t.m, state) &&
                     on(t.v, state) && on(t.m_scale, 4) && on(t.v_scale, 4);
   return fits ? AA_OK : AA_ERR_ALIGN;
+}
+
+// Memory that a tensor of an update reads, or writes, too.
+struct Stretch {
+  uintptr_t from, to;
+  bool written;
+};
+
+// Whether any memory that is written is another tensor's, or the same tensor's, under another name: AA_ERR_SHAPE.
+int32_t check_apart(const aa_adamw_tensor *tensors, int32_t n) {
+  Stretch *all = new (std::nothrow) Stretch[(size_t)n * 7];
+  if (!all) return AA_ERR_HIP;
+  size_t k = 0;
+  const auto add = [&](const void *p, int64_t bytes, bool written) {
+    const uintptr_t from = reinterpret_cast<uintptr_t>(p);
+    if (p && bytes > 0) all[k++] = {from, from + (uintptr_t)bytes, written};
+  };
+  for (int32_t i = 0; i < n; ++i) {
+    const aa_adamw_tensor &t = tensors[i];
+    const int64_t scales = t.state_bits == 8 ? (t.n + kStateBlock - 1) / kStateBlock * 4 : 0;
+    add(t.param, t.n * 4, true);
+    add(t.grad, t.n * type_bytes(t.grad_dtype), false);
+    add(t.copy, t.n * 2, true);
+    add(t.m, t.n * (t.state_bits / 8), true);
+    add(t.v, t.n * (t.state_bits / 8), true);
+    add(t.m_scale, scales, true);
+    add(t.v_scale, scales, true);
+  }
+  std::sort(all, all + k, [](const Stretch &x, const Stretch &y) { return x.from < y.from; });
+  uintptr_t written = 0, any = 0;  // where what has been seen ends
+  bool apart = true;
+  for (size_t i = 0; i < k; ++i) {
+    apart = apart && all[i].from >= (all[i].written ? any : written);
+    any = std::max(any, all[i].to);
+    if (all[i].written) written = std::max(written, all[i].to);
+  }
+  delete[] all;
+  return apart ? AA_OK : AA_ERR_SHAPE;
 }
 
 // A table as aa_adamw_table made it.
@@ -277,6 +318,7 @@ int32_t aa_adamw_table(const aa_adamw_tensor *tensors, int32_t n_tensors, void *
   const int64_t chunks = aa_adamw_chunks(tensors, n_tensors);
   if (chunks < 0) return (int32_t)chunks;
   AA_TRY(check_table(table, table_bytes_, n_tensors, chunks));
+  AA_TRY(check_apart(tensors, n_tensors));
   return hip_status(launch_adamw_table(tensors, n_tensors, static_cast<char *>(table), as_stream(stream)));
 }
 
@@ -289,6 +331,7 @@ int32_t aa_grad_norm(void *table, size_t table_bytes_, int32_t n_tensors, int64_
   AdamWArgs a{};
   a.table = static_cast<char *>(table);
   a.map = (int64_t)table_map(n_tensors);
+  a.n_tensors = n_tensors;
   a.n_chunks = n_chunks;
   a.max_norm = max_norm;
   a.scale = scale;
@@ -312,6 +355,7 @@ int32_t aa_adamw_step(void *table, size_t table_bytes_, int32_t n_tensors, int64
   AdamWArgs a{};
   a.table = static_cast<char *>(table);
   a.map = (int64_t)table_map(n_tensors);
+  a.n_tensors = n_tensors;
   a.n_chunks = n_chunks;
   a.cfg = *cfg;
   a.log_beta1 = (float)log((double)cfg->beta1);

@@ -332,3 +332,61 @@ def test_many_elements():
     side.synchronize()
     x.check(0, old[0], 10)
     assert (x.p.storage_offset() == 5) and (f64(x.p.as_strided((3,), (1,), 5 + n)) == 0).all()
+
+
+def test_neighbours_and_shared_gradients():
+    """Tensors that touch each other in one piece of memory are apart, and one gradient may be two tensors'."""
+    n, m = 777, 512
+    p, g = normal((n + m,), F32, 1).cuda(), normal((n,), BF16, 2).cuda()
+    first, second = torch.zeros(n + m, device="cuda"), torch.zeros(n + m, device="cuda")
+    old = f64(p)
+    cut = lambda t: (t[:n], t[n:])
+    listed = [api.adamw_tensor(x, g[:x.numel()], a, b) for x, a, b in zip(cut(p), cut(first), cut(second))]
+    t = torch.zeros(1, dtype=torch.int32, device="cuda")
+    api.adamw_step(api.AdamWTable(listed), CFG_ALONE, None, None, None, t)
+    # after the first update of states that were 0 the step is lr g / (|g| + eps)
+    both = np.concatenate([f64(g), f64(g)[:m]])
+    want = -1e-2 * both / (np.abs(both) + 1e-8)
+    assert np.abs(f64(p) - old - want).max() < 1e-2 * 16 * U32 + 4 * 2 * U32
+    with pytest.raises(api.AAError):
+        api.AdamWTable(listed + listed[:1])
+
+
+CFG_ALONE = api.adamw_config(1e-2)
+
+
+def test_numbers_that_are_not_the_tables():
+    """A call whose numbers of tensors or chunks are others than the table's updates nothing."""
+    x = [Tensor(5000), Tensor(300)]
+    table = api.AdamWTable([k.listed() for k in x])
+    before = [k.p.clone() for k in x]
+    t, out = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(2, device="cuda")
+    for tensors, chunks in ((1, table.chunks), (2, table.chunks - 1)):
+        other = type("Other", (), dict(ptr=table.ptr, bytes=table.bytes, buf=table.buf, n=tensors, chunks=chunks))
+        api.adamw_step(other, CFG_ALONE, None, None, None, t)
+        api.grad_norm(other, 1.0, None, out)
+        assert out[0].item() == 0.0 and all(torch.equal(k.p, b) for k, b in zip(x, before))
+
+
+def test_another_device_is_refused(monkeypatch):
+    """Tensors of another device than the call's: here the call's device is said to be one that there is not."""
+    z = lambda *s, t=F32: torch.zeros(*s, dtype=t, device="cuda")
+    x, half, w, ws, c = z(4, 8), z(4, 8, t=BF16), z(8, 8, t=BF16), api.LayerWorkspace(8), z(1, t=torch.int32)
+    tensor = api.adamw_tensor(z(9), z(9), z(9), z(9))
+    table, cfg, ids, out = api.AdamWTable([tensor]), api.route_config("softmax", 2), z(4, 2, t=torch.int32), z(2)
+    calls = [lambda: api.layer_norm(x, None, None, 1e-5, None, x),
+             lambda: api.layer_norm_grad(x, x, None, z(4), z(4), None, None, x, z(8), z(8), False, ws),
+             lambda: api.linear(half, w, None, "none", None, None, z(4, 8, t=BF16)),
+             lambda: api.linear_grad(half, "none", None, c, None, z(8), False, ws),
+             lambda: api.balance(x, c, cfg, ids, 0.1, 0.1, z(8, t=torch.int32), None, None, ws),
+             lambda: api.balance_grad(x, c, cfg, None, None, z(8, t=torch.int32), 0.1, 0.1, None, x),
+             lambda: api.adamw_tensor(z(9), z(9), z(9), z(9)),
+             lambda: api.grad_norm(table, 1.0, None, out),
+             lambda: api.adamw_step(table, CFG_ALONE, None, None, None, c)]
+    for call in calls[:1] + calls[2:6]:
+        call()
+    torch.cuda.synchronize()
+    monkeypatch.setattr(api, "_device", lambda: 1)
+    for call in calls:
+        with pytest.raises(api.AAError, match="device"):
+            call()

@@ -203,3 +203,22 @@ def test_chunks_of_tensors(L):
     assert L.aa_adamw_table_bytes(3, 100) % 256 == 0 and L.aa_adamw_table_bytes(3, 100) < L.aa_adamw_table_bytes(300, 10_000)
     # a tensor without elements needs no memory
     assert L.aa_adamw_chunks(tensors(dict(n=0, param=None, grad=None, m=None, v=None)), 1) == 0
+
+
+def apart(*changes):
+    """tensors() with memory of their own, a megabyte for each array."""
+    fields = ("param", "grad", "copy", "m", "v", "m_scale", "v_scale")
+    place = lambda k: {f: P + ((k * len(fields) + i) << 20) for i, f in enumerate(fields)}
+    return tensors(*(dict(place(k), state_bits=8, **change) for k, change in enumerate(changes)))
+
+
+TWICE = [("param", "param", 0), ("param", "grad", 0), ("copy", "copy", 0), ("copy", "param", 19_996), ("m", "v", 4999),
+         ("v", "v", 0), ("m_scale", "m_scale", 76), ("v_scale", "m", 0), ("grad", "copy", 9998), ("grad", "v_scale", 0)]
+
+
+@pytest.mark.parametrize("field,other,by,same", [(f, o, by, s) for f, o, by in TWICE for s in (False, True) if not s or f != o])
+def test_memory_listed_twice_is_refused(L, field, other, by, same):
+    pair = apart({}, {})
+    setattr(pair[1], field, getattr(pair[1 if same else 0], other) + by)
+    call = dict(TABLE, tensors=pair)
+    assert L.aa_adamw_table(*call.values()) == SHAPE
