@@ -615,25 +615,27 @@ class LayerWorkspace:
         _take(self, int(lib().aa_layer_workspace_bytes(d_max)), device)
 
 
-def _current():
-    return torch.cuda.current_device() if _device is None else _device()
+_current = _device or torch.cuda.current_device
+_stream_on = _raw_stream or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _here(t, name):
+def _here(t, name, device):
     """A GPU tensor is on the device that the call's stream is of."""
-    if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != _current():
-        raise AAError(f"{name}: on device {t.get_device()}, the current one is {_current()}")
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != device:
+        raise AAError(f"{name}: on device {t.get_device()}, the call's is {device}")
 
 
-def _flat(t, name, dtype, shape=None, least=0):
-    """_array of a tensor on the current device."""
-    _here(t, name)
+def _flat(t, name, device, dtype, shape=None, least=0):
+    """_array of a tensor on the call's device."""
+    if t is None:
+        return None
+    _here(t, name, device)
     return _array(t, name, dtype, shape, least)
 
 
-def _layer_scratch(ws):
+def _layer_scratch(ws, device):
     scratch = _scratch(ws, "a LayerWorkspace")
-    _here(ws.buf, "ws")
+    _here(ws.buf, "ws", device)
     return scratch
 
 
@@ -642,45 +644,52 @@ def _layer_scratch(ws):
 _F32, _I32, _Tensor = torch.float32, torch.int32, torch.Tensor
 
 
-def _count(count):
-    if count is None:
+def _scalar(t, name, device, dtype=_F32):
+    """Pointer of one value; None stays None."""
+    if t is None:
         return None
-    if type(count) is _Tensor and count.dtype is _I32 and count.is_cuda and count.get_device() == _current() and count.dim() == 1 and count.numel() == 1:
-        return count.data_ptr()
-    return _flat(count, "count", _I32, least=1)
+    if type(t) is _Tensor and t.dtype is dtype and t.get_device() == device and t.shape == (1,):
+        return t.data_ptr()
+    return _flat(t, name, device, dtype, least=1)
 
 
-def _vector(t, name, n):
+def _count(count, device):
+    return _scalar(count, "count", device, _I32)
+
+
+def _vector(t, name, device, n):
     """Pointer of n neighbouring float32 values; None stays None."""
     if t is None:
         return None
-    if type(t) is _Tensor and t.dtype is _F32 and t.is_cuda and t.get_device() == _current() and t.shape == (n,) and t.is_contiguous():
+    if type(t) is _Tensor and t.dtype is _F32 and t.get_device() == device and t.shape == (n,) and t.is_contiguous():
         return t.data_ptr()
-    return _flat(t, name, _F32, (n,))
+    return _flat(t, name, device, _F32, (n,))
 
 
-def _rows_like(t, name, dtype, n, d):
+def _rows_like(t, name, device, dtype, n, d):
     """(pointer, row stride) of n rows of d neighbouring columns of the given type (or more rows)."""
-    if type(t) is _Tensor and t.dtype is dtype and t.is_cuda and t.get_device() == _current() and t.shape == (n, d):
+    if type(t) is _Tensor and t.dtype is dtype and t.get_device() == device and t.shape == (n, d):
         ld, step = t.stride()
         if step == 1:
             return t.data_ptr(), ld if n > 1 else d
-    _here(t, name)
+    _here(t, name, device)
     return _matrix(t, name, dtype, d, n)
 
 
 def _first_rows(t, name, types):
-    """(type code, pointer, row stride, rows, columns) of the matrix that a call's sizes and type come from."""
-    if type(t) is _Tensor and t.is_cuda and t.get_device() == _current() and t.dim() == 2:
-        code = types.get(t.dtype)
+    """(device, type code, pointer, row stride, rows, columns) of the matrix that a call's device, sizes and type come from."""
+    if type(t) is _Tensor and t.is_cuda and t.dim() == 2:
+        device, code = _current(), types.get(t.dtype)
         n, d = t.shape
         ld, step = t.stride()
-        if code is not None and step == 1:
-            return code, t.data_ptr(), ld if n > 1 else d, n, d
-    _here(t, name)
+        if code is not None and step == 1 and t.get_device() == device:
+            return device, code, t.data_ptr(), ld if n > 1 else d, n, d
+        _here(t, name, device)
     code = _type(t, name, types is _HALVES)
     p, ld = _matrix(t, name)
-    return code, p, ld, t.shape[0], t.shape[1]
+    device = _current()
+    _here(t, name, device)
+    return device, code, p, ld, t.shape[0], t.shape[1]
 
 
 _HALVES = {t: c for t, c in DTYPES.items() if t is not _F32}
@@ -688,75 +697,77 @@ _HALVES = {t: c for t, c in DTYPES.items() if t is not _F32}
 
 def layer_norm(x, gamma, beta, eps, count, out, mean=None, rstd=None):
     """gamma, beta: float32 [d] or None (1 and 0); mean, rstd: float32 [n], for the backward pass."""
-    dt, xp, ldx, n, d = _first_rows(x, "x", DTYPES)
-    op, ldo = _rows_like(out, "out", x.dtype, n, d)
-    _check(lib().aa_layer_norm(xp, dt, ldx, _count(count), n, d, _vector(gamma, "gamma", d), _vector(beta, "beta", d), eps,
-                               op, ldo, _vector(mean, "mean", n), _vector(rstd, "rstd", n), _stream()), "aa_layer_norm")
+    dev, dt, xp, ldx, n, d = _first_rows(x, "x", DTYPES)
+    op, ldo = _rows_like(out, "out", dev, x.dtype, n, d)
+    _check(lib().aa_layer_norm(xp, dt, ldx, _count(count, dev), n, d, _vector(gamma, "gamma", dev, d),
+                               _vector(beta, "beta", dev, d), eps, op, ldo, _vector(mean, "mean", dev, n),
+                               _vector(rstd, "rstd", dev, n), _stream_on(dev)), "aa_layer_norm")
 
 
 def layer_norm_grad(dout, x, gamma, mean, rstd, residual, count, dx, dgamma, dbeta, accumulate, ws):
     """residual: what is added to dx, or None; dgamma, dbeta: either may be None, and ws where both are."""
-    dt, gp, ldg, n, d = _first_rows(dout, "dout", DTYPES)
-    xp, ldx = _rows_like(x, "x", dout.dtype, n, d)
-    rp, ldr = (None, 0) if residual is None else _rows_like(residual, "residual", dout.dtype, n, d)
-    op, ldo = _rows_like(dx, "dx", dout.dtype, n, d)
-    scratch = (None, 0) if dgamma is None and dbeta is None else _layer_scratch(ws)
-    _check(lib().aa_layer_norm_grad(gp, dt, ldg, xp, ldx, _count(count), n, d,
-                                    _vector(gamma, "gamma", d), _vector(mean, "mean", n), _vector(rstd, "rstd", n), rp, ldr,
-                                    op, ldo, _vector(dgamma, "dgamma", d), _vector(dbeta, "dbeta", d),
-                                    int(bool(accumulate)), *scratch, _stream()), "aa_layer_norm_grad")
+    dev, dt, gp, ldg, n, d = _first_rows(dout, "dout", DTYPES)
+    xp, ldx = _rows_like(x, "x", dev, dout.dtype, n, d)
+    rp, ldr = (None, 0) if residual is None else _rows_like(residual, "residual", dev, dout.dtype, n, d)
+    op, ldo = _rows_like(dx, "dx", dev, dout.dtype, n, d)
+    scratch = (None, 0) if dgamma is None and dbeta is None else _layer_scratch(ws, dev)
+    _check(lib().aa_layer_norm_grad(gp, dt, ldg, xp, ldx, _count(count, dev), n, d,
+                                    _vector(gamma, "gamma", dev, d), _vector(mean, "mean", dev, n),
+                                    _vector(rstd, "rstd", dev, n), rp, ldr, op, ldo,
+                                    _vector(dgamma, "dgamma", dev, d), _vector(dbeta, "dbeta", dev, d),
+                                    int(bool(accumulate)), *scratch, _stream_on(dev)), "aa_layer_norm_grad")
 
 
 def linear(x, w, bias, act, residual, count, out, pre=None):
     """w [d_out, d_in] (gated: [2 d_out, d_in]) and bias (float32, or None) for all rows; pre: what the activation is taken
     of, for the backward pass."""
     a = _name_of(DENSE_ACTIVATIONS, act, "act")
-    dt, xp, ldx, n, d_in = _first_rows(x, "x", _HALVES)
+    dev, dt, xp, ldx, n, d_in = _first_rows(x, "x", _HALVES)
     _require(isinstance(w, torch.Tensor) and w.dim() == 2 and w.shape[1] == d_in, "w: [rows, d_in]")
     wide, dtype = w.shape[0], x.dtype
     _require(a != 2 or wide % 2 == 0, "w: [rows, d_in]")
     d_out = wide // 2 if a == 2 else wide
-    op, ldo = _rows_like(out, "out", dtype, n, d_out)
-    rp, ldr = (None, 0) if residual is None else _rows_like(residual, "residual", dtype, n, d_out)
-    pp, ldp = (None, 0) if pre is None else _rows_like(pre, "pre", dtype, n, wide)
-    _check(lib().aa_linear(xp, dt, ldx, _count(count), n, d_in, d_out, _flat(w, "w", dtype),
-                           _vector(bias, "bias", wide), a, rp, ldr, op, ldo, pp, ldp, _stream()),
+    op, ldo = _rows_like(out, "out", dev, dtype, n, d_out)
+    rp, ldr = (None, 0) if residual is None else _rows_like(residual, "residual", dev, dtype, n, d_out)
+    pp, ldp = (None, 0) if pre is None else _rows_like(pre, "pre", dev, dtype, n, wide)
+    _check(lib().aa_linear(xp, dt, ldx, _count(count, dev), n, d_in, d_out, _flat(w, "w", dev, dtype),
+                           _vector(bias, "bias", dev, wide), a, rp, ldr, op, ldo, pp, ldp, _stream_on(dev)),
            "aa_linear")
 
 
 def linear_grad(dout, act, pre, count, dpre, dbias, accumulate, ws):
     """pre: not needed without an activation; dpre or dbias may be None, and ws where dbias is."""
     a = _name_of(DENSE_ACTIVATIONS, act, "act")
-    dt, gp, ldg, n, d = _first_rows(dout, "dout", _HALVES)
+    dev, dt, gp, ldg, n, d = _first_rows(dout, "dout", _HALVES)
     dtype = dout.dtype
     wide = 2 * d if a == 2 else d
-    pp, ldp = (None, 0) if a == 0 else _rows_like(pre, "pre", dtype, n, wide)
-    op, ldo = (None, 0) if dpre is None else _rows_like(dpre, "dpre", dtype, n, wide)
-    scratch = (None, 0) if dbias is None else _layer_scratch(ws)
-    _check(lib().aa_linear_grad(gp, dt, ldg, _count(count), n, d, a, pp, ldp, op, ldo,
-                                _vector(dbias, "dbias", wide), int(bool(accumulate)), *scratch,
-                                _stream()), "aa_linear_grad")
+    pp, ldp = (None, 0) if a == 0 else _rows_like(pre, "pre", dev, dtype, n, wide)
+    op, ldo = (None, 0) if dpre is None else _rows_like(dpre, "dpre", dev, dtype, n, wide)
+    scratch = (None, 0) if dbias is None else _layer_scratch(ws, dev)
+    _check(lib().aa_linear_grad(gp, dt, ldg, _count(count, dev), n, d, a, pp, ldp, op, ldo,
+                                _vector(dbias, "dbias", dev, wide), int(bool(accumulate)), *scratch,
+                                _stream_on(dev)), "aa_linear_grad")
 
 
 def balance(logits, count, cfg, ids, coef, z_coef, counts, share, loss, ws):
     """counts: int32 [E]; share: float32 [E] or None; loss: float32 [2] or None; ws: a LayerWorkspace of E columns."""
-    dt, x, ld, n, E = _first_rows(logits, "logits", DTYPES)
+    dev, dt, x, ld, n, E = _first_rows(logits, "logits", DTYPES)
     _require(counts is not None, "counts: needed")
-    _check(lib().aa_balance(x, dt, ld, _count(count), n, E, C.byref(cfg), _flat(ids, "ids", torch.int32, (n, cfg.top_k)),
-                            coef, z_coef, _flat(counts, "counts", torch.int32, (E,)),
-                            _vector(share, "share", E), _vector(loss, "loss", 2),
-                            *_layer_scratch(ws), _stream()), "aa_balance")
+    _check(lib().aa_balance(x, dt, ld, _count(count, dev), n, E, C.byref(cfg),
+                            _flat(ids, "ids", dev, torch.int32, (n, cfg.top_k)), coef, z_coef,
+                            _flat(counts, "counts", dev, torch.int32, (E,)), _vector(share, "share", dev, E), _vector(loss, "loss", dev, 2),
+                            *_layer_scratch(ws, dev), _stream_on(dev)), "aa_balance")
 
 
 def balance_grad(logits, count, cfg, ids, dweights, counts, coef, z_coef, dloss, dlogits):
     """dweights None: the balance loss alone (ids is then not read and may be None); dloss: a float32 tensor of one, or None."""
-    dt, x, ld, n, E = _first_rows(logits, "logits", DTYPES)
-    out, ld_out = _rows_like(dlogits, "dlogits", logits.dtype, n, E)
-    _check(lib().aa_balance_grad(x, dt, ld, _count(count), n, E, C.byref(cfg),
-                                 _flat(ids, "ids", torch.int32, (n, cfg.top_k)),
-                                 _flat(dweights, "dweights", torch.float32, (n, cfg.top_k)),
-                                 _flat(counts, "counts", torch.int32, (E,)), coef, z_coef,
-                                 _flat(dloss, "dloss", torch.float32, least=1), out, ld_out, _stream()),
+    dev, dt, x, ld, n, E = _first_rows(logits, "logits", DTYPES)
+    out, ld_out = _rows_like(dlogits, "dlogits", dev, logits.dtype, n, E)
+    _check(lib().aa_balance_grad(x, dt, ld, _count(count, dev), n, E, C.byref(cfg),
+                                 _flat(ids, "ids", dev, torch.int32, (n, cfg.top_k)),
+                                 _flat(dweights, "dweights", dev, torch.float32, (n, cfg.top_k)),
+                                 _flat(counts, "counts", dev, torch.int32, (E,)), coef, z_coef,
+                                 _flat(dloss, "dloss", dev, torch.float32, least=1), out, ld_out, _stream_on(dev)),
            "aa_balance_grad")
 
 
@@ -769,10 +780,10 @@ def adamw_tensor(param, grad, m, v, copy=None, m_scale=None, v_scale=None, decay
     _require(isinstance(param, torch.Tensor), "param: a tensor")
     n, bits8 = param.numel(), isinstance(m, torch.Tensor) and m.dtype == torch.float8_e4m3fn
     code = _type(grad, "grad")
-    state = torch.float8_e4m3fn if bits8 else torch.float32
+    state, device = torch.float8_e4m3fn if bits8 else torch.float32, param.get_device()
 
     def flat(t, name, dtype, size=n):
-        p = _flat(t, name, dtype)
+        p = _flat(t, name, device, dtype)
         _require(p is not None and t.numel() == size, f"{name}: {size} elements are needed")
         return p
 
@@ -801,30 +812,31 @@ class AdamWTable:
         self.bytes = int(lib().aa_adamw_table_bytes(self.n, self.chunks))
         self.buf = torch.empty(self.bytes + 256, dtype=torch.uint8, device=device)
         self.ptr = self.buf.data_ptr() + (-self.buf.data_ptr()) % 256
-        _check(lib().aa_adamw_table(listed, self.n, self.ptr, self.bytes, _stream()), "aa_adamw_table")
+        dev = self.device = _current()
+        for t in [self.buf] + [t[0] for t in self._tensors]:
+            _here(t, "tensors", dev)
+        _check(lib().aa_adamw_table(listed, self.n, self.ptr, self.bytes, _stream_on(dev)), "aa_adamw_table")
 
 
 def adamw_config(lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.0, seed=0):
     return aa_adamw_config(lr, beta1, beta2, eps, weight_decay, 0, seed)
 
 
-def _scalar(t, name, dtype=torch.float32):
-    return _flat(t, name, dtype, least=1)
-
-
 def grad_norm(table, max_norm, scale, out):
     """out: float32 [2], the norm of all gradients and the factor for adamw_step; scale: a float32 tensor of one, or None."""
     _require(out is not None, "out: needed")
-    _here(table.buf, "table")
-    _check(lib().aa_grad_norm(table.ptr, table.bytes, table.n, table.chunks, max_norm, _scalar(scale, "scale"),
-                              _flat(out, "out", torch.float32, least=2), _stream()), "aa_grad_norm")
+    dev = _current()
+    _require(table.device == dev, "table: on another device than the current one")
+    _check(lib().aa_grad_norm(table.ptr, table.bytes, table.n, table.chunks, max_norm, _scalar(scale, "scale", dev),
+                              _flat(out, "out", dev, torch.float32, least=2), _stream_on(dev)), "aa_grad_norm")
 
 
 def adamw_step(table, cfg, lr_factor, grad_factor, count, t):
     """lr_factor, grad_factor: float32 tensors of one, or None (1); count: an int32 tensor of one, or None; t: the int32 tensor of
     one that counts the updates."""
     _require(t is not None, "t: needed")
-    _here(table.buf, "table")
+    dev = _current()
+    _require(table.device == dev, "table: on another device than the current one")
     _check(lib().aa_adamw_step(table.ptr, table.bytes, table.n, table.chunks, C.byref(cfg),
-                               _scalar(lr_factor, "lr_factor"), _scalar(grad_factor, "grad_factor"), _count(count),
-                               _scalar(t, "t", torch.int32), _stream()), "aa_adamw_step")
+                               _scalar(lr_factor, "lr_factor", dev), _scalar(grad_factor, "grad_factor", dev), _count(count, dev),
+                               _scalar(t, "t", dev, torch.int32), _stream_on(dev)), "aa_adamw_step")

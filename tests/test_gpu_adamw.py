@@ -362,7 +362,7 @@ def test_numbers_that_are_not_the_tables():
     before = [k.p.clone() for k in x]
     t, out = torch.zeros(1, dtype=torch.int32, device="cuda"), torch.zeros(2, device="cuda")
     for tensors, chunks in ((1, table.chunks), (2, table.chunks - 1)):
-        other = type("Other", (), dict(ptr=table.ptr, bytes=table.bytes, buf=table.buf, n=tensors, chunks=chunks))
+        other = type("Other", (), dict(ptr=table.ptr, bytes=table.bytes, device=table.device, n=tensors, chunks=chunks))
         api.adamw_step(other, CFG_ALONE, None, None, None, t)
         api.grad_norm(other, 1.0, None, out)
         assert out[0].item() == 0.0 and all(torch.equal(k.p, b) for k, b in zip(x, before))
@@ -380,13 +380,13 @@ def test_another_device_is_refused(monkeypatch):
              lambda: api.linear_grad(half, "none", None, c, None, z(8), False, ws),
              lambda: api.balance(x, c, cfg, ids, 0.1, 0.1, z(8, t=torch.int32), None, None, ws),
              lambda: api.balance_grad(x, c, cfg, None, None, z(8, t=torch.int32), 0.1, 0.1, None, x),
-             lambda: api.adamw_tensor(z(9), z(9), z(9), z(9)),
+             lambda: api.AdamWTable([tensor]),
              lambda: api.grad_norm(table, 1.0, None, out),
              lambda: api.adamw_step(table, CFG_ALONE, None, None, None, c)]
     for call in calls[:1] + calls[2:6]:
         call()
     torch.cuda.synchronize()
-    monkeypatch.setattr(api, "_device", lambda: 1)
+    monkeypatch.setattr(api, "_current", lambda: 1)
     for call in calls:
         with pytest.raises(api.AAError, match="device"):
             call()
