@@ -117,7 +117,8 @@ hipError_t act_grad(ActGradArgs a, hipStream_t st) {
   // four, 30,000 x 5000 139 and 129; 6001 x 1536 13.6 and 14.9; of lines off 16 bytes 50,000 x 1100 82 and 104), no more than
   // there are rows or the workspace has room for.
   const bool much = a.d % 8 == 0 && (int64_t)a.n_max * a.d >= 16ll << 20;
-  const int64_t stripes = ((int64_t)a.d + CL * 8 - 1) / (CL * 8), fill = (much ? 1024 : 2048) / stripes, turns = ((int64_t)a.n_max + kRows - 1) / kRows;
+  const int64_t stripes = ((int64_t)a.d + CL * 8 - 1) / (CL * 8), fill = (much ? 1024 : 2048) / stripes;
+  const int64_t turns = ((int64_t)a.n_max + kRows - 1) / kRows;
   const int64_t room = column_parts((int64_t)a.d * kHalves);
   int64_t parts = fill < turns ? fill : turns;
   parts = parts < room ? parts : room;
