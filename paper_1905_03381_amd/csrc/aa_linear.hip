@@ -115,14 +115,15 @@ hipError_t act_grad(ActGradArgs a, hipStream_t st) {
   constexpr int kRows = 256 / CL, kHalves = ACT == AA_ACT_GATED ? 2 : 1;
   // Parts: eight blocks a compute unit, four where each still has much to do (bf16: 16,384 x 8192 gelu 166 us by eight, 155 by
   // four, 30,000 x 5000 139 and 129; 6001 x 1536 13.6 and 14.9; of lines off 16 bytes 50,000 x 1100 82 and 104), no more than
-  // there are rows or the workspace has room for.
+  // there are rows or the workspace has room for, and one where eight turns have them all (32 x 1024 6.6 us, in parts 9.3;
+  // sixteen turns 11.2 and 9.2), of 16 lanes four (64 x 100 6.2 and 9.2, eight turns 10.4 and 9.1).
   const bool much = a.d % 8 == 0 && (int64_t)a.n_max * a.d >= 16ll << 20;
   const int64_t stripes = ((int64_t)a.d + CL * 8 - 1) / (CL * 8), fill = (much ? 1024 : 2048) / stripes;
   const int64_t turns = ((int64_t)a.n_max + kRows - 1) / kRows;
   const int64_t room = column_parts((int64_t)a.d * kHalves);
   int64_t parts = fill < turns ? fill : turns;
   parts = parts < room ? parts : room;
-  a.parts = (int32_t)(parts > 1 ? parts : 1);
+  a.parts = (int32_t)(parts > 1 && turns > (CL == 16 ? 4 : 8) ? parts : 1);
   hipLaunchKernelGGL((k_act_grad<T, ACT, CL>), dim3((uint32_t)stripes, (uint32_t)a.parts), dim3(256), 0, st, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !a.dbias || a.parts == 1) return e;

@@ -515,7 +515,9 @@ hipError_t layer_norm_grad(const NormArgs &a, hipStream_t st) {
       [&](auto tpr, auto nv) {
         constexpr int TPR = decltype(tpr)::value, NV = decltype(nv)::value, kRows = kGradThreads / TPR;
         const int64_t want = ((int64_t)a.n_max + kRows - 1) / kRows;
-        const int parts = (int)(want < most ? want : most);
+        // (a block that is alone takes four turns in less than a second launch does: 32 rows of 1024 7.9 us, in parts 10.9; eight
+        // turns 12.8 and 10.8)
+        const int parts = want <= 4 ? 1 : (int)(want < most ? want : most);
         const dim3 grid(parts), block(kGradThreads);
         if (passing<T>(a)) hipLaunchKernelGGL((k_layer_norm_grad<T, TPR, NV, true>), grid, block, 0, st, a);
         else hipLaunchKernelGGL((k_layer_norm_grad<T, TPR, NV, false>), grid, block, 0, st, a);
