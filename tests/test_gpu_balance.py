@@ -83,6 +83,16 @@ def test_rows(n, count, E, K, kind):
     check_balance(x, ids, kind, count, run(x, ids, kind, count))
 
 
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("n", [15, 32, 33, 64, 65, 128, 129, 256, 257])
+@pytest.mark.parametrize("E,K", [(8, 2), (64, 6), (200, 8), (700, 9)])
+def test_turns_of_one_block(n, E, K, kind):
+    """Either side of the rows that a block takes alone."""
+    x, ids = case(n, E, K, F32, n)
+    x, ids = x.cuda(), ids.cuda()
+    check_balance(x, ids, kind, n - 1, run(x, ids, kind, n - 1))
+
+
 @pytest.mark.parametrize("n", [60, 3000])
 def test_counts_alone_and_rows_that_are_not_in_use(n):
     x, ids = case(n, 64, 4, BF16, 7)

@@ -268,3 +268,13 @@ def test_far_rows():
     mean, rstd = statistics(x)
     dout = normal((n, d), BF16, 4).cuda()
     check_grad(dout, x, np.ones(d), mean, rstd, None, None, run_grad(dout, x, None, mean, rstd, None, None))
+
+
+@pytest.mark.parametrize("d", [120, 500, 1000, 2000, 5000, 9000])
+@pytest.mark.parametrize("n", [2, 4, 5, 16, 32, 33, 128, 129])
+def test_turns_of_one_block(n, d):
+    """Either side of the rows that a block takes alone."""
+    x, dout = rows(n, d, BF16, d).cuda(), normal((n, d), BF16, d + 9).cuda()
+    gamma, _, g64, _ = vectors(d, d + 50)
+    mean, rstd = statistics(x)
+    check_grad(dout, x, g64, mean, rstd, None, n - 1, run_grad(dout, x, gamma, mean, rstd, None, n - 1))

@@ -153,6 +153,17 @@ def test_grad_sizes(n, d, act):
         check_grad(dout, act, pre, None, got, accumulate=i == 1)
 
 
+@pytest.mark.parametrize("act", ["none", "gelu", "gated"])
+@pytest.mark.parametrize("n", [4, 5, 32, 33, 64, 65])
+@pytest.mark.parametrize("d", [100, 384, 385, 1000])
+def test_turns_of_one_block(n, d, act):
+    """Either side of the rows that a block takes alone."""
+    dout, pre = normal((n, d), BF16, 1).cuda(), normal((n, 2 * d if act == "gated" else d), BF16, 2).cuda()
+    pre = None if act == "none" else pre
+    got = run_grad(dout, act, pre, n - 1, accumulate=n % 2 == 0)
+    check_grad(dout, act, pre, n - 1, got, accumulate=n % 2 == 0)
+
+
 @pytest.mark.parametrize("count", [0, -1, 1, 77, 500])
 @pytest.mark.parametrize("act", ["none", "gelu", "gated"])
 def test_grad_rows_in_use(count, act):
