@@ -541,8 +541,8 @@ int32_t aa_linear(const void *x, int32_t dtype, int64_t ldx, const int32_t *coun
                   int32_t d_out, const void *w, const float *bias, int32_t act, const void *residual, int64_t ldr,
                   void *out, int64_t ldo, void *pre, int64_t ldpre, void *stream);
 
-/* Its gradient as far as h: dpre[t] = dout[t] act'(pre[t]) (AA_ACT_GATED: the gate's, then up's, 2 d_out wide), and
- * dbias = the sum of dpre over the rows in use, before it is rounded (accumulate != 0 adds to what dbias
+/* Its gradient as far as h: dpre[t] = dout[t] act'(pre[t]) in dtype, what the products below take (AA_ACT_GATED: the gate's,
+ * then up's, 2 d_out wide), and dbias = the sum of dpre over the rows in use, before it is rounded (accumulate != 0 adds to what dbias
  * holds; no rows: zeros, or nothing).  dpre or dbias may be NULL, not both; pre is not read with AA_ACT_NONE.
  * dpre may be pre, and but for AA_ACT_GATED dout.  ws is needed where dbias is (d_max: dbias' columns).  The
  * gradients of x and w are those of a block of one expert: aa_expert_grad_input and aa_expert_grad_weight of dpre

@@ -39,6 +39,10 @@ __device__ __forceinline__ float through(float d, float h, float up, float *du) 
 }
 
 // CL lanes along the columns, 256 / CL rows at a time; blockIdx.y: the part.  6001 x 1544 f16, silu: 15.6 us, 3.6 TB/s.
+// dpre is rounded to the rows' 16 bits (without an activation it is dout, and nothing is rounded): it is what the matrix
+// instructions of the gradients of rows and matrix take, and as much as dout itself holds.  Each of their terms is then off by
+// half a step (6001 x 1000 -> 1544 silu f16: results furthest from 64 bits by 2.9e-4 of them, from a dpre of 32 bits 2.1e-4).
+// What the rounding takes away, multiplied as well, would be the products' work a second time.
 template <typename T, int ACT, int CL>
 __global__ __launch_bounds__(256) void k_act_grad(const ActGradArgs a) {
   constexpr int kRows = 256 / CL, kHalves = ACT == AA_ACT_GATED ? 2 : 1;

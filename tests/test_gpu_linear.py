@@ -279,3 +279,30 @@ def test_far_rows():
     layer.check(out, None)
     dpre, dbias = run_grad(out, "silu", x, None, dpre=out)
     assert np.isfinite(f64(dpre)).all() and np.isfinite(f64(dbias)).all()
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("n,count,d_in,d_out", [(700, 601, 100, 154), (300, 300, 128, 96), (40, 33, 65, 33)])
+@pytest.mark.parametrize("dtype", HALVES)
+def test_gradients_through_a_dpre_of_16_bits(dtype, n, count, d_in, d_out, act):
+    """The gradients of the rows and of the matrix are those of dpre as the products take it, in 16 bits: beyond their own sums'
+    and results' roundings nothing is lost, and against 64 bits throughout each term is off by dpre's half step."""
+    layer = Layer(n, d_in, d_out, act, dtype, count=count, seed=d_in)
+    m, wide, u = count, layer.wide, half_step(dtype)
+    pre = None if act == "none" else normal((n, wide), dtype, 3, 2.0).cuda()
+    dout = normal((n, d_out), dtype, 4).cuda()
+    dpre, _ = run_grad(dout, act, pre, count)
+    group = torch.tensor([0, m], dtype=torch.int32, device="cuda")
+    dx, dw = torch.zeros_like(layer.x), torch.zeros(1, wide, d_in, device="cuda")
+    api.expert_grad_input(dpre, group, layer.w[None], "none", None, dx)
+    api.expert_grad_weight(dpre, layer.x, None, 1, group, dw, False, api.ExpertWorkspace(n, 1, 1))
+    d, off = R.linear_grad(f64(dout)[:m], None if pre is None else f64(pre)[:m], act) if act != "none" else \
+        (f64(dout)[:m], 0.0 * f64(dout)[:m])
+    off = off + (u * (np.abs(d) + off) + tiny(dtype)) * (act != "none")
+    held, x, w = f64(dpre)[:m], f64(layer.x)[:m], f64(layer.w)
+    for got, mul, ends, depth, half in ((f64(dx)[:m], lambda v: v @ w, lambda v: v @ np.abs(w), wide, u),
+                                        (f64(dw)[0], lambda v: v.T @ x, lambda v: v.T @ np.abs(x), m, 0.0)):
+        own = (depth + 64) * U32 * ends(np.abs(held))
+        check(got, mul(held), own + half * (np.abs(mul(held)) + own) + tiny(dtype), "of the dpre that is held")
+        both = own + ends(off)
+        check(got, mul(d), both + half * (np.abs(mul(d)) + both) + tiny(dtype), "of dpre in 64 bits")
