@@ -544,6 +544,7 @@ int32_t aa_linear(const void *x, int32_t dtype, int64_t ldx, const int32_t *coun
 /* Its gradient as far as h: dpre[t] = dout[t] act'(pre[t]) in dtype, what the products below take (AA_ACT_GATED: the gate's,
  * then up's, 2 d_out wide), and dbias = the sum of dpre over the rows in use, before it is rounded (accumulate != 0 adds to what dbias
  * holds; no rows: zeros, or nothing).  dpre or dbias may be NULL, not both; pre is not read with AA_ACT_NONE.
+ * A NaN in pre is handed on, but for AA_ACT_RELU, whose gradient is dout where pre > 0 and 0 elsewhere.
  * dpre may be pre, and but for AA_ACT_GATED dout.  ws is needed where dbias is (d_max: dbias' columns).  The
  * gradients of x and w are those of a block of one expert: aa_expert_grad_input and aa_expert_grad_weight of dpre
  * with offsets {0, m}; that of residual is dout. */

@@ -29,9 +29,9 @@ __device__ __forceinline__ float through(float d, float h, float up, float *du) 
     return d * (z + h * z * (1.f - z));
   }
   if (ACT == AA_ACT_GELU) {
-    // (beyond 20 the sigmoid is 0 or 1 in 32 bits, and h^2 no concern)
+    // (beyond 20 the sigmoid is 0 or 1 in 32 bits, and h^2 no concern; a NaN stays one)
     constexpr float k = 1.5957691216057308f;
-    h = fminf(fmaxf(h, -20.f), 20.f);
+    h = h < -20.f ? -20.f : h > 20.f ? 20.f : h;
     const float z = sigmoid_near(gelu_argument(h));
     return d * (z + h * z * (1.f - z) * (k + 3.f * k * 0.044715f * h * h));
   }

@@ -306,3 +306,21 @@ def test_gradients_through_a_dpre_of_16_bits(dtype, n, count, d_in, d_out, act):
         check(got, mul(held), own + half * (np.abs(mul(held)) + own) + tiny(dtype), "of the dpre that is held")
         both = own + ends(off)
         check(got, mul(d), both + half * (np.abs(mul(d)) + both) + tiny(dtype), "of dpre in 64 bits")
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gated"])
+@pytest.mark.parametrize("n,d", [(9, 40), (9, 41), (700, 520)])
+def test_grad_of_what_is_not_a_number(n, d, act):
+    """A NaN that went into the activation comes out of its gradient, there and in its column's sum, and nowhere else."""
+    wide = 2 * d if act == "gated" else d
+    for dtype in HALVES:
+        dout, pre = normal((n, d), dtype, 1).cuda(), normal((n, wide), dtype, 2).cuda()
+        at = [(0, 0), (3, 7), (n - 1, d - 1)]
+        for i, j in at:
+            pre[i, j] = float("nan")
+        ill = np.zeros((n, d), bool)
+        ill[tuple(zip(*at))] = True
+        dpre, dbias = run_grad(dout, act, pre, None)
+        ill = np.concatenate([ill, ill], 1) if act == "gated" else ill
+        assert (np.isnan(f64(dpre)) == ill).all()
+        assert (np.isnan(f64(dbias)) == ill.any(0)).all()
