@@ -390,3 +390,24 @@ def test_another_device_is_refused(monkeypatch):
     for call in calls:
         with pytest.raises(api.AAError, match="device"):
             call()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("lr,factor,wd", [(1e-5, None, 1e-2), (1e-5, 0.5, 1e-2), (1e-4, None, 1e-3), (1e-3, 0.01, 1e-3)])
+def test_a_small_decay_is_right_on_average(lr, factor, wd, bits):
+    """lr weight_decay of about a rounding of the parameters.  A new parameter is rounded once, by half a step at most, to either
+    side as often (the gradient's step, of many roundings and different everywhere, lies between): over n elements the mean
+    decay, sum sign(p) (got - want) / sum |p|, is off by at most 6 deviations of those, 6 2^-24 sqrt(sum p^2) / sum |p|, and
+    8 U of the decay and of the step's mean."""
+    n = 1 << 19
+    cfg = (F(lr), CFG[1], CFG[2], CFG[3], F(wd))
+    x = Tensor(n, F32, None, bits, seed=11)
+    old, _ = update([x], 9, cfg=cfg, lr_factor=factor)
+    p, g, m, v = old[0]
+    f = 1.0 if factor is None else F(factor)
+    want = R.adamw(p, g, m, v, 10, cfg, 1.0, lr_factor=f)[0]
+    drift = (np.sign(p) * (f64(x.p) - want)).sum() / np.abs(p).sum()
+    decay = cfg[0] * f * cfg[4]
+    deviation = 6 * 2.0 ** -24 * np.sqrt((p * p).sum()) / np.abs(p).sum()
+    assert deviation < decay / 8   # (it would be seen)
+    assert abs(drift) <= deviation + 8 * U32 * (decay + cfg[0] * f * 6), (drift, decay, deviation)
