@@ -88,18 +88,22 @@ __device__ __forceinline__ Eight load_grad(const TensorEntry &e, int64_t i, int 
   return load_some<PASSING>(static_cast<const float *>(e.grad) + i, n);
 }
 
+// Whether the call's numbers are the table's.
+__device__ __forceinline__ bool is_table(const AdamWArgs &a) {
+  const int32_t *numbers = reinterpret_cast<const int32_t *>(a.table);
+  return numbers[0] == (int32_t)a.n_chunks && numbers[1] == a.n_tensors;
+}
+
 // Calls work(tensor's number, its entry, first and last element) for the parts of tensors in this block's chunks, a run of
-// neighbouring ones: what is known of a tensor is asked for once a part.
+// neighbouring ones: what is known of a tensor is asked for once a part.  ours: is_table().
 template <typename Work>
-__device__ __forceinline__ void walk(const AdamWArgs &a, Work work) {
-  // (numbers that are not the table's: nothing is walked; asked for with the first tensor, not before it)
-  const int chunks = reinterpret_cast<const int32_t *>(a.table)[0], tensors = reinterpret_cast<const int32_t *>(a.table)[1];
+__device__ __forceinline__ void walk(const AdamWArgs &a, bool ours, Work work) {
   const uint32_t all = (uint32_t)a.n_chunks, each = all / gridDim.x, more = all % gridDim.x;
   const int64_t begin = (int64_t)each * blockIdx.x + min(blockIdx.x, more);
   const int64_t end = begin + each + (blockIdx.x < more ? 1 : 0);
   for (int64_t c = begin; c < end;) {
     const int of_chunk = reinterpret_cast<const int32_t *>(a.table + a.map)[c];
-    if (chunks != (int)a.n_chunks || tensors != a.n_tensors) return;
+    if (!ours) return;  // (nothing is walked; known only after the first tensor has been asked for)
     const int tensor = __builtin_amdgcn_readfirstlane(of_chunk);
     const TensorEntry &e = reinterpret_cast<const TensorEntry *>(a.table + kTableEntries)[tensor];
     const int64_t next = e.first_chunk + (e.n + kChunk - 1) / kChunk, to = next < end ? next : end;
@@ -163,7 +167,8 @@ __global__ __launch_bounds__(256) void k_grad_norm(const AdamWArgs a) {
   __shared__ int last;
   double *parts = reinterpret_cast<double *>(a.table + kTableParts);
   double sum = 0.0;
-  walk(a, [&](int, const TensorEntry &e, int64_t from, int64_t to) {
+  const bool ours = is_table(a);
+  walk(a, ours, [&](int, const TensorEntry &e, int64_t from, int64_t to) {
     if (e.grad_dtype == AA_BF16) sum += squares(static_cast<const __bf16 *>(e.grad), from, to);
     else if (e.grad_dtype == AA_F16) sum += squares(static_cast<const _Float16 *>(e.grad), from, to);
     else sum += squares(static_cast<const float *>(e.grad), from, to);
@@ -190,9 +195,10 @@ __global__ __launch_bounds__(256) void k_grad_norm(const AdamWArgs a) {
   __syncthreads();
   if (threadIdx.x != 0) return;
   const float scale = a.scale ? *a.scale : 1.f;
+  // (the factor of a norm that is not finite, or of another table's gradients, leaves the update out)
   const float norm = (float)(sqrt(room[0] + room[1] + room[2] + room[3]) * fabs((double)scale));
   a.out[0] = norm;
-  a.out[1] = !(norm < __builtin_inff()) ? __builtin_nanf("") : norm > a.max_norm ? scale * (a.max_norm / norm) : scale;
+  a.out[1] = !ours || !(norm < __builtin_inff()) ? __builtin_nanf("") : norm > a.max_norm ? scale * (a.max_norm / norm) : scale;
 }
 
 // What all elements of an update have in common (decay: lr weight_decay).
@@ -331,8 +337,9 @@ template <bool PASSING>
 __global__ __launch_bounds__(256) void k_adamw_step(const AdamWArgs a) {
   const int32_t before = *a.t;
   const float factor = a.grad_factor ? *a.grad_factor : 1.f;
-  // an empty batch, or gradients that are not finite: nothing changes
-  const bool skip = (a.count && *a.count <= 0) || !(fabsf(factor) < __builtin_inff());
+  // an empty batch, gradients that are not finite, or another table's numbers: nothing changes
+  const bool ours = is_table(a);  // (asked for with the others)
+  const bool skip = (a.count && *a.count <= 0) || !(fabsf(factor) < __builtin_inff()) || !ours;
   // The counter's new value is stored by the last block to come here: all waves of all have read the old one then.
   asm volatile("" ::"s"(before));
   __syncthreads();
@@ -351,7 +358,7 @@ __global__ __launch_bounds__(256) void k_adamw_step(const AdamWArgs a) {
   s.k0 = (uint32_t)a.cfg.seed;
   s.k1 = (uint32_t)(a.cfg.seed >> 32);
   s.t = (uint32_t)before + 1u;
-  walk(a, [&](int tensor, const TensorEntry &e, int64_t from, int64_t to) {
+  walk(a, true, [&](int tensor, const TensorEntry &e, int64_t from, int64_t to) {
     const float decay = s.decay * e.decay;
     if (e.bits == 32) {
       for (int64_t i = from + threadIdx.x * 8; i < to; i += 256 * 8) {

@@ -411,3 +411,26 @@ def test_a_small_decay_is_right_on_average(lr, factor, wd, bits):
     deviation = 6 * 2.0 ** -24 * np.sqrt((p * p).sum()) / np.abs(p).sum()
     assert deviation < decay / 8   # (it would be seen)
     assert abs(drift) <= deviation + 8 * U32 * (decay + cfg[0] * f * 6), (drift, decay, deviation)
+
+
+def test_numbers_of_another_table_count_no_update():
+    """A call whose numbers of tensors or chunks are not the table's is no update: the counter stays, and the factor that the norm
+    hands out leaves a following update out, too."""
+    x = [Tensor(5000, F32, BF16, seed=1), Tensor(300, BF16, BF16, 8, seed=2)]
+    table = api.AdamWTable([k.listed() for k in x])
+    kept = [t.clone() for k in x for t in (k.p, k.copy, k.m.view(torch.uint8), k.v.view(torch.uint8))]
+    t, out = torch.tensor([4], dtype=torch.int32, device="cuda"), torch.zeros(2, device="cuda")
+    for tensors, chunks in ((1, table.chunks), (2, table.chunks - 1), (2, 0), (1, 0)):
+        other = type("Other", (), dict(ptr=table.ptr, bytes=table.bytes, device=table.device, n=tensors, chunks=chunks))
+        api.adamw_step(other, CFG_ALONE, None, None, None, t)
+        assert int(t.item()) == 4
+        out.fill_(7.0)
+        api.grad_norm(other, 1.0, None, out)
+        assert np.isnan(f64(out)[1])
+        api.adamw_step(table, CFG_ALONE, None, out[1:], None, t)
+        assert int(t.item()) == 4
+    assert all(torch.equal(a, b) for a, b in zip(kept, [t for k in x for t in (k.p, k.copy, k.m.view(torch.uint8), k.v.view(torch.uint8))]))
+    # the table's own numbers still count
+    api.adamw_step(table, CFG_ALONE, None, None, None, t)
+    api.grad_norm(table, 1.0, None, out)
+    assert int(t.item()) == 5 and np.isfinite(f64(out)).all()
