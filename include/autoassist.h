@@ -618,8 +618,8 @@ int32_t aa_adamw_table(const aa_adamw_tensor *tensors, int32_t n_tensors, void *
 
 /* Norm of all gradients together, and the factor that an update takes them with:
  *   out[0] = |s| sqrt(sum g^2),  out[1] = s min(1, max_norm / out[0]),  s = *scale (device scalar; NULL: 1).
- * Sums are held in 64 bits.  out[1] is NaN if the norm is not finite, or if n_tensors or n_chunks is not the table's (out[0] is then that
- * of no gradients, 0): aa_adamw_step then leaves everything as it is.
+ * Sums are held in 64 bits.  out[1] is NaN if the norm is not finite, or if n_tensors or n_chunks is not the
+ * table's (out[0] is 0 then, that of no gradients): aa_adamw_step then leaves everything as it is.
  * max_norm > 0 (infinity: no clipping). */
 int32_t aa_grad_norm(void *table, size_t table_bytes, int32_t n_tensors, int64_t n_chunks, float max_norm,
                      const float *scale, float *out, void *stream);

@@ -36,6 +36,11 @@ class Norm:
                             *self.grads, False, self.ws)
 
 
+def _need_kept(part):
+    if not part.kept:
+        raise api.AAError("backward: what the last forward kept is needed, and it ran without train=True or not at all")
+
+
 class Dense:
     """act(w x + bias) for up to n_max rows: w [d_out, d_in] (gated: [2 d_out, d_in]) in dtype, bias in fp32."""
 
@@ -44,7 +49,7 @@ class Dense:
         wide = 2 * d_out if act == "gated" else d_out
         g = torch.Generator(device=device)
         g.manual_seed(seed)
-        self.n_max, self.act = n_max, act
+        self.n_max, self.act, self.kept = n_max, act, False
         self.w = (torch.randn(wide, d_in, generator=g, device=device) * d_in ** -0.5).to(dtype)
         self.bias = z(wide, t=torch.float32)
         self.grads = [z(wide, d_in, t=torch.float32), z(wide, t=torch.float32)]
@@ -64,10 +69,14 @@ class Dense:
         return x[:self.n_max]
 
     def forward(self, x, count, out, train=True):
+        """train=False: nothing is kept for backward."""
+        self.kept = False
         api.linear(self._rows(x, "x"), self.w, self.bias, self.act, None, count, out, self.pre if train else None)
+        self.kept = train
 
     def backward(self, x, count, dout, dx=None):
-        """Gradients of the last forward with train=True of the same x and count: self.grads, and of x into dx."""
+        """Gradients of the last forward of the same x and count, which was one with train=True: self.grads, and of x into dx."""
+        _need_kept(self)
         x, dout = self._rows(x, "x"), self._rows(dout, "dout")
         api.linear_grad(dout, self.act, self.pre, count, self.dpre, self.grads[1], False, self.ws)
         dpre = dout if self.dpre is None else self.dpre
@@ -150,8 +159,7 @@ class ExpertBlock:
     def backward(self, x, count, step, dout, dx):
         """Gradients of the last forward of the same x, count and step, which was one with train=True: self.grads, and of x
         into dx."""
-        if not self.kept:
-            raise api.AAError("backward: what the last forward kept is needed, and it ran without train=True or not at all")
+        _need_kept(self)
         offsets, order, slot = self.plan
         d_router, d_gate_up, d_down = self.grads[:3]
         below = x
@@ -216,6 +224,8 @@ class Boss:
 
     def backward(self, x, count, step, dout):
         """Gradients of the last forward of the same x, count and step, which was one with train=True, into grads."""
+        for part in [self.enter] + self.blocks + [self.leave]:  # (before any gradient is written)
+            _need_kept(part)
         here, there = self.dx
         self.leave.backward(self.norm.out, count, dout, self.dnorm)
         self.norm.backward(self.x[-1], count, self.dnorm, None, here)

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from paper_1905_03381_amd import api
-from paper_1905_03381_amd.boss import ExpertBlock
+from paper_1905_03381_amd.boss import Boss, Dense, ExpertBlock
 
 CALLS = ["expert_forward", "route", "expert_combine", "expert_combine_grad", "expert_grad_weight", "expert_grad_input",
          "route_grad", "dropout"]
@@ -75,3 +75,55 @@ def test_wrong_arguments_are_this_librarys_error(call):
     """Tensors of other dimensions, on the host, none at all: AAError, not what Python says about their shapes."""
     with pytest.raises(api.AAError):
         call()
+
+
+AROUND = ["layer_norm", "layer_norm_grad", "linear", "linear_grad", "balance", "balance_grad"]
+
+
+@pytest.fixture
+def all_made(made, monkeypatch):
+    """The same with the calls around a block."""
+    monkeypatch.setattr(api, "LayerWorkspace", lambda *a, **k: None)
+    for name in AROUND:
+        monkeypatch.setattr(api, name, lambda *a, _name=name: made.append((_name, a)))
+    return made
+
+
+@pytest.mark.parametrize("act", ["none", "gelu", "gated"])
+def test_a_dense_layers_backward_needs_the_last_forward_to_have_trained(all_made, act):
+    """`pre` of another batch's forward would be mixed with these rows."""
+    layer, x, out = Dense(8, 16, 12, act, device="cpu"), rows(8), rows(8, 12)
+    count = torch.tensor([8], dtype=torch.int32)
+    with pytest.raises(api.AAError):
+        layer.backward(x, count, out)
+    layer.forward(x, count, out)
+    layer.backward(x, count, out)
+    layer.backward(x, count, out)
+    layer.forward(x, count, out, train=False)
+    all_made.clear()
+    with pytest.raises(api.AAError):
+        layer.backward(x, count, out)
+    assert not all_made
+
+
+@pytest.mark.parametrize("layers", [0, 1, 2])
+def test_a_models_backward_is_refused_before_any_gradient_is_written(all_made, layers):
+    model = Boss(8, 16, 24, 12, 3, 4, 2, layers=layers, device="cpu", balance=0.1)
+    x, out, count = rows(8), rows(8, 3), torch.tensor([8], dtype=torch.int32)
+    with pytest.raises(api.AAError):
+        model.backward(x, count, 0, out)
+    assert not all_made
+    model.forward(x, count, 0, out)
+    model.backward(x, count, 0, out)
+    model.forward(x, count, 0, out, train=False)
+    all_made.clear()
+    with pytest.raises(api.AAError):
+        model.backward(x, count, 0, out)
+    assert not all_made
+    # a part of it that has run for something else in between
+    model.forward(x, count, 0, out)
+    model.enter.forward(x, count, model.x[0], train=False)
+    all_made.clear()
+    with pytest.raises(api.AAError):
+        model.backward(x, count, 0, out)
+    assert not all_made
