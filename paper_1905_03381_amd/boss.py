@@ -156,9 +156,11 @@ class ExpertBlock:
                         self.balance_ws)
         self.kept = train
 
-    def backward(self, x, count, step, dout, dx):
+    def backward(self, x, count, step, dout, dx, loss_scale=None):
         """Gradients of the last forward of the same x, count and step, which was one with train=True: self.grads, and of x
-        into dx."""
+        into dx.  loss_scale: a float32 tensor of one, the factor that dout has been given (None: 1); the balance losses'
+        gradients are given it, too.  In f16 they need one: of a pool of thousands of rows a logit's is below the type's
+        smallest step."""
         _need_kept(self)
         offsets, order, slot = self.plan
         d_router, d_gate_up, d_down = self.grads[:3]
@@ -172,7 +174,7 @@ class ExpertBlock:
         api.expert_grad_weight(self.dpre, x, order, self.top_k, offsets, d_gate_up, False, self.ws)
         api.expert_grad_input(self.dpre, offsets, self.gate_up, "none", None, self.dx_pairs)
         if self.balance:
-            api.balance_grad(self.logits, count, self.cfg, self.ids, self.dweights, self.counts, *self.balance, None,
+            api.balance_grad(self.logits, count, self.cfg, self.ids, self.dweights, self.counts, *self.balance, loss_scale,
                              self.dlogits)
         else:
             api.route_grad(self.logits, count, self.cfg, self.ids, self.dweights, self.dlogits)
@@ -222,15 +224,16 @@ class Boss:
             block.forward(below, count, step, above, train)
         self.leave.forward(self.norm.forward(self.x[-1], count), count, out, train)
 
-    def backward(self, x, count, step, dout):
-        """Gradients of the last forward of the same x, count and step, which was one with train=True, into grads."""
+    def backward(self, x, count, step, dout, loss_scale=None):
+        """Gradients of the last forward of the same x, count and step, which was one with train=True, into grads; loss_scale as
+        in ExpertBlock."""
         for part in [self.enter] + self.blocks + [self.leave]:  # (before any gradient is written)
             _need_kept(part)
         here, there = self.dx
         self.leave.backward(self.norm.out, count, dout, self.dnorm)
         self.norm.backward(self.x[-1], count, self.dnorm, None, here)
         for block, below in zip(self.blocks[::-1], self.x[-2::-1]):
-            block.backward(below, count, step, here, there)
+            block.backward(below, count, step, here, there, loss_scale)
             here, there = there, here
         self.enter.backward(x, count, here)
 
@@ -266,7 +269,7 @@ class AdamW:
 
     def step(self, count=None, lr_factor=None, grad_scale=None):
         """count: the batch's rows, with none of them nothing changes; lr_factor, grad_scale: float32 tensors of one, factors
-        of the step size and of the gradients."""
+        of the step size and of the gradients (1 / loss_scale after a backward that had one)."""
         factor = grad_scale
         if self.max_norm is not None:
             api.grad_norm(self.table, self.max_norm, grad_scale, self.norm)

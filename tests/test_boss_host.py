@@ -127,3 +127,14 @@ def test_a_models_backward_is_refused_before_any_gradient_is_written(all_made, l
     with pytest.raises(api.AAError):
         model.backward(x, count, 0, out)
     assert not all_made
+
+
+def test_a_loss_scale_reaches_the_balance_losses(all_made):
+    model = Boss(8, 16, 24, 12, 3, 4, 2, device="cpu", balance=0.1)
+    x, out, count, scale = rows(8), rows(8, 3), torch.tensor([8], dtype=torch.int32), torch.tensor([8.0])
+    for given in (None, scale):
+        model.forward(x, count, 0, out)
+        all_made.clear()
+        model.backward(x, count, 0, out, loss_scale=given)
+        dloss = [args[8] for name, args in all_made if name == "balance_grad"]
+        assert len(dloss) == 2 and all(d is given for d in dloss)

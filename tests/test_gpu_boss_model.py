@@ -9,6 +9,7 @@ import numpy as np
 import pytest
 import torch
 
+import layers_ref as R
 from layers_ref import BF16, F16, F32, U32, check, device_count, f64, normal
 from paper_1905_03381_amd import api
 from paper_1905_03381_amd.boss import AdamW, Boss, ExpertBlock
@@ -182,3 +183,49 @@ def test_the_workload_runs(capsys):
     got = json.loads(capsys.readouterr().out.strip().splitlines()[-1])
     assert len(got["stages"]) == 5 and got["kept_per_pool"] > 0
     assert all(np.isfinite(v) for v in [got["loss_first"], got["loss_last"]] + sum(got["balance_loss"], []))
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 16, 2.0 ** 10])
+@pytest.mark.parametrize("norm", [False, True])
+def test_the_balance_loss_follows_a_loss_scale(norm, scale):
+    """f16, a pool whose balance gradient (1e-7 a logit here) is a step of the type or two: scaled with the loss it is as
+    exact as any.  dout is 0, so that the router's gradient is the balance's alone: each logit's is off by half a step and what
+    32 bits lose, 256 U at most, and the sum over m rows by m U of its terms."""
+    n, m, d, E, K = 4200, 4096, 64, 16, 2
+    block = ExpertBlock(n, d, 32, E, K, dtype=F16, balance=0.01, z_loss=1e-6, norm=norm)
+    x, cnt = normal((n, d), F16, 3).cuda(), device_count(m)
+    block.forward(x, cnt, 0, torch.zeros_like(x))
+    block.backward(x, cnt, 0, torch.zeros_like(x), torch.zeros_like(x), loss_scale=torch.tensor([scale], device="cuda"))
+    logits, rows = f64(block.logits)[:m], f64(block.norm.out if norm else x)[:m]
+    dl = R.balance_grad(logits, "softmax", f64(block.counts), K, float(np.float32(0.01)), float(np.float32(1e-6)))
+    assert np.abs(dl).max() < 2e-6
+    off = R.half_step(F16) * np.abs(dl) + R.tiny(F16) / scale + 256 * U32 * np.abs(dl).max(1, keepdims=True)
+    want, size = dl.T @ rows, np.abs(dl).T @ np.abs(rows)
+    check(f64(block.grads[0])[0] / scale, want, off.T @ np.abs(rows) + (m + 64) * U32 * size, "router")
+
+
+def test_gradients_under_a_loss_scale_are_as_many_times_larger():
+    """A power of two moves no digits (bf16 has the range): bit by bit, in all of the model."""
+    n, scale = 150, 8.0
+    x, dout, cnt = normal((n, 24), BF16, 3).cuda(), normal((n, 2), BF16, 4).cuda(), device_count(140)
+    a, b = (Boss(n, 24, 64, 32, 2, 8, 2, balance=0.1, z_loss=0.01) for _ in range(2))
+    for model in (a, b):
+        model.forward(x, cnt, 0, torch.zeros_like(dout))
+    a.backward(x, cnt, 0, dout)
+    b.backward(x, cnt, 0, dout * scale, loss_scale=torch.tensor([scale], device="cuda"))
+    for g, h in zip(a.grads, b.grads):
+        assert torch.equal(g * scale, h)
+
+
+def test_an_update_of_scaled_gradients_is_the_unscaled():
+    """grad_scale = 1 / loss_scale gives them back."""
+    n, scale = 64, 1024.0
+    x, dout, cnt = normal((n, 24), BF16, 3).cuda(), normal((n, 2), BF16, 4).cuda(), device_count(n)
+    models = [small_model(n) for _ in range(2)]
+    opts = [AdamW(m, 1e-2, weight_decay=0.1, max_norm=0.5) for m in models]
+    for model, opt, s in zip(models, opts, (1.0, scale)):
+        model.forward(x, cnt, 0, torch.zeros_like(dout))
+        model.backward(x, cnt, 0, dout * s, loss_scale=torch.tensor([s], device="cuda"))
+        opt.step(cnt, grad_scale=torch.tensor([1 / s], device="cuda"))
+    for v, w in zip(opts[0].masters, opts[1].masters):
+        assert torch.equal(v, w)
