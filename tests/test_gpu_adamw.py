@@ -434,3 +434,14 @@ def test_numbers_of_another_table_count_no_update():
     api.adamw_step(table, CFG_ALONE, None, None, None, t)
     api.grad_norm(table, 1.0, None, out)
     assert int(t.item()) == 5 and np.isfinite(f64(out)).all()
+
+
+@pytest.mark.parametrize("bits,grad", [(32, F32), (8, BF16)])
+def test_more_than_the_caches_hold(bits, grad):
+    """8192 chunks and more, an odd end."""
+    n = 8200 * 2048 + 1931
+    x = Tensor(n, grad, BF16, bits, seed=6)
+    old, t = update([Tensor(77), x], 9)
+    assert t == 10
+    x.check(1, old[1], 10)
+    assert (f64(x.p.as_strided((3,), (1,), n)) == 0).all() and (f64(x.copy.as_strided((3,), (1,), n)) == 0).all()

@@ -266,3 +266,48 @@ def test_after_the_routing():
     side.synchronize()
     assert (got[0].cpu().numpy() == np.diff(offsets.cpu().numpy())).all()
     check_balance(x, ids, "softmax", None, got)
+
+
+def routing_gradient(x, ids, kind, dweights, scale):
+    """Of renormalised weights in 64 bits, relative to the highest choice; 0 where the scores' sum is 0 in 64 bits."""
+    out = np.zeros_like(x)
+    for t in range(len(x)):
+        c = [e for e in ids[t] if e >= 0]
+        v = x[t, c] if kind == "softmax" else np.minimum(x[t, c], 0.0)
+        if v.max() - (x[t].max() if kind == "softmax" else 0.0) < -745.2:
+            continue
+        z = 1 / (1 + np.exp(-np.abs(x[t, c])))
+        s = np.exp(v - v.max()) * (1.0 if kind == "softmax" else z)
+        w, g = s / s.sum(), dweights[t, :len(c)] * scale
+        rest = 1.0 if kind == "softmax" else np.where(x[t, c] > 0, 1 - z, z)
+        out[t, c] = w * rest * (g - (w * g).sum())
+    return out
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("E,K", [(5, 2), (16, 3), (32, 4), (60, 6), (128, 8), (256, 16), (64, 20), (200, 17), (300, 9), (1024, 40)])
+def test_grad_of_choices_far_below_the_others(E, K, dtype, kind):
+    """Renormalised choices (by a bias) that are 45 to 700 below the row's best, nothing in 32 bits beside them, or 800, nothing
+    in 64; rows of ordinary choices between them."""
+    n, scale = 70, 1.5
+    x, g = normal((n, E), torch.float64, E, 1.5), torch.Generator().manual_seed(E)
+    ids = torch.stack([torch.randperm(E, generator=g)[:K] for _ in range(n)])
+    for t in range(n):
+        deep = [0, 45, 90, 300, 700, 800][t % 6]
+        if deep:
+            x[t, ids[t]] = -deep + normal((K,), torch.float64, 100 + t)
+    x = x.to(dtype)
+    dweights = normal((n, K), F32, 8, 0.01)
+    counts = R.choices(ids.numpy(), E)
+    out = torch.full((n, E), 7.0, dtype=dtype, device="cuda")
+    api.balance_grad(x.cuda(), None, api.route_config(kind, K, renormalise=True, scale=scale), ids.to(torch.int32).cuda(), dweights.cuda(),
+                     torch.from_numpy(counts.astype(np.int32)).cuda(), 0.5, 0.25, None, out)
+    x64, dw = f64(x), f64(dweights)
+    route = routing_gradient(x64, ids.numpy(), kind, dw, scale)
+    assert (np.abs(route[2::6]).max(1) > 1e-5).all() and (np.abs(route[4::6]).max(1) > 1e-5).all() and (route[5::6] == 0).all()
+    want = R.balance_grad(x64, kind, counts.astype(float), K, 0.5, 0.25) + route
+    # (a weight: an exponential of a difference of up to 10, a sum of K, a quotient)
+    mag = scale * np.abs(dw).sum(1, keepdims=True)
+    bound = grad_bound(x64, kind, counts.astype(float), K, 0.5, 0.25, 1.0, dtype, want)
+    check(out, want, bound + (64 + K) * U32 * mag, "dlogits")

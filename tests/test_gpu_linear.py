@@ -324,3 +324,33 @@ def test_grad_of_what_is_not_a_number(n, d, act):
         ill = np.concatenate([ill, ill], 1) if act == "gated" else ill
         assert (np.isnan(f64(dpre)) == ill).all()
         assert (np.isnan(f64(dbias)) == ill.any(0)).all()
+
+
+@pytest.mark.parametrize("act,n,d_in,d_out", [("gated", 16_500, 24, 4100), ("gelu", 8300, 40, 8200)])
+def test_results_past_the_caches(act, n, d_in, d_out):
+    """Out and pre of 128 MB or more on 16-byte boundaries, last rows and columns of a tile in part."""
+    layer = Layer(n, d_in, d_out, act, BF16, count=n - 3)
+    ld, ldp = -(-d_out // 8) * 8, -(-layer.wide // 8) * 8
+    assert n * d_out * 2 >= 128 << 20 and n * layer.wide * 2 >= 128 << 20
+    # (one storage each, a row more than there are)
+    out = torch.full((n + 1, ld), 77.0, dtype=BF16, device="cuda")
+    pre = torch.full((n + 1, ldp), 77.0, dtype=BF16, device="cuda")
+    assert out.data_ptr() % 16 == 0 and pre.data_ptr() % 16 == 0
+    api.linear(layer.x, layer.w, layer.bias, act, None, device_count(n - 3), out[:n, :d_out], pre[:n, :layer.wide])
+    torch.cuda.synchronize()
+    whole = layer.x
+    for lo in range(0, n, 1000):
+        hi = min(lo + 1000, n)
+        layer.x, layer.count = whole[lo:hi], min(hi, n - 3) - lo
+        layer.check(out[lo:hi, :d_out], pre[lo:hi, :layer.wide])
+    assert (out[n:] == 77).all() and (pre[n:] == 77).all() and (out[:, d_out:] == 77).all() and (pre[:, layer.wide:] == 77).all()
+
+
+@pytest.mark.parametrize("act,n,d", [("gelu", 16_500, 1032), ("gated", 9000, 1880), ("none", 5001, 3360)])
+def test_grad_of_many_rows(act, n, d):
+    """16 M elements and more in whole lines."""
+    assert d % 8 == 0 and n * d >= 16 << 20
+    dout, pre = normal((n, d), BF16, 1).cuda(), None if act == "none" else normal((n, 2 * d if act == "gated" else d), BF16, 2).cuda()
+    got = run_grad(dout, act, pre, n - 2)
+    check_grad(dout, act, pre, n - 2, got)
+    assert (f64(got[0][n - 2:]) == 77.0).all()
