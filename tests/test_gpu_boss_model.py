@@ -229,3 +229,40 @@ def test_an_update_of_scaled_gradients_is_the_unscaled():
         opt.step(cnt, grad_scale=torch.tensor([1 / s], device="cuda"))
     for v, w in zip(opts[0].masters, opts[1].masters):
         assert torch.equal(v, w)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("p", [0.0, 0.2])
+def test_the_calls_of_a_block_without_norm_and_balance(dtype, p):
+    """Its results, bit by bit, from the calls it stands for."""
+    n, m, d, f, E, K, step = 90, 77, 64, 48, 8, 2, 5
+    z = lambda *s, t=dtype: torch.zeros(*s, dtype=t, device="cuda")
+    x, dout, cnt = normal((n, d), dtype, 3).cuda(), normal((n, d), dtype, 4).cuda(), device_count(m)
+    block, out, dx = ExpertBlock(n, d, f, E, K, dtype=dtype, p=p), z(n, d), z(n, d)
+    block.forward(x, cnt, step, out)
+    block.backward(x, cnt, step, dout, dx)
+    router, gate_up, down = block.weights()
+    ws, one = api.ExpertWorkspace(n, K, E), torch.tensor([0, m], dtype=torch.int32, device="cuda")
+    logits, ids, weights = z(n, E), z(n, K, t=torch.int32), z(n, K, t=F32)
+    offsets, order, slot = z(E + 1, t=torch.int32), z(n * K, t=torch.int32), z(n, K, t=torch.int32)
+    h, pre, y, o = z(n * K, f), z(n * K, 2 * f), z(n * K, d), z(n, d)
+    api.expert_forward(x, None, 1, one, router, "none", logits)
+    api.route(logits, cnt, None, block.cfg, ids, weights, (offsets, order, slot), ws)
+    api.expert_forward(x, order, K, offsets, gate_up, "gated", h, pre)
+    api.expert_forward(h, None, 1, offsets, down, "none", y)
+    api.expert_combine(y, slot, weights, cnt, x, p, block.seed, step, o)
+    assert torch.equal(out, o)
+    dy, dpre, pairs, of_router = z(n * K, d), z(n * K, 2 * f), z(n * K, d), z(n, d)
+    dweights, dlogits, back = z(n, K, t=F32), z(n, E), z(n, d)
+    grads = [z(*w.shape, t=F32) for w in block.weights()]
+    api.expert_combine_grad(dout, y, slot, weights, cnt, p, block.seed, step, dy, dweights)
+    api.expert_grad_weight(dy, h, None, 1, offsets, grads[2], False, ws)
+    api.expert_grad_input(dy, offsets, down, "gated", pre, dpre)
+    api.expert_grad_weight(dpre, x, order, K, offsets, grads[1], False, ws)
+    api.expert_grad_input(dpre, offsets, gate_up, "none", None, pairs)
+    api.route_grad(logits, cnt, block.cfg, ids, dweights, dlogits)
+    api.expert_grad_weight(dlogits, x, None, 1, one, grads[0], False, ws)
+    api.expert_grad_input(dlogits, one, router, "none", None, of_router)
+    api.dropout(of_router, cnt, dout, 0.0, 0, 0, back)
+    api.expert_combine(pairs, slot, None, cnt, back, 0.0, 0, 0, back)
+    assert torch.equal(dx, back) and all(torch.equal(a, b) for a, b in zip(block.grads, grads))
