@@ -26,6 +26,7 @@ struct ProductArgs {
   float *partial;   // grad_weight: room for the parts of a split sum
   size_t partial_bytes;
   int32_t parts;    // (chosen at launch) parts a tile's sum over rows comes in
+  int32_t odd;      // (set at launch) rows of out or pre may begin inside a word of four bytes
   // dense layer: one group, rows [0, m) by count; the rows' bias and residual (NULL: none)
   const int32_t *count;
   const float *bias;

@@ -288,7 +288,7 @@ __global__ __launch_bounds__(kFewWaves *kWave) void k_dense_few(const ProductArg
 #pragma unroll
   for (int m = 0; m < MF; ++m) {
     const int q = q0 + m * 16 + (lane & 15);
-    if (q < rows) finish<T, kForward, ACT, true>(a, q, c, four_columns(acc[0][m]), four_columns(acc[NF - 1][m]));
+    if (q < rows) finish<T, kForward, ACT, true, false>(a, q, c, four_columns(acc[0][m]), four_columns(acc[NF - 1][m]));
   }
 }
 

@@ -343,13 +343,14 @@ __device__ __forceinline__ void store_run(T *p, const Run<N> &x, int n) {
   }
 }
 
-template <typename T, int N>
+// WORDS: rows of odd widths, half of which begin inside a word of four bytes.
+template <bool WORDS, typename T, int N>
 __device__ __forceinline__ void store_dense(bool passing, T *p, const Run<N> &x, int n) {
   if (passing) {
     store_run<T, N, true>(p, x, n);
     return;
   }
-  if constexpr (N == 8) {  // (rows of odd widths: half of them begin inside a word of four bytes)
+  if constexpr (WORDS && N == 8) {
     if (n >= 8 && (reinterpret_cast<uintptr_t>(p) & 2)) {
       Line<T> t;
 #pragma unroll
@@ -406,7 +407,7 @@ __device__ __forceinline__ float gelu_argument(float x) {
 }
 
 // Neighbouring results of place q, column j on (j < width): through the activation and out.
-template <typename T, int MODE, int ACT, bool DENSE, int N>
+template <typename T, int MODE, int ACT, bool DENSE, bool WORDS, int N>
 __device__ __forceinline__ void finish(const ProductArgs &a, int64_t q, int j, const Run<N> &v, const Run<N> &up) {
   T *o = static_cast<T *>(a.out) + q * a.ldo + j;
   const int n = (MODE == kForward ? a.d_out : a.d_in) - j;
@@ -420,14 +421,14 @@ __device__ __forceinline__ void finish(const ProductArgs &a, int64_t q, int j, c
 #pragma unroll
       for (int i = 0; i < N; ++i) r.v[i] = v.v[i] * sigmoid_near(ACT == AA_ACT_GELU ? gelu_argument(v.v[i]) : v.v[i]);
     }
-    if (DENSE && ACT != AA_ACT_GATED && a.pre) store_dense(a.passing_pre, static_cast<T *>(a.pre) + q * a.ldpre + j, v, n);
+    if (DENSE && ACT != AA_ACT_GATED && a.pre) store_dense<WORDS>(a.passing_pre, static_cast<T *>(a.pre) + q * a.ldpre + j, v, n);
     if (ACT == AA_ACT_GATED) {
 #pragma unroll
       for (int i = 0; i < N; ++i) r.v[i] = v.v[i] * (DENSE ? sigmoid_near(v.v[i]) : sigmoid_fast(v.v[i])) * up.v[i];
       if (a.pre) {
         T *h = static_cast<T *>(a.pre) + q * a.ldpre + j;
-        store_dense(DENSE && a.passing_pre, h, v, n);
-        store_dense(DENSE && a.passing_pre, h + a.d_out, up, n);
+        store_dense<WORDS>(DENSE && a.passing_pre, h, v, n);
+        store_dense<WORDS>(DENSE && a.passing_pre, h + a.d_out, up, n);
       }
     }
     if (DENSE && a.residual) {
@@ -459,7 +460,7 @@ __device__ __forceinline__ void finish(const ProductArgs &a, int64_t q, int j, c
     }
     store_run(o + a.d_in, du, n);
   }
-  store_dense(DENSE && a.passing, o, r, n);
+  store_dense<WORDS>(DENSE && a.passing, o, r, n);
 }
 
 template <typename T, int N>
@@ -786,33 +787,43 @@ __global__ __launch_bounds__(WI *WJ *kWave, 2) void k_product(const ProductArgs 
     const int lane = fresh_thread((int)t) & 63, group = lane >> 4;
     const int ti = done.i0 + wi * FI * 16 + (lane & 15);
     const int tj = done.j0 + wj * kOut * 16 + (kOut >= 2 ? (group & 1) * 16 + (group >> 1) * 8 : group * 4);
+    const auto write = [&](auto words) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < FI; ++i) {
-      const int r = ti + i * 16;
+      for (int i = 0; i < FI; ++i) {
+        const int r = ti + i * 16;
 #pragma unroll
-      for (int p = 0; p < kRuns; ++p) {
-        const int c = tj + p * 32;
-        const auto run = [&](int first) __attribute__((always_inline)) {
-          if constexpr (kOut >= 2) return eight_columns(acc[i][first + 2 * p], acc[i][first + 2 * p + 1]);
-          else return four_columns(acc[i][first]);
-        };
-        const auto v = run(0);
-        auto up = v;
-        if (GATED) up = run(GATED ? kOut : 0);
-        if (r < done.i_end && c < columns) {
-          if constexpr (MODE == kGradWeight) {
-            const size_t at = ((size_t)done.e * a.d_out + r) * a.d_in + c;
-            if (a.parts > 1)
-              store_run(a.partial + (done.unit * BM + (r - done.i0)) * BN + (c - done.j0), v, 8);
-            else if (a.out_f32)
-              finish_weight(static_cast<float *>(a.out) + at, v, a.d_in - c, a.accumulate);
-            else
-              finish_weight(static_cast<T *>(a.out) + at, v, a.d_in - c, a.accumulate);
-          } else {
-            finish<T, MODE, ACT, DENSE>(a, r, c, v, up);
+        for (int p = 0; p < kRuns; ++p) {
+          const int c = tj + p * 32;
+          const auto run = [&](int first) __attribute__((always_inline)) {
+            if constexpr (kOut >= 2) return eight_columns(acc[i][first + 2 * p], acc[i][first + 2 * p + 1]);
+            else return four_columns(acc[i][first]);
+          };
+          const auto v = run(0);
+          auto up = v;
+          if (GATED) up = run(GATED ? kOut : 0);
+          if (r < done.i_end && c < columns) {
+            if constexpr (MODE == kGradWeight) {
+              const size_t at = ((size_t)done.e * a.d_out + r) * a.d_in + c;
+              if (a.parts > 1)
+                store_run(a.partial + (done.unit * BM + (r - done.i0)) * BN + (c - done.j0), v, 8);
+              else if (a.out_f32)
+                finish_weight(static_cast<float *>(a.out) + at, v, a.d_in - c, a.accumulate);
+              else
+                finish_weight(static_cast<T *>(a.out) + at, v, a.d_in - c, a.accumulate);
+            } else {
+              finish<T, MODE, ACT, DENSE, decltype(words)::value>(a, r, c, v, up);
+            }
           }
         }
       }
+    };
+    // (The experts' rows that begin on words have a loop of their own: 12,002 rows of 16 groups, gradient 1000 <- 520 relu 27.8 us
+    // with the code for the others between, 27.3 without; forward 512 -> 520 12.9 and 12.6.)
+    if constexpr (MODE != kGradWeight && !DENSE) {
+      if (a.odd) write(std::true_type());
+      else write(std::false_type());
+    } else {
+      write(std::integral_constant<bool, DENSE>());
     }
     if (t >= t_end) break;
   }
@@ -950,7 +961,7 @@ __global__ __launch_bounds__(256) void k_product_few(const ProductArgs a) {
         for (int f = 0; f < kOut; ++f) {
           const int q = q0 + m * 16 + (lane & 15), c = j0 + f * 16 + (lane >> 4) * 4;
           if (q < hi && c < a.d_out)
-            finish<T, kForward, ACT, false>(a, q, c, four_columns(acc[f][m]), four_columns(acc[GATED ? f + kOut : f][m]));
+            finish<T, kForward, ACT, false, false>(a, q, c, four_columns(acc[f][m]), four_columns(acc[GATED ? f + kOut : f][m]));
         }
     }
     __syncthreads();  // (the sums are read)
@@ -998,6 +1009,8 @@ hipError_t launch_tiles(ProductArgs a, hipStream_t st) {
   } else {  // every group may end inside a tile; there are no more groups with rows than rows
     ni = a.rows_max / BM + (a.rows_max < a.n_experts ? a.rows_max : a.n_experts);
   }
+  const auto on_words = [](const void *p, int64_t ld) { return ((reinterpret_cast<uintptr_t>(p) | (uintptr_t)ld * 2) & 2) == 0; };
+  a.odd = !on_words(a.out, a.ldo) || (a.pre && (!on_words(a.pre, a.ldpre) || a.d_out % 2 != 0));
   // blocks that fit the chip at once walk the tiles
   const int64_t blocks = min(kFit, (ni * nj * a.parts + 7) / 8 * 8);
   if (blocks == 0) return hipSuccess;
