@@ -156,7 +156,9 @@ hipError_t by_act(const ActGradArgs &a, hipStream_t st) {
 // up's) of 16 MF rows; its waves share the summed dimension out in chunks of 64, straight from memory into the matrix
 // instructions' registers, kAhead of them on their way, and join their sums in LDS.  Rows are asked for whether they are in use
 // or not: the count would be waited for first.  ODD: rows that may begin inside a word of four bytes.
-// Four waves; eight or sixteen were slower (one row 4096 -> 136: 6.6, 7.2, 8.2 us).  One row 2048 -> 4096, 17 MB: 6 to 7.6 us.
+// Four waves; eight or sixteen were slower (one row 4096 -> 136: 6.6, 7.2, 8.2 us).  One row 2048 -> 4096, 17 MB: 5.2 to 7.6 us;
+// its waves wait for 75 % of that: each has eight chunks, of which kAhead are asked for before the first is there, so that memory is
+// waited for twice in turn, and then the join.
 constexpr int kFewWaves = 4;
 
 // Sixteen bytes of a row at any address.  A load that begins inside a word of four bytes takes as long as four (9 rows 4781 ->
